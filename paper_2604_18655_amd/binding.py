@@ -1,4 +1,4 @@
-"""ctypes binding of include/mlora_w4.h.  Tensors are torch CUDA(HIP) tensors used as plain
+"""ctypes binding of the headers in include/.  Tensors are torch CUDA(HIP) tensors used as plain
 device buffers; work is enqueued on torch's current stream."""
 from __future__ import annotations
 
@@ -23,6 +23,13 @@ exported_symbols = (
     "mlora_w4_layer_step_fused", "mlora_rms_scale", "mlora_lora_int16_expand",
     "mlora_ds2d_rows", "mlora_ds2d_layout", "mlora_ds2d_workspace_bytes", "mlora_ds2d_late_drafts",
     "mlora_ds2d_step",
+)
+# of mlora_rope.h, mlora_stream_cache.h and mlora_logit_rules.h: what a decoding loop does around these
+loop_symbols = (
+    "mlora_rope_frequencies", "mlora_rope_tables", "mlora_rope_apply",
+    "mlora_stream_cache_append", "mlora_stream_cache_compress",
+    "mlora_attention_mass_workspace_bytes", "mlora_attention_mass_add",
+    "mlora_logit_rules_apply",
 )
 
 
@@ -59,6 +66,43 @@ class _TreeAttnStruct(C.Structure):
                 ("len_stream", C.c_void_p),
                 ("k_new", C.c_void_p), ("v_new", C.c_void_p),
                 ("parent", C.c_void_p), ("is_forecast", C.c_void_p)]
+
+
+class _RopeStruct(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("context", C.c_double)]
+
+
+class _RopeRowsStruct(C.Structure):
+    _fields_ = [("M", C.c_int32), ("rows_per_stream", C.c_int32), ("base", C.c_void_p), ("offset", C.c_void_p),
+                ("quarter_turns", C.c_void_p)]
+
+
+class _RopeTensorStruct(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("x_row", C.c_int64), ("x_head", C.c_int64),
+                ("y_row", C.c_int64), ("y_head", C.c_int64), ("heads", C.c_int32), ("rotate", C.c_int32)]
+
+
+class _StreamCacheStruct(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_streams", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("cap", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("mass", C.c_void_p), ("slot_pos", C.c_void_p), ("len", C.c_void_p), ("next_pos", C.c_void_p),
+                ("tickets", C.c_void_p)]
+
+
+class _AttentionMassStruct(C.Structure):
+    _fields_ = [("cache", _StreamCacheStruct), ("n_q_heads", C.c_int32), ("rows_per_stream", C.c_int32),
+                ("scale", C.c_float), ("k_prefill", C.c_void_p), ("mass_prefill", C.c_void_p),
+                ("len_prefill", C.c_int32), ("decay", C.c_float)]
+
+
+class _LogitRulesStruct(C.Structure):
+    _fields_ = [("n_streams", C.c_int32), ("rows_per_stream", C.c_int32), ("tokens_per_stream", C.c_int32),
+                ("vocab", C.c_int32), ("logits_dtype", C.c_int32), ("parent", C.c_void_p), ("counts", C.c_void_p),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias", C.c_void_p), ("bias_row", C.c_void_p), ("n_bias", C.c_int32), ("masks", C.c_void_p),
+                ("mask_row", C.c_void_p), ("n_masks", C.c_int32)]
 
 
 def lib_path() -> str:
@@ -128,6 +172,24 @@ def load_library():
         lib.mlora_ds2d_late_drafts.argtypes = [dp]
         lib.mlora_ds2d_step.restype = C.c_int
         lib.mlora_ds2d_step.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        rp, cp = C.POINTER(_RopeStruct), C.POINTER(_StreamCacheStruct)
+        lib.mlora_rope_frequencies.restype = C.c_int
+        lib.mlora_rope_frequencies.argtypes = [rp, C.POINTER(C.c_double)]
+        lib.mlora_rope_tables.restype = C.c_int
+        lib.mlora_rope_tables.argtypes = [rp, C.POINTER(_RopeRowsStruct), vp, vp, vp]
+        lib.mlora_rope_apply.restype = C.c_int
+        lib.mlora_rope_apply.argtypes = [rp, C.POINTER(_RopeRowsStruct), C.POINTER(_RopeTensorStruct), i32, i32, i32, vp]
+        lib.mlora_stream_cache_append.restype = C.c_int
+        lib.mlora_stream_cache_append.argtypes = [cp, vp, vp, i32, vp, i32, i32, i32, i32, vp]
+        lib.mlora_stream_cache_compress.restype = C.c_int
+        lib.mlora_stream_cache_compress.argtypes = [cp, cp, vp, i32, i32, i32, vp]
+        mp = C.POINTER(_AttentionMassStruct)
+        lib.mlora_attention_mass_workspace_bytes.restype = sz
+        lib.mlora_attention_mass_workspace_bytes.argtypes = [mp, i32]
+        lib.mlora_attention_mass_add.restype = C.c_int
+        lib.mlora_attention_mass_add.argtypes = [mp, vp, vp, i32, vp, sz, vp]
+        lib.mlora_logit_rules_apply.restype = C.c_int
+        lib.mlora_logit_rules_apply.argtypes = [C.POINTER(_LogitRulesStruct), vp, vp, vp, i32, vp, vp]
         lib.mlora_w4_workspace_status.restype = C.c_int
         lib.mlora_w4_workspace_status.argtypes = [vp, C.POINTER(i32), vp]
         lib.mlora_w4_debug_spin_limit.restype = i32
@@ -491,3 +553,231 @@ class Ds2dStep:
                                               _ptr(accepted_rows), _ptr(emitted), _ptr(next_tokens),
                                               _ptr(workspace), n, _stream() if stream is None else stream),
                "mlora_ds2d_step")
+
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS = 0, 1, 2, 3
+_EINVAL, _ESHAPE = -1, -2
+
+
+def _buffer(t, where: str, itemsize: int, shape=None, n: Optional[int] = None) -> None:
+    """Refuses what is no dense device tensor of elements of this size, of this shape or number of elements."""
+    if not t.is_cuda or t.element_size() != itemsize or not t.is_contiguous():
+        raise MloraError(_EINVAL, where)
+    if (shape is not None and tuple(t.shape) != tuple(shape)) or (n is not None and t.numel() != n):
+        raise MloraError(_ESHAPE, where)
+
+
+class Rope:
+    """Rotary positions (mlora_rope): `rot` of head_dim features turn, in pairs of the half or the interleaved layout, by
+    frequencies that are plain, divided by factor (linear), of a larger base (base) or stretched where they turn fewer than
+    low..high times within context positions (turns).  Keeps the device table of the frequencies."""
+
+    def __init__(self, head_dim: int, rot: int, layout: int = ROPE_HALF, scaling: int = ROPE_PLAIN, theta: float = 10000.0,
+                 factor: float = 1.0, low: float = 1.0, high: float = 4.0, context: float = 8192.0, device="cuda:0"):
+        import torch
+        self.struct = _RopeStruct(int(head_dim), int(rot), int(layout), int(scaling), float(theta), float(factor),
+                                  float(low), float(high), float(context))
+        freq = (C.c_double * max(1, int(rot) // 2))()
+        _check(load_library().mlora_rope_frequencies(C.byref(self.struct), freq), "mlora_rope_frequencies")
+        self.quarter_turns = torch.tensor(list(freq), dtype=torch.float64).to(device)
+
+    def rows(self, M: int, rows_per_stream: Optional[int], base, offset) -> _RopeRowsStruct:
+        R = int(M if rows_per_stream is None else rows_per_stream)
+        if base is not None:
+            _buffer(base, "rope base", 4, n=M // max(1, R))
+        if offset is not None:
+            _buffer(offset, "rope offset", 4, n=R)
+        return _RopeRowsStruct(int(M), max(1, R), _ptr(base), _ptr(offset), _ptr(self.quarter_turns))
+
+
+class RopeTables:
+    """Marshalled arguments of mlora_rope_tables: cos and sin fp32 [M][rot / 2] of rows at base[stream] + offset[row]."""
+
+    def __init__(self, rope: Rope, cos, sin, M: int, rows_per_stream: Optional[int] = None, base=None, offset=None):
+        for t in (cos, sin):
+            _buffer(t, "mlora_rope_tables", 4, n=M * (rope.struct.rot // 2))
+        self.keep = (rope, cos, sin, base, offset)
+        self.rows = rope.rows(M, rows_per_stream, base, offset)
+        self.args = (C.byref(rope.struct), C.byref(self.rows), _ptr(cos), _ptr(sin))
+        self.fn = load_library().mlora_rope_tables
+
+    def run(self, stream: Optional[int] = None) -> None:
+        st = self.fn(*self.args, _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, "mlora_rope_tables")
+
+
+class RopeTensor:
+    """One tensor of a RopePlan: x and y [M][heads][head_dim], any strides with the features next to each other; y may be x.
+    Without rotate its rows are copied."""
+
+    def __init__(self, x, y, rotate: bool = True):
+        for t in (x, y):
+            if not t.is_cuda or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+                raise MloraError(_EINVAL, "rope tensor")
+        if x.shape != y.shape or x.dtype != y.dtype:
+            raise MloraError(_ESHAPE, "rope tensor")
+        self.x, self.y = x, y
+        self.struct = _RopeTensorStruct(_ptr(x), _ptr(y), x.stride(0), x.stride(1), y.stride(0), y.stride(1),
+                                        int(x.shape[1]), int(bool(rotate)))
+
+
+class RopePlan:
+    """Marshalled arguments of mlora_rope_apply: all tensors turned (inverse: back) in one launch."""
+
+    def __init__(self, rope: Rope, tensors: Sequence[RopeTensor], M: int, dtype: int, inverse: bool = False,
+                 rows_per_stream: Optional[int] = None, base=None, offset=None):
+        for t in tensors:
+            if t.x.shape[0] != M or t.x.shape[2] != rope.struct.head_dim:
+                raise MloraError(_ESHAPE, "mlora_rope_apply")
+            if t.x.element_size() != (2 if dtype == Y_BF16 else 4):
+                raise MloraError(_EINVAL, "mlora_rope_apply")
+        self.keep = (rope, list(tensors), base, offset)
+        self.rows = rope.rows(M, rows_per_stream, base, offset)
+        self.arr = (_RopeTensorStruct * max(1, len(tensors)))(*[t.struct for t in tensors])
+        self.args = (C.byref(rope.struct), C.byref(self.rows), self.arr, len(tensors), int(dtype), int(bool(inverse)))
+        self.fn = load_library().mlora_rope_apply
+
+    def run(self, stream: Optional[int] = None) -> None:
+        st = self.fn(*self.args, _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, "mlora_rope_apply")
+
+
+class StreamCache:
+    """The streams' cache segments of all layers (mlora_stream_cache): k and v bf16 [L][S][H][cap][head_dim], mass fp32 and
+    slot_pos int32 [L][S][H][cap], len and next_pos int32 [S].  k[l], v[l] and len are what TreeAttention takes as
+    k_stream, v_stream and len_stream.  Made outside of a graph capture (its tickets are uploaded here)."""
+
+    def __init__(self, k, v, mass, slot_pos, len, next_pos):
+        import torch
+        if k.dim() != 5:
+            raise MloraError(_ESHAPE, "stream cache")
+        L, S, H, cap, D = (int(x) for x in k.shape)
+        for t in (k, v):
+            _buffer(t, "stream cache", 2, (L, S, H, cap, D))
+        for t in (mass, slot_pos):
+            _buffer(t, "stream cache", 4, (L, S, H, cap))
+        for t in (len, next_pos):
+            _buffer(t, "stream cache", 4, (S,))
+        self.k, self.v, self.mass, self.slot_pos, self.len, self.next_pos = k, v, mass, slot_pos, len, next_pos
+        self.tickets = torch.zeros(S, dtype=torch.int32).to(k.device)        # (an upload: done when it returns)
+        self.shape = (L, S, H, cap, D)
+        self.struct = _StreamCacheStruct(L, S, H, D, cap, _ptr(k), _ptr(v), _ptr(mass), _ptr(slot_pos), _ptr(len),
+                                         _ptr(next_pos), _ptr(self.tickets))
+        self.ref = C.byref(self.struct)
+
+    def append(self, k_new, v_new, rows_per_stream: int, rows, budget: int, sink: int = 0, recent: int = 0,
+               stream: Optional[int] = None) -> None:
+        """Listed rows (int32 [S][n], None: all) of k_new and v_new bf16 [L][S * rows_per_stream][H][head_dim] enter the
+        caches; beyond the budget they take the slots of the lowest rank."""
+        L, S, H, _, D = self.shape
+        n = L * S * rows_per_stream * H * D
+        _buffer(k_new, "mlora_stream_cache_append", 2, n=n)
+        _buffer(v_new, "mlora_stream_cache_append", 2, n=n)
+        listed = 0
+        if rows is not None:
+            listed = rows.numel() // S
+            _buffer(rows, "mlora_stream_cache_append", 4, n=S * listed)
+        st = load_library().mlora_stream_cache_append(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
+                                                      _ptr(rows), listed, budget, sink, recent,
+                                                      _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, "mlora_stream_cache_append")
+
+    def compress(self, to: "StreamCache", kept, budget: int, sink: int = 0, recent: int = 0,
+                 stream: Optional[int] = None) -> None:
+        """The slots of the highest rank, at most budget, to the front of another cache; kept int32 [L][S][H][budget]
+        tells which (-1 beyond)."""
+        L, S, H = self.shape[:3]
+        _buffer(kept, "mlora_stream_cache_compress", 4, n=L * S * H * budget)
+        _check(load_library().mlora_stream_cache_compress(self.ref, to.ref, _ptr(kept), budget, sink, recent,
+                                                          _stream() if stream is None else stream),
+               "mlora_stream_cache_compress")
+
+
+class AttentionMass:
+    """Descriptor of mlora_attention_mass_add: attention weights of the newest rows added to the mass of the cache's slots
+    and of a prefill segment (k_prefill bf16 [L][H][P][head_dim], mass_prefill fp32 [L][H][P])."""
+
+    def __init__(self, cache: StreamCache, n_q_heads: int, rows_per_stream: int, scale: float, k_prefill=None,
+                 mass_prefill=None, decay: float = 1.0):
+        L, S, H, _, D = cache.shape
+        P = 0
+        if k_prefill is not None:
+            P = int(k_prefill.shape[2]) if k_prefill.dim() == 4 else -1
+            _buffer(k_prefill, "attention mass", 2, (L, H, P, D))
+            if mass_prefill is None:
+                raise MloraError(_EINVAL, "attention mass")
+            _buffer(mass_prefill, "attention mass", 4, (L, H, P))
+        self.keep = (cache, k_prefill, mass_prefill)
+        self.streams, self.q_elements = S, L * S * int(rows_per_stream) * int(n_q_heads) * D
+        self.struct = _AttentionMassStruct(cache.struct, int(n_q_heads), int(rows_per_stream), float(scale),
+                                           _ptr(k_prefill), _ptr(mass_prefill), P, float(decay))
+        self.ref = C.byref(self.struct)
+
+    def workspace_bytes(self, n_rows: int = 0) -> int:
+        """For calls with n_rows listed rows per stream, 0: with all rows."""
+        return int(load_library().mlora_attention_mass_workspace_bytes(self.ref, n_rows))
+
+    def run(self, q, rows, workspace, stream: Optional[int] = None) -> None:
+        """q bf16 [L][S * rows_per_stream][n_q_heads][head_dim], rows int32 [S][n] or None (all)."""
+        _buffer(q, "mlora_attention_mass_add", 2, n=self.q_elements)
+        listed = 0
+        if rows is not None:
+            listed = rows.numel() // self.streams
+            _buffer(rows, "mlora_attention_mass_add", 4, n=self.streams * listed)
+        n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        st = load_library().mlora_attention_mass_add(self.ref, q.data_ptr(), _ptr(rows), listed, _ptr(workspace), n,
+                                                     _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, "mlora_attention_mass_add")
+
+
+class LogitRules:
+    """Descriptor of mlora_logit_rules_apply: penalties for tokens that counts (int32 [S][V]) and the rows' paths hold,
+    biases (fp32 [n][V], a row per stream) and grammar masks (bits, int32 [n][(V + 31) / 32], a row per logits row)."""
+
+    def __init__(self, n_streams: int, rows_per_stream: int, tokens_per_stream: int, vocab: int, logits_dtype: int, parent,
+                 counts=None, repetition=None, frequency=None, presence=None, bias=None, bias_row=None, masks=None,
+                 mask_row=None):
+        S, R, T, V = int(n_streams), int(rows_per_stream), int(tokens_per_stream), int(vocab)
+        where = "logit rules"
+        _buffer(parent, where, 4, n=S * R)
+        if counts is not None:
+            _buffer(counts, where, 4, (S, V))
+        for t in (repetition, frequency, presence):
+            if t is not None:
+                _buffer(t, where, 4, n=S)
+        if (bias is None) != (bias_row is None) or (masks is None) != (mask_row is None):
+            raise MloraError(_EINVAL, where)
+        if bias is not None:
+            _buffer(bias, where, 4, (bias.shape[0], V))
+            _buffer(bias_row, where, 4, n=S)
+        if masks is not None:
+            _buffer(masks, where, 4, (masks.shape[0], (V + 31) // 32))
+            _buffer(mask_row, where, 4, n=S * R)
+        self.keep = (parent, counts, repetition, frequency, presence, bias, bias_row, masks, mask_row)
+        self.streams, self.tokens, self.logits, self.itemsize = S, S * T, S * R * V, 2 if logits_dtype == Y_BF16 else 4
+        self.struct = _LogitRulesStruct(S, R, T, V, int(logits_dtype), _ptr(parent), _ptr(counts), _ptr(repetition),
+                                        _ptr(frequency), _ptr(presence), _ptr(bias), _ptr(bias_row),
+                                        0 if bias is None else int(bias.shape[0]), _ptr(masks), _ptr(mask_row),
+                                        0 if masks is None else int(masks.shape[0]))
+        self.ref = C.byref(self.struct)
+
+    def run(self, logits, tokens, out, new_tokens=None, stream: Optional[int] = None) -> None:
+        """logits [S * R][V] -> out (may be logits itself); tokens int32 [S][T]; new_tokens int32 [S][n]: counted first."""
+        where = "mlora_logit_rules_apply"
+        _buffer(logits, where, self.itemsize, n=self.logits)
+        _buffer(out, where, self.itemsize, n=self.logits)
+        _buffer(tokens, where, 4, n=self.tokens)
+        fresh = 0
+        if new_tokens is not None:
+            fresh = new_tokens.numel() // self.streams
+            _buffer(new_tokens, where, 4, n=self.streams * fresh)
+        st = load_library().mlora_logit_rules_apply(self.ref, logits.data_ptr(), tokens.data_ptr(),
+                                                    _ptr(new_tokens) if fresh else None, fresh, out.data_ptr(),
+                                                    _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)

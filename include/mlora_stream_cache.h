@@ -32,6 +32,7 @@ extern "C" {
 
 enum {
     MLORA_CACHE_MAX_SLOTS = 1 << 24,   /* cap */
+    MLORA_CACHE_TICKET_WORDS = 32,     /* a line of memory per stream */
     MLORA_CACHE_MAX_HEADS = 1 << 20    /* n_layers * n_streams * n_kv_heads */
 };
 
@@ -45,7 +46,7 @@ typedef struct {
     int32_t *slot_pos;                 /* int32 [L][S][H][cap] */
     int32_t *len;                      /* int32 [S]: live slots, the same in all layers and heads */
     int32_t *next_pos;                 /* int32 [S]: position of the stream's next token */
-    uint32_t *tickets;                 /* uint32 [S]: zero when a call starts, zero again when it ends (append alone uses them) */
+    uint32_t *tickets;                 /* uint32 [S][MLORA_CACHE_TICKET_WORDS]: zero when a call starts, zero again when it ends (append alone uses them) */
 } mlora_stream_cache;
 
 /* Row j of the n that a stream appends goes to slot len + j while the live slots are fewer than max(len, budget); the others go to

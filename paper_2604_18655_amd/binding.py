@@ -662,7 +662,7 @@ class StreamCache:
         for t in (len, next_pos):
             _buffer(t, "stream cache", 4, (S,))
         self.k, self.v, self.mass, self.slot_pos, self.len, self.next_pos = k, v, mass, slot_pos, len, next_pos
-        self.tickets = torch.zeros(S, dtype=torch.int32).to(k.device)        # (an upload: done when it returns)
+        self.tickets = torch.zeros((S, 32), dtype=torch.int32).to(k.device)  # (an upload: done when it returns)
         self.shape = (L, S, H, cap, D)
         self.struct = _StreamCacheStruct(L, S, H, D, cap, _ptr(k), _ptr(v), _ptr(mass), _ptr(slot_pos), _ptr(len),
                                          _ptr(next_pos), _ptr(self.tickets))

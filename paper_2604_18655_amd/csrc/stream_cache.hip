@@ -426,7 +426,8 @@ struct CompressArgs {
 
 // One head's slots, all of them found: AT_ONCE rows of keys and of values side by side, AHEAD times.  from_slot(j) is the slot of
 // row j, the same for all lanes of a row; j counts from the first row of `to`.
-template <int D, int LANES, class From>
+// STREAM: past the caches, where there is more of it than they hold.
+template <int D, int LANES, bool STREAM, class From>
 __device__ __forceinline__ void copy_rows(const CompressArgs &a, size_t from, size_t to, int rows, int lane, const From &from_slot)
 {
     constexpr int PIECES = D / 8, AT_ONCE = LANES / PIECES, AHEAD = 4;
@@ -438,12 +439,15 @@ __device__ __forceinline__ void copy_rows(const CompressArgs &a, size_t from, si
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + u * AT_ONCE + row, src = from_slot(j);
-            if (j < rows) kv[u] = ks[(size_t)src * PIECES], vv[u] = vs[(size_t)src * PIECES];
+            const u32x4 *const kp = ks + (size_t)src * PIECES, *const vp = vs + (size_t)src * PIECES;
+            if (j < rows) kv[u] = STREAM ? __builtin_nontemporal_load(kp) : *kp, vv[u] = STREAM ? __builtin_nontemporal_load(vp) : *vp;
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + u * AT_ONCE + row;
-            if (j < rows) kt[(size_t)j * PIECES] = kv[u], vt[(size_t)j * PIECES] = vv[u];
+            if (j >= rows) continue;
+            if (STREAM) __builtin_nontemporal_store(kv[u], kt + (size_t)j * PIECES), __builtin_nontemporal_store(vv[u], vt + (size_t)j * PIECES);
+            else        kt[(size_t)j * PIECES] = kv[u], vt[(size_t)j * PIECES] = vv[u];
         }
     }
 }
@@ -488,7 +492,7 @@ __global__ __launch_bounds__(THREADS) void cache_select(const CompressArgs a)
             a.to.mass[to + i] = hd.mass[slot_of[i]];
             a.to.slot_pos[to + i] = hd.pos[slot_of[i]];
         }
-        copy_rows<D, THREADS>(a, slots, to, keep, tid, [&](int j) { return slot_of[min(j, keep - 1)]; });
+        copy_rows<D, THREADS, false>(a, slots, to, keep, tid, [&](int j) { return slot_of[min(j, keep - 1)]; });
     }
 }
 
@@ -506,7 +510,7 @@ __global__ __launch_bounds__(256) void cache_gather(const CompressArgs a)
         a.to.mass[to + lane] = a.from.mass[from + slot];
         a.to.slot_pos[to + lane] = a.from.slot_pos[from + slot];
     }
-    copy_rows<D, 64>(a, from, to, __popcll(__ballot(slot >= 0)), lane, [&](int j) { return __shfl(slot, j); });
+    copy_rows<D, 64, true>(a, from, to, __popcll(__ballot(slot >= 0)), lane, [&](int j) { return __shfl(slot, j); });
 }
 
 mlora_status check(const mlora_stream_cache *c)

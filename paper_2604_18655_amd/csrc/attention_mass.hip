@@ -12,6 +12,7 @@
 //
 // Query vectors are counted (stream, listed row, query head of the group): v = (s * N + j) * G + g.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -23,8 +24,6 @@ namespace {
 
 constexpr int MASS_WAVES = 4;
 constexpr int KC = 32;                   // keys of a chunk in mass_stats
-constexpr int KT = 2;                    // key tiles (of 16) of a wave in mass_add
-constexpr int ADD_KEYS = MASS_WAVES * KT * 16;
 constexpr int BATCH = 512;               // query vectors whose maxima mass_add holds at a time
 constexpr float NEG_BIG = -1.0e30f;      // "no key seen yet"
 constexpr float UNSEEN = -3.0e38f;       // score of a key that is not visible: exp2(UNSEEN - NEG_BIG) is 0
@@ -35,11 +34,14 @@ struct MassArgs {
     const uint16_t *q, *k, *k_prefill;
     float *mass, *mass_prefill;
     const int *slot_pos, *len, *next_pos, *rows;
+    float2 *rows_ml;                     // wide calls: [L * H][vecs], maximum and 1 / sum
+    int *q_row;                          // wide calls: [vecs], vector of a.q of a layer's first head (of its query heads), -1: does not count
     float2 *part;                        // [L * H][p_splits + s_splits][vecs]: maximum (of scores in units of log 2) and sum
     int L, S, H, G, R, N, cap, P;        // N: listed rows of a stream
     int vecs;                            // S * N * G
     int p_splits, s_splits;              // blocks that share the keys of a query tile: prefill, stream segment
-    int p_blocks, s_blocks;              // blocks of a layer and head: prefill; one stream
+    int p_blocks, s_blocks;              // blocks of a layer and head: prefill; one stream (mass_stats)
+    int p_tiles, s_tiles;                // the same (mass_add)
     float scale2, decay;                 // scale2 = scale * log2(e)
 };
 
@@ -80,70 +82,108 @@ __device__ __forceinline__ float over_quarters(float v, const Op &op)
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// One block: QT tiles of 16 query vectors (of one stream, or of all streams on the prefill segment) against a share of the keys.
+// What a block works on: a layer's and head's prefill segment or a stream's own, and a number within it.
+struct Unit {
+    int lh, l, h, s, number;
+    bool prefill;
+    int n, newest;                       // listed rows of the stream, and the position of the first one
+    int vecs, keys;                      // query vectors and keys
+    const uint16_t *k;
+    const int *pos;
+    size_t at;                           // of the segment's first slot
+    __device__ __forceinline__ Unit(const MassArgs &a, int p_blocks, int s_blocks, int D)
+    {
+        const int per_head = p_blocks + a.S * s_blocks;
+        lh = (int)blockIdx.x / per_head;
+        l = lh / a.H;
+        h = lh - l * a.H;
+        number = (int)blockIdx.x - lh * per_head;
+        prefill = number < p_blocks;
+        s = 0;
+        if (!prefill) {
+            number -= p_blocks;
+            s = number / s_blocks;
+            number -= s * s_blocks;
+        }
+        n = prefill ? 0 : listed(a, s);
+        newest = prefill ? 0 : a.next_pos[s] - n;
+        vecs = prefill ? a.vecs : n * a.G;
+        keys = prefill ? a.P : max(0, min(a.len[s], a.cap));
+        at = prefill ? (size_t)lh * a.P : (((size_t)l * a.S + s) * a.H + h) * a.cap;
+        k = (prefill ? a.k_prefill : a.k) + at * D;
+        pos = a.slot_pos + at;
+    }
+    // place of query vector v's features in a.q, and its number over all streams; false: it does not count
+    __device__ __forceinline__ bool vector(const MassArgs &a, int v, int D, size_t &q, int &number_of) const
+    {
+        const int j = v / a.G, g = v - j * a.G;
+        int st = s, row = j;
+        if (prefill) st = j / a.N, row = j - st * a.N;
+        number_of = (st * a.N + row) * a.G + g;
+        q = 0;
+        if (prefill && !counts(a, st, row)) return false;
+        q = q_at(a, l, h, st, row, g, D);
+        return true;
+    }
+};
+
+// Maximum and sum of QT tiles of 16 query vectors over a share of the keys.
 template <int D, int QT>
-__global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
+__device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, float2 (*ml)[128])
 {
     constexpr int DK = D / 32;
-    __shared__ float2 ml[MASS_WAVES][QT * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int per_head = a.p_blocks + a.S * a.s_blocks, lh = (int)blockIdx.x / per_head, l = lh / a.H, h = lh - l * a.H;
-    int b = (int)blockIdx.x - lh * per_head;
-    const bool prefill = b < a.p_blocks;
-    int s = 0;
-    if (!prefill) {
-        b -= a.p_blocks;
-        s = b / a.s_blocks;
-        b -= s * a.s_blocks;
-    }
-    const int splits = prefill ? a.p_splits : a.s_splits, tile = b / splits, z = b - tile * splits;
-    const int v0 = tile * QT * 16, n = prefill ? 0 : listed(a, s);
-    const int mine = prefill ? a.vecs : n * a.G;                     // query vectors of this segment
-    const int keys = prefill ? a.P : max(0, min(a.len[s], a.cap));
-    if (v0 >= mine) return;
-    const int newest = prefill ? 0 : a.next_pos[s] - n;              // position of the first listed row
-    const size_t seg = prefill ? (size_t)lh * a.P : (((size_t)l * a.S + s) * a.H + h) * a.cap;
-    const uint16_t *const kb = (prefill ? a.k_prefill : a.k) + seg * D;
-    const int *const pb = a.slot_pos + seg;
+    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.number / splits, z = w.number - tile * splits;
+    const int v0 = tile * QT * 16;
+    if (v0 >= w.vecs) return;
 
+    // keys as A operands (past the end: the last key), a chunk ahead of the one that is worked on
+    struct Keys {
+        uint4 f[KC / 16][DK];
+        int pos;
+    };
+    const int chunks = (w.keys + KC - 1) / KC, stride = splits * MASS_WAVES;
+    const auto ask = [&](Keys &x, int c) {
+        const int k0 = c * KC, last = w.keys - 1;
+#pragma unroll
+        for (int j = 0; j < KC / 16; ++j) {
+            const uint16_t *const kp = w.k + (size_t)min(k0 + 16 * j + l16, last) * D + 8 * lq;
+#pragma unroll
+            for (int kk = 0; kk < DK; ++kk) x.f[j][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
+        }
+        x.pos = w.prefill ? 0 : w.pos[min(k0 + (lane & 31), last)];
+    };
+    Keys even, odd;
+    int c = z * MASS_WAVES + wave;
+    if (c < chunks) ask(even, c);
     // this lane's query vectors (B operands: lane (l16, lq) holds features 8 * lq .. of vector l16 of a tile)
     uint4 qf[QT][DK];
     float m[QT], sum[QT];
     int pos[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        const int v = min(v0 + 16 * t + l16, mine - 1), j = v / a.G, g = v - j * a.G;
-        int st = s, row = j;
-        if (prefill) st = j / a.N, row = j - st * a.N;
-        if (prefill && !counts(a, st, row)) row = -1;
-        const uint16_t *const qp = a.q + (row < 0 ? 0 : q_at(a, l, h, st, row, g, D)) + 8 * lq;
+        const int v = min(v0 + 16 * t + l16, w.vecs - 1);
+        size_t q;
+        int number;
+        w.vector(a, v, D, q, number);
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const uint4 *>(qp + 32 * kk);
-        pos[t] = newest + j;
+        for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
+        pos[t] = w.newest + v / a.G;
         m[t] = NEG_BIG;
         sum[t] = 0.f;
     }
-    const int chunks = (keys + KC - 1) / KC;
-    for (int c = z * MASS_WAVES + wave; c < chunks; c += splits * MASS_WAVES) {
-        const int k0 = c * KC, nk = min(KC, keys - k0);
-        // keys as A operands (past the end: the last key)
-        uint4 kf[KC / 16][DK];
-#pragma unroll
-        for (int j = 0; j < KC / 16; ++j) {
-            const uint16_t *const kp = kb + (size_t)(k0 + min(16 * j + l16, nk - 1)) * D + 8 * lq;
-#pragma unroll
-            for (int kk = 0; kk < DK; ++kk) kf[j][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
-        }
-        const int at = prefill ? 0 : pb[k0 + min(lane & 31, nk - 1)];
-        const bool masked = nk < KC || (!prefill && __any(at > newest));
+    const auto work = [&](const Keys &x, int c) {
+        const int nk = min(KC, w.keys - c * KC);
+        const bool masked = nk < KC || (!w.prefill && __any(x.pos > w.newest));
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
+            if (QT > 1 && v0 + 16 * t >= w.vecs) break;
             f32x4 sc[KC / 16];
 #pragma unroll
             for (int j = 0; j < KC / 16; ++j) {
                 sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < DK; ++kk) sc[j] = mfma16(kf[j][kk], qf[t][kk], sc[j]);
+                for (int kk = 0; kk < DK; ++kk) sc[j] = mfma16(x.f[j][kk], qf[t][kk], sc[j]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sc[j][e] *= a.scale2;
             }
@@ -153,8 +193,8 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = 16 * j + 4 * lq + e;
-                        const int key_pos = __shfl(at, key);         // (all lanes: before any condition)
-                        sc[j][e] = key < nk && (prefill || key_pos <= pos[t]) ? sc[j][e] : UNSEEN;
+                        const int key_pos = __shfl(x.pos, key);      // (all lanes: before any condition)
+                        sc[j][e] = key < nk && (w.prefill || key_pos <= pos[t]) ? sc[j][e] : UNSEEN;
                     }
             }
             float top = m[t];
@@ -170,6 +210,12 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
             sum[t] = sum[t] * __builtin_amdgcn_exp2f(m[t] - top) + add;
             m[t] = top;
         }
+    };
+    for (; c < chunks; c += 2 * stride) {
+        if (c + stride < chunks) ask(odd, c + stride);
+        work(even, c);
+        if (c + 2 * stride < chunks) ask(even, c + 2 * stride);
+        if (c + stride < chunks) work(odd, c + stride);
     }
     // the quarters' keys, then the waves'
 #pragma unroll
@@ -180,42 +226,53 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
     }
     __syncthreads();
     const int v = v0 + (int)threadIdx.x;
-    if (threadIdx.x < QT * 16 && v < mine) {
+    if (threadIdx.x < QT * 16 && v < w.vecs) {
         float top = NEG_BIG, all = 0.f;
 #pragma unroll
-        for (int w = 0; w < MASS_WAVES; ++w) top = fmaxf(top, ml[w][threadIdx.x].x);
+        for (int i = 0; i < MASS_WAVES; ++i) top = fmaxf(top, ml[i][threadIdx.x].x);
 #pragma unroll
-        for (int w = 0; w < MASS_WAVES; ++w) all += ml[w][threadIdx.x].y * __builtin_amdgcn_exp2f(ml[w][threadIdx.x].x - top);
-        const int row = (prefill ? 0 : a.p_splits) + z;
-        a.part[((size_t)lh * (a.p_splits + a.s_splits) + row) * a.vecs + (prefill ? v : s * a.N * a.G + v)] = make_float2(top, all);
+        for (int i = 0; i < MASS_WAVES; ++i) all += ml[i][threadIdx.x].y * __builtin_amdgcn_exp2f(ml[i][threadIdx.x].x - top);
+        const int row = (w.prefill ? 0 : a.p_splits) + z;
+        a.part[((size_t)w.lh * (a.p_splits + a.s_splits) + row) * a.vecs + (w.prefill ? v : w.s * a.N * a.G + v)] = make_float2(top, all);
     }
 }
 
-// One block: 128 keys of a segment against all query vectors that may see them.
-template <int D>
+template <int D, int PT, int QT>
+__global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
+{
+    __shared__ float2 ml[MASS_WAVES][128];
+    const Unit w(a, a.p_blocks, a.s_blocks, D);
+    if (PT != QT && w.prefill) stats_tiles<D, PT>(a, w, ml);
+    else                       stats_tiles<D, QT>(a, w, ml);
+}
+
+// maximum and 1 / sum of a query vector over all blocks that looked at its keys; a row that sees nothing: 0
+__device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int number)
+{
+    const int splits = a.p_splits + a.s_splits;
+    const float2 *const part = a.part + (size_t)lh * splits * a.vecs + number;
+    float top = NEG_BIG, all = 0.f;
+    for (int z = 0; z < splits; ++z) {
+        const float2 x = part[(size_t)z * a.vecs];
+        const float t2 = fmaxf(top, x.x);
+        all = all * __builtin_amdgcn_exp2f(top - t2) + x.y * __builtin_amdgcn_exp2f(x.x - t2);
+        top = t2;
+    }
+    return make_float2(top, all > 0.f ? 1.f / all : all);            // (NaN stays)
+}
+
+// One block: KT tiles of 16 keys per wave against all query vectors that may see them.
+template <int D, int KT>
 __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 {
-    constexpr int DK = D / 32;
+    constexpr int DK = D / 32, KEYS = MASS_WAVES * KT * 16;
     __shared__ __align__(16) float top_of[BATCH], inv_of[BATCH];
     __shared__ int pos_of[BATCH];
     __shared__ const uint16_t *q_of[BATCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int p_blocks = (a.P + ADD_KEYS - 1) / ADD_KEYS, s_blocks = (a.cap + ADD_KEYS - 1) / ADD_KEYS;
-    const int per_head = p_blocks + a.S * s_blocks, lh = (int)blockIdx.x / per_head, l = lh / a.H, h = lh - l * a.H;
-    int b = (int)blockIdx.x - lh * per_head;
-    const bool prefill = b < p_blocks;
-    int s = 0;
-    if (!prefill) {
-        b -= p_blocks;
-        s = b / s_blocks;
-        b -= s * s_blocks;
-    }
-    const int keys = prefill ? a.P : max(0, min(a.len[s], a.cap));
-    if (b * ADD_KEYS >= keys) return;
-    const int n = prefill ? 0 : listed(a, s), newest = prefill ? 0 : a.next_pos[s] - n;
-    const int mine = prefill ? a.vecs : n * a.G;
-    const size_t seg = prefill ? (size_t)lh * a.P : (((size_t)l * a.S + s) * a.H + h) * a.cap;
-    const int k0 = b * ADD_KEYS + wave * KT * 16;
+    const Unit w(a, a.p_tiles, a.s_tiles, D);
+    if (w.number * KEYS >= w.keys) return;
+    const int k0 = w.number * KEYS + wave * KT * 16;
 
     // this lane's keys (B operands)
     uint4 kf[KT][DK];
@@ -223,43 +280,33 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     float acc[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-        const int key = min(k0 + 16 * t + l16, keys - 1);
-        const uint16_t *const kp = (prefill ? a.k_prefill : a.k) + (seg + key) * D + 8 * lq;
+        const int key = min(k0 + 16 * t + l16, w.keys - 1);
+        const uint16_t *const kp = w.k + (size_t)key * D + 8 * lq;
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
-        at[t] = prefill ? 0 : a.slot_pos[seg + key];
+        at[t] = w.prefill ? 0 : w.pos[key];
         acc[t] = 0.f;
     }
-    bool masked = false;
-#pragma unroll
-    for (int t = 0; t < KT; ++t) masked |= !prefill && at[t] > newest;
-    masked = __any(masked);
 
-    for (int base = 0; base < mine; base += BATCH) {
-        const int here = min(BATCH, mine - base), pad = (here + 15) / 16 * 16;
-        __syncthreads();
+    for (int base = 0; base < w.vecs; base += BATCH) {
+        const int here = min(BATCH, w.vecs - base), pad = (here + 15) / 16 * 16;
+        if (base > 0) __syncthreads();
         for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
-            const int v = min(base + i, mine - 1), j = v / a.G, g = v - j * a.G;
-            int st = s, row = j;
-            if (prefill) st = j / a.N, row = j - st * a.N;
-            const bool ok = base + i < mine && (!prefill || counts(a, st, row));
-            float top = NEG_BIG, all = 0.f;
-            const int splits = a.p_splits + a.s_splits;
-            const float2 *const part = a.part + (size_t)lh * splits * a.vecs + ((size_t)st * a.N + row) * a.G + g;
-            if (ok) {
-                for (int z = 0; z < splits; ++z) {
-                    const float2 x = part[(size_t)z * a.vecs];
-                    const float t2 = fmaxf(top, x.x);
-                    all = all * __builtin_amdgcn_exp2f(top - t2) + x.y * __builtin_amdgcn_exp2f(x.x - t2);
-                    top = t2;
-                }
-            }
-            top_of[i] = top;
-            inv_of[i] = all > 0.f ? 1.f / all : all;                 // (a row that sees nothing adds nothing; NaN stays)
-            pos_of[i] = newest + j;
-            q_of[i] = a.q + (ok ? q_at(a, l, h, st, row, g, D) : 0);
+            const int v = min(base + i, w.vecs - 1);
+            size_t q;
+            int number;
+            const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
+            const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NEG_BIG, 0.f);
+            top_of[i] = row.x;
+            inv_of[i] = row.y;
+            pos_of[i] = w.newest + v / a.G;
+            q_of[i] = a.q + q;
         }
         __syncthreads();
+        bool masked = false;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) masked |= !w.prefill && at[t] > w.newest;
+        masked = __any(masked);
         for (int t0 = 0; t0 < pad; t0 += 16) {
             // query vectors as A operands: element e of a score belongs to vector 4 * lq + e
             uint4 qf[DK];
@@ -274,9 +321,9 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
                 for (int kk = 0; kk < DK; ++kk) sc = mfma16(qf[kk], kf[t][kk], sc);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float w = __builtin_amdgcn_exp2f(sc[e] * a.scale2 - top[e]) * inv[e];
-                    if (masked) w = at[t] <= pos_of[t0 + 4 * lq + e] ? w : 0.f;
-                    acc[t] += inv[e] != 0.f ? w : 0.f;
+                    float x = __builtin_amdgcn_exp2f(sc[e] * a.scale2 - top[e]) * inv[e];
+                    if (masked) x = at[t] <= pos_of[t0 + 4 * lq + e] ? x : 0.f;
+                    acc[t] += inv[e] != 0.f ? x : 0.f;
                 }
             }
         }
@@ -285,8 +332,359 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     for (int t = 0; t < KT; ++t) {
         const float add = over_quarters(acc[t], [](float x, float y) { return x + y; });
         const int key = k0 + 16 * t + l16;
-        float *const to = (prefill ? a.mass_prefill : a.mass) + seg + key;
-        if (lq == 0 && key < keys) *to = a.decay * *to + add;
+        float *const to = (w.prefill ? a.mass_prefill : a.mass) + w.at + key;
+        if (lq == 0 && key < w.keys) *to = a.decay * *to + add;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Many query vectors (a prompt's chunk): the side that a wave keeps is 64 vectors (or keys) in registers, the other passes by in
+// chunks of 64 rows that the block's waves share through LDS, on the 32x32x16 products.  A row's 16-byte pieces are
+// exchanged by its number, so that both the writes (rows side by side) and the reads (32 rows of one piece) use all banks.
+// Bound by the exponentials, 16 of a score's 24 cycles per 64 lanes: see the launch rule for what it measured.
+// ---------------------------------------------------------------------------------------------
+constexpr int WIDE_ROWS = 64;            // rows of a chunk
+constexpr int WIDE_OWN = 256;            // vectors or keys of a block
+constexpr float FAR = 1.0995e12f;        // 2^40: how far sums may grow above their maximum before they are scaled down
+
+template <int D>
+struct Stage {
+    static constexpr int PIECES = D / 8, PER = WIDE_ROWS * PIECES / 256;            // pieces of a row, of a thread
+    static constexpr int BYTES = WIDE_ROWS * D * 2;
+    static __device__ __forceinline__ int row(int i) { return (i * 256 + (int)threadIdx.x) / PIECES; }
+    static __device__ __forceinline__ int piece() { return (int)threadIdx.x % PIECES; }
+    static __device__ __forceinline__ int place(int row, int piece) { return row * PIECES + (piece ^ (D == 128 ? row & 15 : row >> 1 & 7)); }
+};
+
+// What the wave keeps is there before the loop: the compiler would wait for it inside, and for the loads on their way with it.
+__device__ __forceinline__ void all_loaded() { __builtin_amdgcn_s_waitcnt(0x0F70); }              // vmcnt 0, the others unchanged
+
+// Scores of 32 rows of a chunk against what the wave keeps: element i of sc[t] is row 8 * (i / 4) + 4 * (lane / 32) + i % 4
+// against column 32 * t + lane % 32.  at[kk]: where the lane's pieces stand in the first half of the first buffer.  slice(i), i = 0 ..
+// 7, is an eighth of the vector work on the last 32 rows' scores; the two are written in turn and kept so, because the
+// matrix unit works beside the vector unit only if it is fed in between, and a chain of one exponential after the other
+// waits for each.
+template <int D, int BUFFER, int HALF, class Slice>
+__device__ __forceinline__ void wide_scores(const u32x4 *chunks, const int (&at)[D / 16], const u32x4 (&own)[2][D / 16], f32x16 (&sc)[2], const Slice &slice)
+{
+    constexpr int DK = D / 16, FROM = (BUFFER * WIDE_ROWS + HALF * 32) * Stage<D>::PIECES;
+    const auto piece = [&](int kk) { return __builtin_bit_cast(uint4, chunks[at[kk] + FROM]); };
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[t][i] = 0.f;
+    uint4 f = piece(0);
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) {
+        const uint4 now = f;
+        if (kk + 1 < DK) f = piece(kk + 1);
+        sc[0] = mfma32(now, __builtin_bit_cast(uint4, own[0][kk]), sc[0]);
+        if (DK == 4) slice(2 * kk);
+        __builtin_amdgcn_sched_barrier(0);
+        sc[1] = mfma32(now, __builtin_bit_cast(uint4, own[1][kk]), sc[1]);
+        slice(DK == 4 ? 2 * kk + 1 : kk);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Maximum and sum of 256 query vectors over every splits-th chunk of keys.
+template <int D>
+__global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
+{
+    constexpr int DK = D / 16;
+    using St = Stage<D>;
+    __shared__ u32x4 chunk[2 * WIDE_ROWS * St::PIECES];
+    __shared__ __align__(16) int key_pos[4][WIDE_ROWS];              // (read while the next but one is written)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh2 = lane >> 5;
+    const Unit w(a, a.p_blocks, a.s_blocks, D);
+    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.number / splits, z = w.number - tile * splits;
+    const int v0 = tile * WIDE_OWN;
+    if (v0 >= w.vecs) return;
+    const int mine = v0 + wave * 64;                                 // first vector of the wave
+
+    u32x4 qf[2][DK];
+    float m[2], sum[2];
+    int pos[2], at[DK];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int v = min(mine + 32 * t + l32, w.vecs - 1);
+        size_t q;
+        int number;
+        w.vector(a, v, D, q, number);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const u32x4 *>(a.q + q + 16 * kk + 8 * lh2);
+        pos[t] = w.prefill ? 0 : w.newest + v / a.G;
+        m[t] = NEG_BIG;
+        sum[t] = 0.f;
+    }
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) at[kk] = St::place(l32, 2 * kk + lh2);
+    const int first_pos = w.prefill ? 0 : w.newest + min(mine, w.vecs - 1) / a.G;
+    const int chunks = (w.keys + WIDE_ROWS - 1) / WIDE_ROWS;
+    u32x4 next[St::PER];
+    int next_pos = 0, next_k0 = 0;
+    bool masked = false;                                             // the chunk holds keys that some of the wave's vectors do not see
+    // (what is loaded is not looked at here: that would wait for it)
+    const auto ask = [&](int c) {
+        next_k0 = min(c, chunks - 1) * WIDE_ROWS;
+        const uint16_t *const rows = w.k + (size_t)next_k0 * D;
+        const int last = w.keys - 1 - next_k0;
+#pragma unroll
+        for (int i = 0; i < St::PER; ++i) next[i] = *reinterpret_cast<const u32x4 *>(rows + (unsigned)(min(St::row(i), last) * D + St::piece() * 8));
+        if (!w.prefill) next_pos = w.pos[next_k0 + min(lane, last)];
+    };
+    const auto put = [&](int buffer, int c) {
+#pragma unroll
+        for (int i = 0; i < St::PER; ++i) chunk[buffer * WIDE_ROWS * St::PIECES + St::place(St::row(i), St::piece())] = next[i];
+        // (a prefill segment hides what lies past its end)
+        const int p = next_k0 + lane < w.keys ? next_pos : 0x7FFFFFFF;
+        if (tid < WIDE_ROWS) key_pos[c & 3][lane] = p;
+        return (bool)__any(p > first_pos);
+    };
+    const auto hide = [&](f32x16 (&sc)[2], int c, int half) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int p = key_pos[c & 3][32 * half + 8 * (i / 4) + 4 * lh2 + i % 4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sc[t][i] = p <= pos[t] ? sc[t][i] : -__builtin_inff();
+        }
+    };
+    // Sums relative to a maximum that may lie a little behind: the sum itself tells when it does too far.  A slice: four scores, and
+    // the sum of the slice before.
+    float more[2], e[4];
+    const auto slice_of = [&](const f32x16 (&sc)[2]) {
+        return [&](int i) {
+            const int t = i / 4, first = i % 4 * 4;
+            float old[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                old[u] = e[u];
+                e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][first + u], a.scale2, -m[t]));
+            }
+            if (i % 4 == 1) more[t] = (old[0] + old[1]) + (old[2] + old[3]);
+            else if (i > 0) more[(i - 1) / 4] += (old[0] + old[1]) + (old[2] + old[3]);
+        };
+    };
+    const auto settle = [&](const f32x16 (&sc)[2]) {
+        more[1] += (e[0] + e[1]) + (e[2] + e[3]);
+        if (__any(more[0] > FAR || more[1] > FAR)) {                 // rare, but for the first chunk: once more
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float high = sc[t][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) high = fmaxf(high, sc[t][i]);
+                high = fmaxf(high * a.scale2, m[t]);
+                sum[t] *= __builtin_amdgcn_exp2f(m[t] - high);
+                m[t] = high;
+                more[t] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) more[t] += __builtin_amdgcn_exp2f(fmaf(sc[t][i], a.scale2, -high));
+            }
+        }
+        sum[0] += more[0];
+        sum[1] += more[1];
+    };
+    f32x16 x[2], y[2];
+    if (chunks > 0) {
+        ask(z);
+        masked = put(0, 0);
+    }
+    __syncthreads();
+    all_loaded();
+    if (chunks > 0) ask(z + splits);
+    wide_scores<D, 0, 0>(chunk, at, qf, x, [](int) {});
+    // a chunk: its second half's products beside its first half's exponentials, then the next chunk's first half's beside its second
+    // half's (behind the last chunk: the last one again, of no use)
+    const auto step = [&](auto buffer, int i) {
+        constexpr int B = decltype(buffer)::value;
+        if (masked) hide(x, i, 0);
+        wide_scores<D, B, 1>(chunk, at, qf, y, slice_of(x));
+        settle(x);
+        const bool masked_next = put(B ^ 1, i + 1);
+        __syncthreads();
+        ask(z + (i + 2) * splits);
+        if (masked) hide(y, i, 1);
+        masked = masked_next;
+        wide_scores<D, B ^ 1, 0>(chunk, at, qf, x, slice_of(y));
+        settle(y);
+    };
+    const int mine_chunks = z < chunks ? (chunks - z + splits - 1) / splits : 0;
+    for (int i = 0; i < mine_chunks; i += 2) {
+        step(std::integral_constant<int, 0>{}, i);
+        if (i + 1 < mine_chunks) step(std::integral_constant<int, 1>{}, i + 1);
+    }
+    // the two halves' keys
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const float om = __shfl_xor(m[t], 32), os = __shfl_xor(sum[t], 32), high = fmaxf(m[t], om);
+        const float all = sum[t] * __builtin_amdgcn_exp2f(m[t] - high) + os * __builtin_amdgcn_exp2f(om - high);
+        const int v = mine + 32 * t + l32, row = (w.prefill ? 0 : a.p_splits) + z;
+        if (lh2 == 0 && v < w.vecs)
+            a.part[((size_t)w.lh * (a.p_splits + a.s_splits) + row) * a.vecs + (w.prefill ? v : w.s * a.N * a.G + v)] = make_float2(high, all);
+    }
+}
+
+// Every query vector's maximum and 1 / sum, once for the blocks of mass_add_wide.  A vector that does not count: a maximum that
+// makes all weights 0.
+__global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
+{
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (long long)a.L * a.H * a.vecs) return;
+    const int lh = (int)(i / a.vecs), number = (int)(i - (long long)lh * a.vecs), j = number / a.G, s = j / a.N;
+    const bool ok = counts(a, s, j - s * a.N);
+    a.rows_ml[i] = ok ? whole_row(a, lh, number) : make_float2(1e30f, 0.f);
+    if (lh == 0) a.q_row[number] = ok ? (s * a.R + (a.rows ? a.rows[j] : j - s * a.N)) * a.H * a.G + number - j * a.G : -1;
+}
+
+// 256 keys of a segment against all query vectors that may see them.
+template <int D>
+__global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
+{
+    constexpr int DK = D / 16;
+    using St = Stage<D>;
+    __shared__ u32x4 chunk[2 * WIDE_ROWS * St::PIECES];
+    __shared__ __align__(16) float top_of[4][WIDE_ROWS], inv_of[4][WIDE_ROWS];
+    __shared__ __align__(16) int pos_of[4][WIDE_ROWS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh2 = lane >> 5;
+    const Unit w(a, a.p_tiles, a.s_tiles, D);
+    if (w.number * WIDE_OWN >= w.keys) return;
+    const int k0 = w.number * WIDE_OWN + wave * 64;
+
+    u32x4 kf[2][DK];
+    int pos[2], at[DK];
+    float acc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int key = min(k0 + 32 * t + l32, w.keys - 1);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const u32x4 *>(w.k + (size_t)key * D + 16 * kk + 8 * lh2);
+        pos[t] = w.prefill ? 0 : w.pos[key];
+        acc[t] = 0.f;
+    }
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) at[kk] = St::place(l32, 2 * kk + lh2);
+    const bool any_hidden = !w.prefill && __any(pos[0] > w.newest || pos[1] > w.newest);          // from the first listed row, at least
+    const int chunks = (w.vecs + WIDE_ROWS - 1) / WIDE_ROWS;
+    const float2 *const ml = a.rows_ml + (size_t)w.lh * a.vecs + (w.prefill ? 0 : w.s * a.N * a.G);
+    const int *const q_row = a.q_row + (w.prefill ? 0 : w.s * a.N * a.G);
+    const uint16_t *const q = a.q + ((size_t)w.l * a.S * a.R * a.H + w.h) * a.G * D;
+    u32x4 next[St::PER];
+    float2 next_ml = make_float2(0.f, 0.f);
+    int rows[St::PER], next_v0 = 0;                                  // where the next chunk's rows stand: a chunk ahead of them
+    unsigned bad = 0;                                                // a bit for each of the chunk's that does not count
+    // (what is loaded is not looked at here: that would wait for it)
+    const auto find = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < St::PER; ++i) rows[i] = q_row[(unsigned)min(c * WIDE_ROWS + St::row(i), w.vecs - 1)];
+    };
+    const auto ask = [&](int c) {
+        next_v0 = c * WIDE_ROWS;
+        int any = next_v0 + WIDE_ROWS > w.vecs ? -1 : 0;
+#pragma unroll
+        for (int i = 0; i < St::PER; ++i) {
+            any |= rows[i];
+            next[i] = *reinterpret_cast<const u32x4 *>(q + ((unsigned)max(rows[i], 0) * D + St::piece() * 8));
+        }
+        bad = 0;
+        if (__any(any < 0)) {
+#pragma unroll
+            for (int i = 0; i < St::PER; ++i) bad |= rows[i] < 0 || next_v0 + St::row(i) >= w.vecs ? 1u << i : 0u;
+        }
+        find(c + 1);
+        next_ml = ml[(unsigned)min(next_v0 + lane, w.vecs - 1)];
+    };
+    const auto put = [&](int buffer, int c) {
+        // (rows that do not count are zeros: what their place holds may be NaN)
+        if (__any(bad != 0)) {
+#pragma unroll
+            for (int i = 0; i < St::PER; ++i)
+                if (bad >> i & 1) next[i] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < St::PER; ++i) chunk[buffer * WIDE_ROWS * St::PIECES + St::place(St::row(i), St::piece())] = next[i];
+        if (tid < WIDE_ROWS) {
+            const bool past = next_v0 + lane >= w.vecs;
+            top_of[c & 3][lane] = past ? 1e30f : next_ml.x;
+            inv_of[c & 3][lane] = past ? 0.f : next_ml.y;
+            pos_of[c & 3][lane] = w.newest + (next_v0 + lane) / a.G;
+        }
+    };
+    const auto hide = [&](f32x16 (&sc)[2], int c, int half) {
+        const int first_pos = pos_of[c & 3][32 * half];
+        if (!__any(pos[0] > first_pos || pos[1] > first_pos)) return;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int p = pos_of[c & 3][32 * half + 8 * (i / 4) + 4 * lh2 + i % 4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sc[t][i] = pos[t] > p ? -__builtin_inff() : sc[t][i];
+        }
+    };
+    // A slice: four scores, and the weights of the slice before.  Maxima and sums come from LDS two slices ahead.
+    float e[4];
+    f32x4 top, inv, old_inv = {0.f, 0.f, 0.f, 0.f}, top_next, inv_next;
+    const auto slice_of = [&](const f32x16 (&sc)[2], int c, int half) {
+        const float *const tops = &top_of[c & 3][32 * half + 4 * lh2], *const invs = &inv_of[c & 3][32 * half + 4 * lh2];
+        top_next = *reinterpret_cast<const f32x4 *>(tops);
+        inv_next = *reinterpret_cast<const f32x4 *>(invs);
+        return [&, tops, invs](int i) {
+            const int g = i / 2, t = i % 2;
+            if (t == 0) {
+                old_inv = inv;
+                top = top_next;
+                inv = inv_next;
+                if (g < 3) {
+                    top_next = *reinterpret_cast<const f32x4 *>(tops + 8 * g + 8);
+                    inv_next = *reinterpret_cast<const f32x4 *>(invs + 8 * g + 8);
+                }
+            }
+            float old[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                old[u] = e[u];
+                e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][4 * g + u], a.scale2, -top[u]));
+            }
+            if (i > 0) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc[1 - t] = fmaf(old[u], t == 0 ? old_inv[u] : inv[u], acc[1 - t]);
+            }
+        };
+    };
+    const auto settle = [&] {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[1] = fmaf(e[u], inv[u], acc[1]);
+    };
+    f32x16 x[2], y[2];
+    if (chunks > 0) {
+        find(0);
+        ask(0);
+        put(0, 0);
+    }
+    __syncthreads();
+    all_loaded();
+    if (chunks > 0) ask(1);
+    wide_scores<D, 0, 0>(chunk, at, kf, x, [](int) {});
+    const auto step = [&](auto buffer, int c) {                      // (see mass_stats_wide)
+        constexpr int B = decltype(buffer)::value;
+        if (any_hidden) hide(x, c, 0);
+        wide_scores<D, B, 1>(chunk, at, kf, y, slice_of(x, c, 0));
+        settle();
+        put(B ^ 1, c + 1);
+        __syncthreads();
+        ask(c + 2);
+        if (any_hidden) hide(y, c, 1);
+        wide_scores<D, B ^ 1, 0>(chunk, at, kf, x, slice_of(y, c, 1));
+        settle();
+    };
+    for (int c = 0; c < chunks; c += 2) {
+        step(std::integral_constant<int, 0>{}, c);
+        if (c + 1 < chunks) step(std::integral_constant<int, 1>{}, c + 1);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const float add = acc[t] + __shfl_xor(acc[t], 32);
+        const int key = k0 + 32 * t + l32;
+        float *const to = (w.prefill ? a.mass_prefill : a.mass) + w.at + key;
+        if (lh2 == 0 && key < w.keys) *to = a.decay * *to + add;
     }
 }
 
@@ -312,8 +710,10 @@ mlora_status check(const mlora_attention_mass *d)
 // How a call is cut: blocks that share a query tile's keys, until the launch has about four blocks per compute unit or a block
 // has fewer than two chunks per wave left.
 struct Plan {
-    int tiles;                           // query tiles of a block
+    bool wide;
+    int p_tiles, s_tiles;                // query tiles of a block: prefill, stream segment
     int p_splits, s_splits, p_blocks, s_blocks;
+    int key_tiles;                       // key tiles of a wave in mass_add
 };
 Plan plan_of(const mlora_attention_mass &d, int N)
 {
@@ -321,18 +721,24 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     const int G = d.n_q_heads / c.n_kv_heads;
     const long long lh = (long long)c.n_layers * c.n_kv_heads, own = (long long)N * G, all = own * c.n_streams;
     Plan p;
-    p.tiles = own > 16 ? 4 : 1;
-    const auto tiles_of = [&](long long vecs) { return (vecs + 16 * p.tiles - 1) / (16 * p.tiles); };
-    const long long pt = d.len_prefill > 0 ? tiles_of(all) : 0, st = tiles_of(own);
-    const long long blocks = lh * (pt + c.n_streams * st), want = std::max(1ll, (1024 + blocks - 1) / blocks);
+    // (a layer's query vectors are reached by 32-bit offsets)
+    p.wide = d.scale > 0.f && own >= WIDE_OWN && d.n_q_heads <= 1024;
+    const auto tiles_of = [&](long long vecs) { return vecs <= 16 ? 1 : c.head_dim == 64 && vecs > 64 ? 8 : 4; };
+    p.s_tiles = own <= 16 ? 1 : 4;
+    p.p_tiles = tiles_of(all);
+    const auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
+    const long long pt = d.len_prefill > 0 ? ceil_div(all, p.wide ? WIDE_OWN : 16 * p.p_tiles) : 0, st = ceil_div(own, p.wide ? WIDE_OWN : 16 * p.s_tiles);
+    const long long blocks = lh * (pt + c.n_streams * st), want = std::max(1ll, ceil_div(p.wide ? 512 : 1024, blocks));
     const auto splits_of = [&](int keys) {
-        const long long chunks = (keys + KC - 1) / KC;
-        return (int)std::max(1ll, std::min({want, (chunks + 2 * MASS_WAVES - 1) / (2 * MASS_WAVES), 32ll}));
+        const long long most = p.wide ? ceil_div(ceil_div(keys, WIDE_ROWS), 2) : ceil_div(ceil_div(keys, KC), 2 * MASS_WAVES);
+        return (int)std::max(1ll, std::min({want, most, 32ll}));
     };
     p.p_splits = d.len_prefill > 0 ? splits_of(d.len_prefill) : 0;
     p.s_splits = splits_of(c.cap);
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
+    const int many = c.head_dim == 64 ? 8 : 4, keys = MASS_WAVES * 16 * many;
+    p.key_tiles = lh * (ceil_div(d.len_prefill, keys) + c.n_streams * ceil_div(c.cap, keys)) < 512 ? 2 : many;
     return p;
 }
 int listed_rows(const mlora_attention_mass &d, int n_rows) { return n_rows > 0 ? n_rows : d.rows_per_stream; }
@@ -340,7 +746,7 @@ size_t bytes_of(const mlora_attention_mass &d, int N)
 {
     const Plan p = plan_of(d, N);
     const size_t vecs = (size_t)d.cache.n_streams * N * (d.n_q_heads / d.cache.n_kv_heads);
-    return (size_t)d.cache.n_layers * d.cache.n_kv_heads * (p.p_splits + p.s_splits) * vecs * sizeof(float2);
+    return (size_t)d.cache.n_layers * d.cache.n_kv_heads * (p.p_splits + p.s_splits + (p.wide ? 1 : 0)) * vecs * sizeof(float2) + (p.wide ? vecs * sizeof(int) : 0);
 }
 
 }  // namespace
@@ -395,19 +801,42 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
     a.s_blocks = p.s_blocks;
     a.scale2 = d->scale * 1.44269504088896340736f;
     a.decay = d->decay;
-    const long long lh = (long long)a.L * a.H, stats = lh * (a.p_blocks + (long long)a.S * a.s_blocks);
-    const long long add = lh * ((a.P + ADD_KEYS - 1) / ADD_KEYS + (long long)a.S * ((a.cap + ADD_KEYS - 1) / ADD_KEYS));
+    a.rows_ml = a.part + (size_t)a.L * a.H * (p.p_splits + p.s_splits) * a.vecs;
+    a.q_row = reinterpret_cast<int *>(a.rows_ml + (size_t)a.L * a.H * a.vecs);
+    const int keys = p.wide ? WIDE_OWN : MASS_WAVES * 16 * p.key_tiles;
+    a.p_tiles = (a.P + keys - 1) / keys;
+    a.s_tiles = (a.cap + keys - 1) / keys;
+    const long long lh = (long long)a.L * a.H, stats = lh * (a.p_blocks + (long long)a.S * a.s_blocks), add = lh * (a.p_tiles + (long long)a.S * a.s_tiles);
     if (stats > 0x7FFFFFFF || add > 0x7FFFFFFF) return MLORA_ESHAPE;
     hipStream_t s = (hipStream_t)stream;
-    const dim3 block(64 * MASS_WAVES);
-    if (c.head_dim == 64) {
-        if (p.tiles == 1) mass_stats<64, 1><<<dim3((unsigned)stats), block, 0, s>>>(a);
-        else              mass_stats<64, 4><<<dim3((unsigned)stats), block, 0, s>>>(a);
-        mass_add<64><<<dim3((unsigned)add), block, 0, s>>>(a);
+    const dim3 block(64 * MASS_WAVES), stats_grid((unsigned)stats), add_grid((unsigned)add);
+    const auto go = [&](auto dim, auto prefill_tiles, auto stream_tiles) {
+        mass_stats<decltype(dim)::value, decltype(prefill_tiles)::value, decltype(stream_tiles)::value><<<stats_grid, block, 0, s>>>(a);
+    };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 4> four{};
+    constexpr std::integral_constant<int, 8> eight{};
+    constexpr std::integral_constant<int, 64> d64{};
+    constexpr std::integral_constant<int, 128> d128{};
+    if (p.wide) {
+        const dim3 merge((unsigned)((lh * a.vecs + 255) / 256));
+        const auto wide = [&](auto dim) {
+            constexpr int D = decltype(dim)::value;
+            mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
+            mass_merge<<<merge, block, 0, s>>>(a);
+            mass_add_wide<D><<<add_grid, block, 0, s>>>(a);
+        };
+        c.head_dim == 64 ? wide(d64) : wide(d128);
+    } else if (c.head_dim == 64) {
+        if (p.s_tiles == 1) p.p_tiles == 1 ? go(d64, one, one) : p.p_tiles == 4 ? go(d64, four, one) : go(d64, eight, one);
+        else                p.p_tiles == 4 ? go(d64, four, four) : go(d64, eight, four);
+        if (p.key_tiles == 2) mass_add<64, 2><<<add_grid, block, 0, s>>>(a);
+        else                  mass_add<64, 8><<<add_grid, block, 0, s>>>(a);
     } else {
-        if (p.tiles == 1) mass_stats<128, 1><<<dim3((unsigned)stats), block, 0, s>>>(a);
-        else              mass_stats<128, 4><<<dim3((unsigned)stats), block, 0, s>>>(a);
-        mass_add<128><<<dim3((unsigned)add), block, 0, s>>>(a);
+        if (p.s_tiles == 1) p.p_tiles == 1 ? go(d128, one, one) : go(d128, four, one);
+        else                go(d128, four, four);
+        if (p.key_tiles == 2) mass_add<128, 2><<<add_grid, block, 0, s>>>(a);
+        else                  mass_add<128, 4><<<add_grid, block, 0, s>>>(a);
     }
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }

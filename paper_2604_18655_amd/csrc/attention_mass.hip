@@ -125,6 +125,18 @@ struct Unit {
         q = q_at(a, l, h, st, row, g, D);
         return true;
     }
+    // the same where it may be any vector if v does not count
+    __device__ __forceinline__ size_t some_vector(const MassArgs &a, int v, int D) const
+    {
+        const int j = v / a.G, g = v - j * a.G;
+        int st = s, row = j;
+        if (prefill) st = j / a.N, row = j - st * a.N;
+        if (a.rows) {
+            row = a.rows[(size_t)st * a.N + row];
+            row = row >= 0 && row < a.R ? row : 0;
+        }
+        return ((((size_t)l * a.S + st) * a.R + row) * a.H * a.G + h * a.G + g) * D;
+    }
 };
 
 // Maximum and sum of QT tiles of 16 query vectors over a share of the keys.
@@ -163,9 +175,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int v = min(v0 + 16 * t + l16, w.vecs - 1);
-        size_t q;
-        int number;
-        w.vector(a, v, D, q, number);
+        const size_t q = w.some_vector(a, v, D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
         pos[t] = w.newest + v / a.G;
@@ -261,8 +271,9 @@ __device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int numbe
     return make_float2(top, all > 0.f ? 1.f / all : all);            // (NaN stays)
 }
 
-// One block: KT tiles of 16 keys per wave against all query vectors that may see them.
-template <int D, int KT>
+// One block: KT tiles of 16 keys per wave against all query vectors that may see them.  TABLE: their maxima, sums and places have been
+// written down (mass_stream).
+template <int D, int KT, bool TABLE>
 __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 {
     constexpr int DK = D / 32, KEYS = MASS_WAVES * KT * 16;
@@ -293,14 +304,21 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
         if (base > 0) __syncthreads();
         for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
             const int v = min(base + i, w.vecs - 1);
-            size_t q;
-            int number;
-            const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
-            const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NEG_BIG, 0.f);
-            top_of[i] = row.x;
-            inv_of[i] = row.y;
-            pos_of[i] = w.newest + v / a.G;
-            q_of[i] = a.q + q;
+            if constexpr (TABLE) {
+                const float2 row = a.rows_ml[(size_t)w.lh * a.vecs + v];
+                top_of[i] = row.x;
+                inv_of[i] = base + i < w.vecs ? row.y : 0.f;
+                q_of[i] = a.q + (((size_t)w.l * a.S * a.R * a.H + w.h) * a.G + max(a.q_row[v], 0)) * D;
+            } else {
+                size_t q;
+                int number;
+                const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
+                const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NEG_BIG, 0.f);
+                top_of[i] = row.x;
+                inv_of[i] = row.y;
+                pos_of[i] = w.newest + v / a.G;
+                q_of[i] = a.q + q;
+            }
         }
         __syncthreads();
         bool masked = false;
@@ -334,6 +352,166 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
         const int key = k0 + 16 * t + l16;
         float *const to = (w.prefill ? a.mass_prefill : a.mass) + w.at + key;
         if (lq == 0 && key < w.keys) *to = a.decay * *to + add;
+    }
+}
+
+// Few query vectors (VT tiles of 16) on a stream's own segment that a block holds at once: its scores stay in registers, and one pass over the keys is
+// all there is.  The prefill segment's maxima and sums are there already (mass_stats); what its masses need is left behind.
+constexpr int STREAM_WAVES = 8;
+constexpr int stream_keys(int TK) { return STREAM_WAVES * 16 * TK; }
+
+// a value combined over the 16 lanes of a quarter of the wave; every lane gets the result
+template <class Op>
+__device__ __forceinline__ float over_sixteen(float v, const Op &op)
+{
+    const auto ror = [](float x, auto n) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(n)::value, 0xF, 0xF, false));
+    };
+    v = op(v, ror(v, std::integral_constant<int, 8>{}));
+    v = op(v, ror(v, std::integral_constant<int, 4>{}));
+    v = op(v, ror(v, std::integral_constant<int, 2>{}));
+    return op(v, ror(v, std::integral_constant<int, 1>{}));
+}
+
+template <int D, int VT, int TK>
+__global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs a)
+{
+    constexpr int DK = D / 32, AHEAD = D == 64 ? (TK < 4 ? TK : 4) : 2, V = 16 * VT;
+    __shared__ __align__(16) float tops[STREAM_WAVES][V], sums[STREAM_WAVES][V], p_top[V], p_sum[V];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
+    const Unit w(a, 0, 1, D);
+    // tiles of 16 keys: wave, wave + 8, ..; past the end: the last key
+    const int tiles = (w.keys + 15) / 16;
+    const auto key_of = [&](int t) { return (t * STREAM_WAVES + wave) * 16 + l16; };
+    const int last = max(w.keys - 1, 0);
+    uint4 kf[AHEAD][DK];
+    int at[TK];
+    const auto ask = [&](int t) {
+        const int key = min(key_of(t), last);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) kf[t % AHEAD][kk] = *reinterpret_cast<const uint4 *>(w.k + (size_t)key * D + 8 * lq + 32 * kk);
+    };
+#pragma unroll
+    for (int t = 0; t < TK; ++t) at[t] = w.pos[min(key_of(t), last)];
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) ask(t);
+    uint4 qf[VT][DK];
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+        const size_t q = w.some_vector(a, min(16 * v + l16, a.N * a.G - 1), D);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) qf[v][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
+    }
+    float *const mass = a.mass + w.at;
+    float old[TK];
+#pragma unroll
+    for (int t = 0; t < TK; ++t) old[t] = mass[min(key_of(t), last)];
+    const int own = w.s * a.N * a.G;
+    if (tid < V) {
+        // this vector on the prefill segment
+        float top = NEG_BIG, all = 0.f;
+        if (tid < w.vecs) {
+            const float2 *const part = a.part + (size_t)w.lh * a.p_splits * a.vecs + own + tid;
+            for (int z = 0; z < a.p_splits; ++z) {
+                const float2 x = part[(size_t)z * a.vecs];
+                const float t2 = fmaxf(top, x.x);
+                all = all * __builtin_amdgcn_exp2f(top - t2) + x.y * __builtin_amdgcn_exp2f(x.x - t2);
+                top = t2;
+            }
+        }
+        p_top[tid] = top;
+        p_sum[tid] = all;
+    }
+    int pos[VT][4];
+    float top[VT][4], sum[VT][4];
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            pos[v][e] = w.newest + (16 * v + 4 * lq + e) / a.G;
+            top[v][e] = NEG_BIG;
+            sum[v][e] = 0.f;
+        }
+    // scores: element e of sc[v][t] is vector 16 * v + 4 * lq + e against key l16 of tile t
+    f32x4 sc[VT][TK];
+#pragma unroll
+    for (int t = 0; t < TK; ++t) {
+        const bool live = key_of(t) < w.keys;
+#pragma unroll
+        for (int v = 0; v < VT; ++v) {
+            sc[v][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < DK; ++kk) sc[v][t] = mfma16(qf[v][kk], kf[t % AHEAD][kk], sc[v][t]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sc[v][t][e] = live && at[t] <= pos[v][e] ? sc[v][t][e] * a.scale2 : UNSEEN;
+                top[v][e] = fmaxf(top[v][e], sc[v][t][e]);
+            }
+        }
+        if (t + AHEAD < TK) ask(t + AHEAD);
+    }
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            top[v][e] = over_sixteen(top[v][e], [](float x, float y) { return fmaxf(x, y); });
+            if (l16 == 0) tops[wave][16 * v + 4 * lq + e] = top[v][e];
+        }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+        f32x4 m = *reinterpret_cast<const f32x4 *>(&tops[0][16 * v + 4 * lq]);
+#pragma unroll
+        for (int i = 1; i < STREAM_WAVES; ++i) {
+            const f32x4 o = *reinterpret_cast<const f32x4 *>(&tops[i][16 * v + 4 * lq]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], o[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            top[v][e] = m[e];
+#pragma unroll
+            for (int t = 0; t < TK; ++t) {
+                sc[v][t][e] = __builtin_amdgcn_exp2f(sc[v][t][e] - m[e]);
+                sum[v][e] += sc[v][t][e];
+            }
+            sum[v][e] = over_sixteen(sum[v][e], [](float x, float y) { return x + y; });
+            if (l16 == 0) sums[wave][16 * v + 4 * lq + e] = sum[v][e];
+        }
+    }
+    __syncthreads();
+    float factor[VT][4];                                             // of a vector's weights
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < STREAM_WAVES; ++i) all += *reinterpret_cast<const f32x4 *>(&sums[i][16 * v + 4 * lq]);
+        const f32x4 pt = *reinterpret_cast<const f32x4 *>(&p_top[16 * v + 4 * lq]), ps = *reinterpret_cast<const f32x4 *>(&p_sum[16 * v + 4 * lq]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int vec = 16 * v + 4 * lq + e;
+            const float m = fmaxf(top[v][e], pt[e]), here = __builtin_amdgcn_exp2f(top[v][e] - m);
+            const float total = all[e] * here + ps[e] * __builtin_amdgcn_exp2f(pt[e] - m), inv = total > 0.f ? 1.f / total : total;      // (NaN stays)
+            const bool counts = vec < w.vecs;
+            factor[v][e] = counts ? here * inv : 0.f;
+            if (a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
+                a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(m, counts ? inv : 0.f);
+                if (w.lh == 0) {
+                    const int j = vec / a.G;
+                    a.q_row[own + vec] = counts ? (w.s * a.R + (a.rows ? a.rows[(size_t)w.s * a.N + j] : j)) * a.H * a.G + vec - j * a.G : -1;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < TK; ++t) {
+        float add = 0.f;
+#pragma unroll
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add += factor[v][e] != 0.f ? sc[v][t][e] * factor[v][e] : 0.f;
+        add = over_quarters(add, [](float x, float y) { return x + y; });
+        if (lq == 0 && key_of(t) < w.keys) mass[key_of(t)] = a.decay * old[t] + add;
     }
 }
 
@@ -408,9 +586,7 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int v = min(mine + 32 * t + l32, w.vecs - 1);
-        size_t q;
-        int number;
-        w.vector(a, v, D, q, number);
+        const size_t q = w.some_vector(a, v, D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const u32x4 *>(a.q + q + 16 * kk + 8 * lh2);
         pos[t] = w.prefill ? 0 : w.newest + v / a.G;
@@ -711,6 +887,8 @@ mlora_status check(const mlora_attention_mass *d)
 // has fewer than two chunks per wave left.
 struct Plan {
     bool wide;
+    int stream;                          // 0, or the key tiles of a wave in mass_stream
+    int stream_vecs;                     // its vector tiles
     int p_tiles, s_tiles;                // query tiles of a block: prefill, stream segment
     int p_splits, s_splits, p_blocks, s_blocks;
     int key_tiles;                       // key tiles of a wave in mass_add
@@ -723,22 +901,25 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     Plan p;
     // (a layer's query vectors are reached by 32-bit offsets)
     p.wide = d.scale > 0.f && own >= WIDE_OWN && d.n_q_heads <= 1024;
+    p.stream_vecs = own <= 16 ? 1 : 2;
+    p.stream = p.wide || own > 32 || c.cap > stream_keys(own <= 16 ? 16 : 9) ? 0 : c.cap <= stream_keys(4) ? 4 : c.cap <= stream_keys(9) ? 9 : 16;
+    if (d.len_prefill > 0 && lh * c.n_streams < 256) p.stream = 0;
     const auto tiles_of = [&](long long vecs) { return vecs <= 16 ? 1 : c.head_dim == 64 && vecs > 64 ? 8 : 4; };
     p.s_tiles = own <= 16 ? 1 : 4;
     p.p_tiles = tiles_of(all);
     const auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
     const long long pt = d.len_prefill > 0 ? ceil_div(all, p.wide ? WIDE_OWN : 16 * p.p_tiles) : 0, st = ceil_div(own, p.wide ? WIDE_OWN : 16 * p.s_tiles);
-    const long long blocks = lh * (pt + c.n_streams * st), want = std::max(1ll, ceil_div(p.wide ? 512 : 1024, blocks));
+    const long long blocks = std::max(1ll, lh * (pt + (p.stream ? 0 : c.n_streams * st))), want = std::max(1ll, ceil_div(p.wide ? 512 : 1024, blocks));
     const auto splits_of = [&](int keys) {
         const long long most = p.wide ? ceil_div(ceil_div(keys, WIDE_ROWS), 2) : ceil_div(ceil_div(keys, KC), 2 * MASS_WAVES);
         return (int)std::max(1ll, std::min({want, most, 32ll}));
     };
     p.p_splits = d.len_prefill > 0 ? splits_of(d.len_prefill) : 0;
-    p.s_splits = splits_of(c.cap);
+    p.s_splits = p.stream ? 0 : splits_of(c.cap);
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
     const int many = c.head_dim == 64 ? 8 : 4, keys = MASS_WAVES * 16 * many;
-    p.key_tiles = lh * (ceil_div(d.len_prefill, keys) + c.n_streams * ceil_div(c.cap, keys)) < 512 ? 2 : many;
+    p.key_tiles = lh * (ceil_div(d.len_prefill, keys) + (p.stream ? 0 : c.n_streams * ceil_div(c.cap, keys))) < 512 ? 2 : many;
     return p;
 }
 int listed_rows(const mlora_attention_mass &d, int n_rows) { return n_rows > 0 ? n_rows : d.rows_per_stream; }
@@ -746,7 +927,7 @@ size_t bytes_of(const mlora_attention_mass &d, int N)
 {
     const Plan p = plan_of(d, N);
     const size_t vecs = (size_t)d.cache.n_streams * N * (d.n_q_heads / d.cache.n_kv_heads);
-    return (size_t)d.cache.n_layers * d.cache.n_kv_heads * (p.p_splits + p.s_splits + (p.wide ? 1 : 0)) * vecs * sizeof(float2) + (p.wide ? vecs * sizeof(int) : 0);
+    return (size_t)d.cache.n_layers * d.cache.n_kv_heads * (p.p_splits + p.s_splits + 1) * vecs * sizeof(float2) + vecs * sizeof(int);
 }
 
 }  // namespace
@@ -805,39 +986,50 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
     a.q_row = reinterpret_cast<int *>(a.rows_ml + (size_t)a.L * a.H * a.vecs);
     const int keys = p.wide ? WIDE_OWN : MASS_WAVES * 16 * p.key_tiles;
     a.p_tiles = (a.P + keys - 1) / keys;
-    a.s_tiles = (a.cap + keys - 1) / keys;
+    a.s_tiles = p.stream ? 0 : (a.cap + keys - 1) / keys;
     const long long lh = (long long)a.L * a.H, stats = lh * (a.p_blocks + (long long)a.S * a.s_blocks), add = lh * (a.p_tiles + (long long)a.S * a.s_tiles);
     if (stats > 0x7FFFFFFF || add > 0x7FFFFFFF) return MLORA_ESHAPE;
     hipStream_t s = (hipStream_t)stream;
     const dim3 block(64 * MASS_WAVES), stats_grid((unsigned)stats), add_grid((unsigned)add);
-    const auto go = [&](auto dim, auto prefill_tiles, auto stream_tiles) {
-        mass_stats<decltype(dim)::value, decltype(prefill_tiles)::value, decltype(stream_tiles)::value><<<stats_grid, block, 0, s>>>(a);
-    };
-    constexpr std::integral_constant<int, 1> one{};
-    constexpr std::integral_constant<int, 4> four{};
-    constexpr std::integral_constant<int, 8> eight{};
-    constexpr std::integral_constant<int, 64> d64{};
-    constexpr std::integral_constant<int, 128> d128{};
-    if (p.wide) {
-        const dim3 merge((unsigned)((lh * a.vecs + 255) / 256));
-        const auto wide = [&](auto dim) {
-            constexpr int D = decltype(dim)::value;
-            mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
-            mass_merge<<<merge, block, 0, s>>>(a);
-            mass_add_wide<D><<<add_grid, block, 0, s>>>(a);
+    const auto all = [&](auto dim) {
+        constexpr int D = decltype(dim)::value, MANY = D == 64 ? 8 : 4;
+        const auto stats = [&](auto prefill_tiles, auto stream_tiles) {
+            mass_stats<D, decltype(prefill_tiles)::value, decltype(stream_tiles)::value><<<stats_grid, block, 0, s>>>(a);
         };
-        c.head_dim == 64 ? wide(d64) : wide(d128);
-    } else if (c.head_dim == 64) {
-        if (p.s_tiles == 1) p.p_tiles == 1 ? go(d64, one, one) : p.p_tiles == 4 ? go(d64, four, one) : go(d64, eight, one);
-        else                p.p_tiles == 4 ? go(d64, four, four) : go(d64, eight, four);
-        if (p.key_tiles == 2) mass_add<64, 2><<<add_grid, block, 0, s>>>(a);
-        else                  mass_add<64, 8><<<add_grid, block, 0, s>>>(a);
-    } else {
-        if (p.s_tiles == 1) p.p_tiles == 1 ? go(d128, one, one) : go(d128, four, one);
-        else                go(d128, four, four);
-        if (p.key_tiles == 2) mass_add<128, 2><<<add_grid, block, 0, s>>>(a);
-        else                  mass_add<128, 4><<<add_grid, block, 0, s>>>(a);
-    }
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 4> four{};
+        constexpr std::integral_constant<int, MANY> many{};
+        const auto narrow_stats = [&] {
+            if (p.s_tiles == 1) p.p_tiles == 1 ? stats(one, one) : p.p_tiles == 4 ? stats(four, one) : stats(many, one);
+            else                p.p_tiles <= 4 ? stats(four, four) : stats(many, four);
+        };
+        if (p.wide) {
+            mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
+            mass_merge<<<dim3((unsigned)((lh * a.vecs + 255) / 256)), block, 0, s>>>(a);
+            mass_add_wide<D><<<add_grid, block, 0, s>>>(a);
+        } else if (p.stream) {
+            if (a.P > 0) narrow_stats();
+            const dim3 grid((unsigned)(lh * a.S)), wide_block(64 * STREAM_WAVES);
+            if (p.stream_vecs == 1) {
+                if (p.stream == 4)      mass_stream<D, 1, 4><<<grid, wide_block, 0, s>>>(a);
+                else if (p.stream == 9) mass_stream<D, 1, 9><<<grid, wide_block, 0, s>>>(a);
+                else                    mass_stream<D, 1, 16><<<grid, wide_block, 0, s>>>(a);
+            } else {
+                if (p.stream == 4) mass_stream<D, 2, 4><<<grid, wide_block, 0, s>>>(a);
+                else               mass_stream<D, 2, 9><<<grid, wide_block, 0, s>>>(a);
+            }
+            if (a.P > 0) {
+                if (p.key_tiles == 2) mass_add<D, 2, true><<<add_grid, block, 0, s>>>(a);
+                else                  mass_add<D, MANY, true><<<add_grid, block, 0, s>>>(a);
+            }
+        } else {
+            narrow_stats();
+            if (p.key_tiles == 2) mass_add<D, 2, false><<<add_grid, block, 0, s>>>(a);
+            else                  mass_add<D, MANY, false><<<add_grid, block, 0, s>>>(a);
+        }
+    };
+    if (c.head_dim == 64) all(std::integral_constant<int, 64>{});
+    else                  all(std::integral_constant<int, 128>{});
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }
 

@@ -27,6 +27,7 @@ constexpr int KC = 32;                   // keys of a chunk in mass_stats
 constexpr int BATCH = 512;               // query vectors whose maxima mass_add holds at a time
 constexpr float NEG_BIG = -1.0e30f;      // "no key seen yet"
 constexpr float UNSEEN = -3.0e38f;       // score of a key that is not visible: exp2(UNSEEN - NEG_BIG) is 0
+constexpr float FAR = 1.0995e12f;        // 2^40: how far sums may grow above their maximum before they are scaled down
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -105,10 +106,11 @@ struct Unit {
             s = number / s_blocks;
             number -= s * s_blocks;
         }
+        keys = prefill ? a.P : max(0, min(a.len[s], a.cap));         // (asked for before the list is looked at)
+        newest = prefill ? 0 : a.next_pos[s];
         n = prefill ? 0 : listed(a, s);
-        newest = prefill ? 0 : a.next_pos[s] - n;
+        newest -= n;
         vecs = prefill ? a.vecs : n * a.G;
-        keys = prefill ? a.P : max(0, min(a.len[s], a.cap));
         at = prefill ? (size_t)lh * a.P : (((size_t)l * a.S + s) * a.H + h) * a.cap;
         k = (prefill ? a.k_prefill : a.k) + at * D;
         pos = a.slot_pos + at;
@@ -149,7 +151,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
     const int v0 = tile * QT * 16;
     if (v0 >= w.vecs) return;
 
-    // keys as A operands (past the end: the last key), a chunk ahead of the one that is worked on
+    // keys as A operands (past the end: the last key), some chunks ahead of the one that is worked on
     struct Keys {
         uint4 f[KC / 16][DK];
         int pos;
@@ -165,9 +167,6 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         }
         x.pos = w.prefill ? 0 : w.pos[min(k0 + (lane & 31), last)];
     };
-    Keys even, odd;
-    int c = z * MASS_WAVES + wave;
-    if (c < chunks) ask(even, c);
     // this lane's query vectors (B operands: lane (l16, lq) holds features 8 * lq .. of vector l16 of a tile)
     uint4 qf[QT][DK];
     float m[QT], sum[QT];
@@ -182,6 +181,14 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         m[t] = NEG_BIG;
         sum[t] = 0.f;
     }
+    // (the keys come after the vectors: loads return in their order, and these are what all products need.  With the keys
+    // first the products started after 9 us of a launch's 20.)
+    constexpr int AHEAD = D == 64 ? 4 : 2;                           // chunks on their way
+    Keys ring[AHEAD];
+    int c = z * MASS_WAVES + wave;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (c + i * stride < chunks) ask(ring[i], c + i * stride);
     const auto work = [&](const Keys &x, int c) {
         const int nk = min(KC, w.keys - c * KC);
         const bool masked = nk < KC || (!w.prefill && __any(x.pos > w.newest));
@@ -194,38 +201,54 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
                 sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < DK; ++kk) sc[j] = mfma16(x.f[j][kk], qf[t][kk], sc[j]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[j][e] *= a.scale2;
             }
+            unsigned see = ~0u;                                      // a bit per score
             if (masked) {
+                see = 0;
 #pragma unroll
                 for (int j = 0; j < KC / 16; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = 16 * j + 4 * lq + e;
                         const int key_pos = __shfl(x.pos, key);      // (all lanes: before any condition)
-                        sc[j][e] = key < nk && (w.prefill || key_pos <= pos[t]) ? sc[j][e] : UNSEEN;
+                        see |= key < nk && (w.prefill || key_pos <= pos[t]) ? 1u << (4 * j + e) : 0u;
                     }
             }
-            float top = m[t];
+            // sums relative to a maximum that may lie behind: the sum itself tells when it does too far
+            float add[2] = {0.f, 0.f};
+            const auto take = [&](bool all) {
 #pragma unroll
-            for (int j = 0; j < KC / 16; ++j)
+                for (int j = 0; j < KC / 16; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[j][e]);
-            float add = 0.f;
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[j][e], a.scale2, -m[t]));
+                        add[j & 1] += all || see >> (4 * j + e) & 1 ? p : 0.f;
+                    }
+            };
+            if (!masked) take(true);
+            else         take(false);
+            if (__any(add[0] + add[1] > FAR)) {                      // (the first chunk, and rarely another)
+                float top = m[t];
 #pragma unroll
-            for (int j = 0; j < KC / 16; ++j)
+                for (int j = 0; j < KC / 16; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) add += __builtin_amdgcn_exp2f(sc[j][e] - top);
-            sum[t] = sum[t] * __builtin_amdgcn_exp2f(m[t] - top) + add;
-            m[t] = top;
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, see >> (4 * j + e) & 1 ? sc[j][e] * a.scale2 : UNSEEN);
+                sum[t] *= __builtin_amdgcn_exp2f(m[t] - top);
+                m[t] = top;
+                add[0] = add[1] = 0.f;
+                take(false);
+            }
+            sum[t] += add[0] + add[1];
         }
     };
-    for (; c < chunks; c += 2 * stride) {
-        if (c + stride < chunks) ask(odd, c + stride);
-        work(even, c);
-        if (c + 2 * stride < chunks) ask(even, c + 2 * stride);
-        if (c + stride < chunks) work(odd, c + stride);
+    while (c < chunks) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (c >= chunks) break;
+            work(ring[i], c);
+            if (c + AHEAD * stride < chunks) ask(ring[i], c + AHEAD * stride);
+            c += stride;
+        }
     }
     // the quarters' keys, then the waves'
 #pragma unroll
@@ -256,18 +279,28 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
     else                       stats_tiles<D, QT>(a, w, ml);
 }
 
+// maximum and sum over what blocks left, four trips at a time
+__device__ __forceinline__ void merge_parts(const float2 *part, int n, int stride, float &top, float &all)
+{
+    for (int z0 = 0; z0 < n; z0 += 4) {
+        float2 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = part[(size_t)min(z0 + u, n - 1) * stride];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (z0 + u >= n) break;
+            const float t2 = fmaxf(top, x[u].x);
+            all = all * __builtin_amdgcn_exp2f(top - t2) + x[u].y * __builtin_amdgcn_exp2f(x[u].x - t2);
+            top = t2;
+        }
+    }
+}
 // maximum and 1 / sum of a query vector over all blocks that looked at its keys; a row that sees nothing: 0
 __device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int number)
 {
     const int splits = a.p_splits + a.s_splits;
-    const float2 *const part = a.part + (size_t)lh * splits * a.vecs + number;
     float top = NEG_BIG, all = 0.f;
-    for (int z = 0; z < splits; ++z) {
-        const float2 x = part[(size_t)z * a.vecs];
-        const float t2 = fmaxf(top, x.x);
-        all = all * __builtin_amdgcn_exp2f(top - t2) + x.y * __builtin_amdgcn_exp2f(x.x - t2);
-        top = t2;
-    }
+    merge_parts(a.part + (size_t)lh * splits * a.vecs + number, splits, a.vecs, top, all);
     return make_float2(top, all > 0.f ? 1.f / all : all);            // (NaN stays)
 }
 
@@ -285,13 +318,40 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     if (w.number * KEYS >= w.keys) return;
     const int k0 = w.number * KEYS + wave * KT * 16;
 
+    const auto look_up = [&](int base, int pad) {
+        for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
+            const int v = min(base + i, w.vecs - 1);
+            if constexpr (TABLE) {
+                const float2 row = a.rows_ml[(size_t)w.lh * a.vecs + v];
+                const int at_row = a.q_row[v];
+                const bool ok = at_row >= 0 && base + i < w.vecs;
+                top_of[i] = ok ? row.x : 1e30f;
+                inv_of[i] = ok ? row.y : 0.f;
+                q_of[i] = a.q + (((size_t)w.l * a.S * a.R * a.H + w.h) * a.G + max(at_row, 0)) * D;
+            } else {
+                size_t q;
+                int number;
+                const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
+                const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(1e30f, 0.f);
+                top_of[i] = row.x;
+                inv_of[i] = row.y;
+                pos_of[i] = w.newest + v / a.G;
+                q_of[i] = a.q + q;
+            }
+        }
+    };
+    // (the first vectors are looked up before the keys are asked for: loads return in their order)
+    look_up(0, (min(BATCH, w.vecs) + 15) / 16 * 16);
+
     // this lane's keys (B operands)
     uint4 kf[KT][DK];
     int at[KT];
-    float acc[KT];
+    float acc[KT], old[KT];
+    float *const mass = (w.prefill ? a.mass_prefill : a.mass) + w.at;
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
         const int key = min(k0 + 16 * t + l16, w.keys - 1);
+        old[t] = mass[key];
         const uint16_t *const kp = w.k + (size_t)key * D + 8 * lq;
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
@@ -301,36 +361,34 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 
     for (int base = 0; base < w.vecs; base += BATCH) {
         const int here = min(BATCH, w.vecs - base), pad = (here + 15) / 16 * 16;
-        if (base > 0) __syncthreads();
-        for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
-            const int v = min(base + i, w.vecs - 1);
-            if constexpr (TABLE) {
-                const float2 row = a.rows_ml[(size_t)w.lh * a.vecs + v];
-                top_of[i] = row.x;
-                inv_of[i] = base + i < w.vecs ? row.y : 0.f;
-                q_of[i] = a.q + (((size_t)w.l * a.S * a.R * a.H + w.h) * a.G + max(a.q_row[v], 0)) * D;
-            } else {
-                size_t q;
-                int number;
-                const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
-                const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NEG_BIG, 0.f);
-                top_of[i] = row.x;
-                inv_of[i] = row.y;
-                pos_of[i] = w.newest + v / a.G;
-                q_of[i] = a.q + q;
-            }
+        if (base > 0) {
+            __syncthreads();
+            look_up(base, pad);
         }
         __syncthreads();
         bool masked = false;
 #pragma unroll
         for (int t = 0; t < KT; ++t) masked |= !w.prefill && at[t] > w.newest;
         masked = __any(masked);
-        for (int t0 = 0; t0 < pad; t0 += 16) {
-            // query vectors as A operands: element e of a score belongs to vector 4 * lq + e
-            uint4 qf[DK];
-            const uint16_t *const qp = q_of[t0 + l16] + 8 * lq;
+        // query vectors as A operands, a tile ahead: element e of a score belongs to vector 4 * lq + e
+        uint4 qn[DK];
+        const auto ask = [&](int t0) {
+            const uint16_t *const qp = q_of[min(t0, pad - 16) + l16] + 8 * lq;
 #pragma unroll
-            for (int kk = 0; kk < DK; ++kk) qf[kk] = *reinterpret_cast<const uint4 *>(qp + 32 * kk);
+            for (int kk = 0; kk < DK; ++kk) qn[kk] = *reinterpret_cast<const uint4 *>(qp + 32 * kk);
+        };
+        ask(0);
+        for (int t0 = 0; t0 < pad; t0 += 16) {
+            uint4 qf[DK];
+#pragma unroll
+            for (int kk = 0; kk < DK; ++kk) qf[kk] = qn[kk];
+            // (vectors that do not count are zeros: what their place holds may be NaN)
+            const bool bad = top_of[t0 + l16] >= 1e30f;
+            if (__any(bad)) {
+#pragma unroll
+                for (int kk = 0; kk < DK; ++kk) qf[kk] = bad ? make_uint4(0, 0, 0, 0) : qf[kk];
+            }
+            ask(t0 + 16);
             const f32x4 top = *reinterpret_cast<const f32x4 *>(top_of + t0 + 4 * lq), inv = *reinterpret_cast<const f32x4 *>(inv_of + t0 + 4 * lq);
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
@@ -339,9 +397,9 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
                 for (int kk = 0; kk < DK; ++kk) sc = mfma16(qf[kk], kf[t][kk], sc);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float x = __builtin_amdgcn_exp2f(sc[e] * a.scale2 - top[e]) * inv[e];
+                    float x = __builtin_amdgcn_exp2f(fmaf(sc[e], a.scale2, -top[e]));
                     if (masked) x = at[t] <= pos_of[t0 + 4 * lq + e] ? x : 0.f;
-                    acc[t] += inv[e] != 0.f ? x : 0.f;
+                    acc[t] = fmaf(x, inv[e], acc[t]);
                 }
             }
         }
@@ -350,8 +408,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     for (int t = 0; t < KT; ++t) {
         const float add = over_quarters(acc[t], [](float x, float y) { return x + y; });
         const int key = k0 + 16 * t + l16;
-        float *const to = (w.prefill ? a.mass_prefill : a.mass) + w.at + key;
-        if (lq == 0 && key < w.keys) *to = a.decay * *to + add;
+        if (lq == 0 && key < w.keys) mass[key] = a.decay * old[t] + add;
     }
 }
 
@@ -381,9 +438,24 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const Unit w(a, 0, 1, D);
     // tiles of 16 keys: wave, wave + 8, ..; past the end: the last key
-    const int tiles = (w.keys + 15) / 16;
     const auto key_of = [&](int t) { return (t * STREAM_WAVES + wave) * 16 + l16; };
     const int last = max(w.keys - 1, 0);
+    // (vectors and what the prefill segment left come before the keys: loads return in their order)
+    uint4 qf[VT][DK];
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+        const size_t q = w.some_vector(a, min(16 * v + l16, a.N * a.G - 1), D);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) qf[v][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
+    }
+    const int own = w.s * a.N * a.G;
+    if (tid < V) {
+        // this vector on the prefill segment
+        float top = NEG_BIG, all = 0.f;
+        if (tid < w.vecs && a.P > 0) merge_parts(a.part + (size_t)w.lh * a.p_splits * a.vecs + own + tid, a.p_splits, a.vecs, top, all);
+        p_top[tid] = top;
+        p_sum[tid] = all;
+    }
     uint4 kf[AHEAD][DK];
     int at[TK];
     const auto ask = [&](int t) {
@@ -395,33 +467,10 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     for (int t = 0; t < TK; ++t) at[t] = w.pos[min(key_of(t), last)];
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) ask(t);
-    uint4 qf[VT][DK];
-#pragma unroll
-    for (int v = 0; v < VT; ++v) {
-        const size_t q = w.some_vector(a, min(16 * v + l16, a.N * a.G - 1), D);
-#pragma unroll
-        for (int kk = 0; kk < DK; ++kk) qf[v][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
-    }
     float *const mass = a.mass + w.at;
     float old[TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t) old[t] = mass[min(key_of(t), last)];
-    const int own = w.s * a.N * a.G;
-    if (tid < V) {
-        // this vector on the prefill segment
-        float top = NEG_BIG, all = 0.f;
-        if (tid < w.vecs) {
-            const float2 *const part = a.part + (size_t)w.lh * a.p_splits * a.vecs + own + tid;
-            for (int z = 0; z < a.p_splits; ++z) {
-                const float2 x = part[(size_t)z * a.vecs];
-                const float t2 = fmaxf(top, x.x);
-                all = all * __builtin_amdgcn_exp2f(top - t2) + x.y * __builtin_amdgcn_exp2f(x.x - t2);
-                top = t2;
-            }
-        }
-        p_top[tid] = top;
-        p_sum[tid] = all;
-    }
     int pos[VT][4];
     float top[VT][4], sum[VT][4];
 #pragma unroll
@@ -523,7 +572,6 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
 // ---------------------------------------------------------------------------------------------
 constexpr int WIDE_ROWS = 64;            // rows of a chunk
 constexpr int WIDE_OWN = 256;            // vectors or keys of a block
-constexpr float FAR = 1.0995e12f;        // 2^40: how far sums may grow above their maximum before they are scaled down
 
 template <int D>
 struct Stage {
@@ -700,15 +748,26 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
     }
 }
 
-// Every query vector's maximum and 1 / sum, once for the blocks of mass_add_wide.  A vector that does not count: a maximum that
-// makes all weights 0.
+// Every query vector's maximum and 1 / sum, once for the blocks of mass_add_wide: eight lanes take turns with what the blocks of
+// mass_stats_wide left (one lane by itself: 9 us for 32 of them).  A vector that does not count: a maximum that makes all weights 0.
 __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (long long)a.L * a.H * a.vecs) return;
-    const int lh = (int)(i / a.vecs), number = (int)(i - (long long)lh * a.vecs), j = number / a.G, s = j / a.N;
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 8, all = (long long)a.L * a.H * a.vecs;
+    const int lane = (int)threadIdx.x % 8;
+    const long long at = i < all ? i : all - 1;
+    const int lh = (int)(at / a.vecs), number = (int)(at - (long long)lh * a.vecs), j = number / a.G, s = j / a.N, splits = a.p_splits + a.s_splits;
+    float top = NEG_BIG, sum = 0.f;
+    if (lane < splits)
+        merge_parts(a.part + ((size_t)lh * splits + lane) * a.vecs + number, (splits - lane + 7) / 8, 8 * a.vecs, top, sum);
     const bool ok = counts(a, s, j - s * a.N);
-    a.rows_ml[i] = ok ? whole_row(a, lh, number) : make_float2(1e30f, 0.f);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+        const float ot = __shfl_xor(top, d), os = __shfl_xor(sum, d), high = fmaxf(top, ot);
+        sum = sum * __builtin_amdgcn_exp2f(top - high) + os * __builtin_amdgcn_exp2f(ot - high);
+        top = high;
+    }
+    if (i >= all || lane != 0) return;
+    a.rows_ml[i] = ok ? make_float2(top, sum > 0.f ? 1.f / sum : sum) : make_float2(1e30f, 0.f);      // (a row that sees nothing adds nothing; NaN stays)
     if (lh == 0) a.q_row[number] = ok ? (s * a.R + (a.rows ? a.rows[j] : j - s * a.N)) * a.H * a.G + number - j * a.G : -1;
 }
 
@@ -883,8 +942,8 @@ mlora_status check(const mlora_attention_mass *d)
     return MLORA_OK;
 }
 
-// How a call is cut: blocks that share a query tile's keys, until the launch has about four blocks per compute unit or a block
-// has fewer than two chunks per wave left.
+// How a call is cut: blocks that share a query tile's keys, until the launch has about two blocks per compute unit (four: 8 streams of
+// 1500 slots, 36 query vectors of 128 features 17.0 -> 19.6 us) or a block has fewer than two chunks per wave left.
 struct Plan {
     bool wide;
     int stream;                          // 0, or the key tiles of a wave in mass_stream
@@ -904,12 +963,12 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     p.stream_vecs = own <= 16 ? 1 : 2;
     p.stream = p.wide || own > 32 || c.cap > stream_keys(own <= 16 ? 16 : 9) ? 0 : c.cap <= stream_keys(4) ? 4 : c.cap <= stream_keys(9) ? 9 : 16;
     if (d.len_prefill > 0 && lh * c.n_streams < 256) p.stream = 0;
-    const auto tiles_of = [&](long long vecs) { return vecs <= 16 ? 1 : c.head_dim == 64 && vecs > 64 ? 8 : 4; };
+    const auto tiles_of = [&](long long vecs) { return vecs <= 16 ? 1 : 4; };
     p.s_tiles = own <= 16 ? 1 : 4;
     p.p_tiles = tiles_of(all);
     const auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
     const long long pt = d.len_prefill > 0 ? ceil_div(all, p.wide ? WIDE_OWN : 16 * p.p_tiles) : 0, st = ceil_div(own, p.wide ? WIDE_OWN : 16 * p.s_tiles);
-    const long long blocks = std::max(1ll, lh * (pt + (p.stream ? 0 : c.n_streams * st))), want = std::max(1ll, ceil_div(p.wide ? 512 : 1024, blocks));
+    const long long blocks = std::max(1ll, lh * (pt + (p.stream ? 0 : c.n_streams * st))), want = std::max(1ll, ceil_div(512, blocks));
     const auto splits_of = [&](int keys) {
         const long long most = p.wide ? ceil_div(ceil_div(keys, WIDE_ROWS), 2) : ceil_div(ceil_div(keys, KC), 2 * MASS_WAVES);
         return (int)std::max(1ll, std::min({want, most, 32ll}));
@@ -918,7 +977,7 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     p.s_splits = p.stream ? 0 : splits_of(c.cap);
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
-    const int many = c.head_dim == 64 ? 8 : 4, keys = MASS_WAVES * 16 * many;
+    const int many = 4, keys = MASS_WAVES * 16 * many;
     p.key_tiles = lh * (ceil_div(d.len_prefill, keys) + (p.stream ? 0 : c.n_streams * ceil_div(c.cap, keys))) < 512 ? 2 : many;
     return p;
 }
@@ -992,20 +1051,19 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
     hipStream_t s = (hipStream_t)stream;
     const dim3 block(64 * MASS_WAVES), stats_grid((unsigned)stats), add_grid((unsigned)add);
     const auto all = [&](auto dim) {
-        constexpr int D = decltype(dim)::value, MANY = D == 64 ? 8 : 4;
+        constexpr int D = decltype(dim)::value;
         const auto stats = [&](auto prefill_tiles, auto stream_tiles) {
             mass_stats<D, decltype(prefill_tiles)::value, decltype(stream_tiles)::value><<<stats_grid, block, 0, s>>>(a);
         };
         constexpr std::integral_constant<int, 1> one{};
         constexpr std::integral_constant<int, 4> four{};
-        constexpr std::integral_constant<int, MANY> many{};
         const auto narrow_stats = [&] {
-            if (p.s_tiles == 1) p.p_tiles == 1 ? stats(one, one) : p.p_tiles == 4 ? stats(four, one) : stats(many, one);
-            else                p.p_tiles <= 4 ? stats(four, four) : stats(many, four);
+            if (p.s_tiles == 1) p.p_tiles == 1 ? stats(one, one) : stats(four, one);
+            else                stats(four, four);
         };
         if (p.wide) {
             mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
-            mass_merge<<<dim3((unsigned)((lh * a.vecs + 255) / 256)), block, 0, s>>>(a);
+            mass_merge<<<dim3((unsigned)((lh * a.vecs + 31) / 32)), block, 0, s>>>(a);
             mass_add_wide<D><<<add_grid, block, 0, s>>>(a);
         } else if (p.stream) {
             if (a.P > 0) narrow_stats();
@@ -1020,12 +1078,12 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
             }
             if (a.P > 0) {
                 if (p.key_tiles == 2) mass_add<D, 2, true><<<add_grid, block, 0, s>>>(a);
-                else                  mass_add<D, MANY, true><<<add_grid, block, 0, s>>>(a);
+                else                  mass_add<D, 4, true><<<add_grid, block, 0, s>>>(a);
             }
         } else {
             narrow_stats();
             if (p.key_tiles == 2) mass_add<D, 2, false><<<add_grid, block, 0, s>>>(a);
-            else                  mass_add<D, MANY, false><<<add_grid, block, 0, s>>>(a);
+            else                  mass_add<D, 4, false><<<add_grid, block, 0, s>>>(a);
         }
     };
     if (c.head_dim == 64) all(std::integral_constant<int, 64>{});

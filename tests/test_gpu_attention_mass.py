@@ -136,3 +136,74 @@ def test_a_long_segment(gpu):
     """Several blocks share a query tile's keys; the last chunk is short."""
     check(gpu, make(10, 1, 1, 1, 4, 64, 9001, 4099, 2, [8999], ordered=True), [[0, 1]], 0.98)
     check(gpu, make(11, 1, 1, 1, 2, 128, 5003, 0, 48, [5003], ordered=True), None)
+
+
+@pytest.mark.parametrize("dim,cap,G,rows", [
+    (64, 40, 4, [0, 3, 5]), (128, 33, 2, [0, 3, 5]), (64, 513, 2, [1, 4, 5]), (128, 600, 1, [0, 5]), (64, 1200, 1, [2, 3]), (128, 1153, 2, [0]),
+    (64, 40, 8, [0, 2, 3, 5]), (128, 40, 8, [0, 2, 3]), (64, 530, 6, [0, 1, 2, 3]),
+])
+def test_streams_in_one_pass_beside_a_prefill_segment(gpu, dim, cap, G, rows):
+    """From 256 heads of streams on: their segments are held by a block each (up to 2048 slots, and 1152 with more than 16 query
+    vectors), every number of slots per wave and both numbers of vector tiles; lists of all lengths, an empty stream."""
+    L, S, H = (8, 8, 4) if cap < 100 else (16, 8, 2)
+    n, rng = len(rows), np.random.default_rng(cap)
+    lists = [(rows[:k] + [-1] * n)[:n] for k in [n, 1, n, 0, n, max(1, n - 1), n, 1]]
+    length = rng.integers(max(1, cap // 2), cap + 1, S)
+    length[:3] = [cap, min(cap, 5), 0]
+    c = make(cap + dim, L, S, H, G, dim, cap, 70, 6, length)
+    c["k"][:, 1, :, 5:] = 0x7FC0                                 # what stands behind the length
+    c["q"][:, [6 * s + r for s in range(S) for r in range(6) if r not in lists[s]]] = 0xFFC0
+    got, got_p = run(gpu, c, lists, 0.9)
+    wide = lambda a: bf16_bits_to_f32(a).astype(np.float64)   # noqa: E731
+    # every fourth layer against the definition (it takes its time)
+    for l in range(0, L, 4):
+        part = {k: v[l:l + 1] if k in ("k", "mass", "slot_pos", "q", "k_prefill", "mass_prefill") else v for k, v in c.items()}
+        with np.errstate(invalid="ignore"):
+            want, shared = D.attention_mass(wide(part["k"]), part["mass"], part["slot_pos"], c["len"], c["next_pos"], wide(part["q"]), 6, lists,
+                                            float(np.float32(c["scale"])), float(np.float32(0.9)), wide(part["k_prefill"]), part["mass_prefill"])
+        finite_q = np.where(np.isfinite(wide(part["q"])), wide(part["q"]), 0)
+        finite_k = np.where(np.isfinite(wide(part["k"])), wide(part["k"]), 0)
+        norm = lambda a: np.sqrt((a ** 2).sum(-1)).max()   # noqa: E731
+        d = (dim + 2) * 2.0 ** -23 * c["scale"] * norm(finite_q) * max(norm(finite_k), norm(wide(part["k_prefill"])))
+        rel = 2 * d + ((cap + 70) ** 0.5 + 16) * 2.0 ** -23
+        for g, w, old in ((got[l:l + 1], want, part["mass"]), (got_p[l:l + 1], shared, part["mass_prefill"])):
+            bound = np.abs(w - 0.9 * old) * rel + (np.abs(old) + np.abs(w)) * 2 * 2.0 ** -24 + 1e-37
+            assert np.all(np.abs(g - w) <= bound), (l, float(np.abs(g - w).max()))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_streams_in_one_pass_without_a_prefill_segment(gpu, dim):
+    check(gpu, make(12, 2, 3, 2, 4, dim, 300, 0, 5, [300, 17, 0]), [[0, 2, 4], [1, -1, 0], [0, 1, 2]], 0.9)
+    check(gpu, make(13, 1, 2, 2, 8, dim, 1000, 0, 5, [999, 64]), [[0, 2, 4], [1, -1, 0]], 0.9)
+    check(gpu, make(14, 1, 1, 1, 2, dim, 2048, 0, 5, [2048]), [[0, 2, 4]])
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 0.3])
+def test_any_sign_of_the_scale(gpu, scale):
+    for R, rows in ((5, [[0, 2, 4], [1, 3, -1]]), (80, None)):
+        c = make(15, 1, 2, 1, 4, 64, 150, 33, R, [150, 90])
+        c["scale"] = scale
+        check(gpu, c, rows)
+
+
+def test_many_listed_rows_of_several_streams(gpu):
+    """The wide products with lists: rows that do not count, with NaN where they stand, and a shared segment."""
+    rng = np.random.default_rng(16)
+    R = 70
+    lists = [sorted(rng.permutation(R)[:64].tolist()), sorted(rng.permutation(R)[:40].tolist()) + [-1] * 24, [-1] * 64]
+    for dim in (64, 128):
+        c = make(17 + dim, 1, 3, 2, 4, dim, 300, 130, R, [300, 150, 20])
+        listed = [s * R + r for s in range(3) for r in lists[s] if r >= 0]
+        c["q"][:, [m for m in range(3 * R) if m not in listed]] = 0x7FC0
+        check(gpu, c, lists, 0.9)
+
+
+def test_scores_that_grow_along_the_keys(gpu):
+    """The running maximum has to follow: every chunk's scores lie far above those before it, and the other way round."""
+    for R, rows in ((3, [[0, 1, 2]]), (70, None)):
+        for order in (1, -1):
+            c = make(18, 1, 1, 1, 4, 64, 900, 0, R, [900], ordered=True)
+            ramp = np.linspace(-40.0, 40.0, 900)[::order]
+            c["k"] = bf16(np.broadcast_to(ramp[:, None] / 8.0, (900, 64))[None, None, None])
+            c["q"] = bf16(np.ones((1, R, 4, 64)) * 8.0)
+            check(gpu, c, rows)

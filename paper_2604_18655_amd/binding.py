@@ -568,6 +568,13 @@ def _buffer(t, where: str, itemsize: int, shape=None, n: Optional[int] = None) -
         raise MloraError(_ESHAPE, where)
 
 
+def _call_buffer(t, where: str, itemsize: int, n: int) -> None:
+    """_buffer for what changes from call to call: one look at the bytes, and the reason only if they are wrong."""
+    if t.nbytes != itemsize * n or not t.is_contiguous() or not t.is_cuda:
+        _buffer(t, where, itemsize, n=n)
+        raise MloraError(_EINVAL, where)
+
+
 class Rope:
     """Rotary positions (mlora_rope): `rot` of head_dim features turn, in pairs of the half or the interleaved layout, by
     frequencies that are plain, divided by factor (linear), of a larger base (base) or stretched where they turn fewer than
@@ -667,34 +674,37 @@ class StreamCache:
         self.struct = _StreamCacheStruct(L, S, H, D, cap, _ptr(k), _ptr(v), _ptr(mass), _ptr(slot_pos), _ptr(len),
                                          _ptr(next_pos), _ptr(self.tickets))
         self.ref = C.byref(self.struct)
+        self.streams, self.heads, self.row_elements = S, L * S * H, L * S * H * D
+        self.append_fn = load_library().mlora_stream_cache_append
+        self.compress_fn = load_library().mlora_stream_cache_compress
 
     def append(self, k_new, v_new, rows_per_stream: int, rows, budget: int, sink: int = 0, recent: int = 0,
                stream: Optional[int] = None) -> None:
         """Listed rows (int32 [S][n], None: all) of k_new and v_new bf16 [L][S * rows_per_stream][H][head_dim] enter the
         caches; beyond the budget they take the slots of the lowest rank."""
-        L, S, H, _, D = self.shape
-        n = L * S * rows_per_stream * H * D
-        _buffer(k_new, "mlora_stream_cache_append", 2, n=n)
-        _buffer(v_new, "mlora_stream_cache_append", 2, n=n)
+        where = "mlora_stream_cache_append"
+        n = self.row_elements * rows_per_stream
+        _call_buffer(k_new, where, 2, n)
+        _call_buffer(v_new, where, 2, n)
         listed = 0
         if rows is not None:
-            listed = rows.numel() // S
-            _buffer(rows, "mlora_stream_cache_append", 4, n=S * listed)
-        st = load_library().mlora_stream_cache_append(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
-                                                      _ptr(rows), listed, budget, sink, recent,
-                                                      _stream() if stream is None else stream)
+            listed = rows.numel() // self.streams
+            _call_buffer(rows, where, 4, self.streams * listed)
+        st = self.append_fn(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
+                            None if rows is None else rows.data_ptr(), listed, budget, sink, recent,
+                            _stream() if stream is None else stream)
         if st != 0:
-            raise MloraError(st, "mlora_stream_cache_append")
+            raise MloraError(st, where)
 
     def compress(self, to: "StreamCache", kept, budget: int, sink: int = 0, recent: int = 0,
                  stream: Optional[int] = None) -> None:
         """The slots of the highest rank, at most budget, to the front of another cache; kept int32 [L][S][H][budget]
         tells which (-1 beyond)."""
-        L, S, H = self.shape[:3]
-        _buffer(kept, "mlora_stream_cache_compress", 4, n=L * S * H * budget)
-        _check(load_library().mlora_stream_cache_compress(self.ref, to.ref, _ptr(kept), budget, sink, recent,
-                                                          _stream() if stream is None else stream),
-               "mlora_stream_cache_compress")
+        _call_buffer(kept, "mlora_stream_cache_compress", 4, self.heads * budget)
+        st = self.compress_fn(self.ref, to.ref, kept.data_ptr(), budget, sink, recent,
+                              _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, "mlora_stream_cache_compress")
 
 
 class AttentionMass:
@@ -716,6 +726,7 @@ class AttentionMass:
         self.struct = _AttentionMassStruct(cache.struct, int(n_q_heads), int(rows_per_stream), float(scale),
                                            _ptr(k_prefill), _ptr(mass_prefill), P, float(decay))
         self.ref = C.byref(self.struct)
+        self.fn = load_library().mlora_attention_mass_add
 
     def workspace_bytes(self, n_rows: int = 0) -> int:
         """For calls with n_rows listed rows per stream, 0: with all rows."""
@@ -723,16 +734,17 @@ class AttentionMass:
 
     def run(self, q, rows, workspace, stream: Optional[int] = None) -> None:
         """q bf16 [L][S * rows_per_stream][n_q_heads][head_dim], rows int32 [S][n] or None (all)."""
-        _buffer(q, "mlora_attention_mass_add", 2, n=self.q_elements)
+        where = "mlora_attention_mass_add"
+        _call_buffer(q, where, 2, self.q_elements)
         listed = 0
         if rows is not None:
             listed = rows.numel() // self.streams
-            _buffer(rows, "mlora_attention_mass_add", 4, n=self.streams * listed)
-        n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-        st = load_library().mlora_attention_mass_add(self.ref, q.data_ptr(), _ptr(rows), listed, _ptr(workspace), n,
-                                                     _stream() if stream is None else stream)
+            _call_buffer(rows, where, 4, self.streams * listed)
+        st = self.fn(self.ref, q.data_ptr(), None if rows is None else rows.data_ptr(), listed,
+                     None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+                     _stream() if stream is None else stream)
         if st != 0:
-            raise MloraError(st, "mlora_attention_mass_add")
+            raise MloraError(st, where)
 
 
 class LogitRules:
@@ -765,19 +777,19 @@ class LogitRules:
                                         0 if bias is None else int(bias.shape[0]), _ptr(masks), _ptr(mask_row),
                                         0 if masks is None else int(masks.shape[0]))
         self.ref = C.byref(self.struct)
+        self.fn = load_library().mlora_logit_rules_apply
 
     def run(self, logits, tokens, out, new_tokens=None, stream: Optional[int] = None) -> None:
         """logits [S * R][V] -> out (may be logits itself); tokens int32 [S][T]; new_tokens int32 [S][n]: counted first."""
         where = "mlora_logit_rules_apply"
-        _buffer(logits, where, self.itemsize, n=self.logits)
-        _buffer(out, where, self.itemsize, n=self.logits)
-        _buffer(tokens, where, 4, n=self.tokens)
+        _call_buffer(logits, where, self.itemsize, self.logits)
+        _call_buffer(out, where, self.itemsize, self.logits)
+        _call_buffer(tokens, where, 4, self.tokens)
         fresh = 0
         if new_tokens is not None:
             fresh = new_tokens.numel() // self.streams
-            _buffer(new_tokens, where, 4, n=self.streams * fresh)
-        st = load_library().mlora_logit_rules_apply(self.ref, logits.data_ptr(), tokens.data_ptr(),
-                                                    _ptr(new_tokens) if fresh else None, fresh, out.data_ptr(),
-                                                    _stream() if stream is None else stream)
+            _call_buffer(new_tokens, where, 4, self.streams * fresh)
+        st = self.fn(self.ref, logits.data_ptr(), tokens.data_ptr(), new_tokens.data_ptr() if fresh else None, fresh,
+                     out.data_ptr(), _stream() if stream is None else stream)
         if st != 0:
             raise MloraError(st, where)

@@ -29,10 +29,10 @@ from . import binding as B
 
 class DecoderLayerStep:
     def __init__(self, proj_q, proj_k, proj_v, proj_o, proj_gate_up, proj_down, attention: B.TreeAttention,
-                 h, rope_cos, rope_sin, row_adapter, M: int, eps: float = 1e-5, h_sq=None):
+                 h, rope_cos, rope_sin, row_adapter, M: int, eps: float = 1e-5, h_sq=None, q=None):
         """proj_*: binding.Proj on the device; attention: descriptor whose k_new / v_new are the
         tensors this step writes k and v to; h bf16 [M][hidden] (int16 tensor); rope tables fp32
-        [M][32]."""
+        [M][32]; q: where the rotated queries go (a tensor of its own if None)."""
         dev = h.device
         hidden, ffn = proj_q.K, proj_gate_up.N // 2
         i16 = lambda n: torch.empty((M, n), dtype=torch.int16, device=dev)
@@ -42,7 +42,7 @@ class DecoderLayerStep:
         self.h_sq = h_sq                                 # [M][parts] from the previous layer, or None
         self.sq2 = torch.empty((M, parts), dtype=torch.float32, device=dev)
         self.out_sq = torch.empty((M, parts), dtype=torch.float32, device=dev)
-        self.q = i16(proj_q.N)
+        self.q = i16(proj_q.N) if q is None else q
         self.k_new, self.v_new = attention.keep[7], attention.keep[8]
         self.attn = i16(proj_q.N)
         self.h2, self.act, self.out = i16(hidden), i16(ffn), i16(hidden)

@@ -674,7 +674,7 @@ class StreamCache:
         self.struct = _StreamCacheStruct(L, S, H, D, cap, _ptr(k), _ptr(v), _ptr(mass), _ptr(slot_pos), _ptr(len),
                                          _ptr(next_pos), _ptr(self.tickets))
         self.ref = C.byref(self.struct)
-        self.streams, self.heads, self.row_elements = S, L * S * H, L * S * H * D
+        self.streams, self.heads, self.row_bytes = S, L * S * H, 2 * L * S * H * D
         self.append_fn = load_library().mlora_stream_cache_append
         self.compress_fn = load_library().mlora_stream_cache_compress
 
@@ -683,9 +683,11 @@ class StreamCache:
         """Listed rows (int32 [S][n], None: all) of k_new and v_new bf16 [L][S * rows_per_stream][H][head_dim] enter the
         caches; beyond the budget they take the slots of the lowest rank."""
         where = "mlora_stream_cache_append"
-        n = self.row_elements * rows_per_stream
-        _call_buffer(k_new, where, 2, n)
-        _call_buffer(v_new, where, 2, n)
+        size = self.row_bytes * rows_per_stream
+        if (k_new.nbytes != size or v_new.nbytes != size or not k_new.is_contiguous() or not v_new.is_contiguous()
+                or not k_new.is_cuda or not v_new.is_cuda):
+            for t in (k_new, v_new):
+                _call_buffer(t, where, 2, size // 2)
         listed = 0
         if rows is not None:
             listed = rows.numel() // self.streams
@@ -782,9 +784,13 @@ class LogitRules:
     def run(self, logits, tokens, out, new_tokens=None, stream: Optional[int] = None) -> None:
         """logits [S * R][V] -> out (may be logits itself); tokens int32 [S][T]; new_tokens int32 [S][n]: counted first."""
         where = "mlora_logit_rules_apply"
-        _call_buffer(logits, where, self.itemsize, self.logits)
-        _call_buffer(out, where, self.itemsize, self.logits)
-        _call_buffer(tokens, where, 4, self.tokens)
+        size = self.itemsize * self.logits
+        if (logits.nbytes != size or out.nbytes != size or tokens.nbytes != 4 * self.tokens or not logits.is_contiguous()
+                or not out.is_contiguous() or not tokens.is_contiguous() or not logits.is_cuda or not out.is_cuda
+                or not tokens.is_cuda):
+            _call_buffer(logits, where, self.itemsize, self.logits)
+            _call_buffer(out, where, self.itemsize, self.logits)
+            _call_buffer(tokens, where, 4, self.tokens)
         fresh = 0
         if new_tokens is not None:
             fresh = new_tokens.numel() // self.streams

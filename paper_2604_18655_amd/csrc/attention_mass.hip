@@ -412,11 +412,10 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     }
 }
 
-// Few query vectors (VT tiles of 16) on a stream's own segment that a block holds at once: its scores stay in registers, and one pass over the keys is
-// all there is.  The prefill segment's maxima and sums are there already (mass_stats); what its masses need is left behind.
-constexpr int STREAM_WAVES = 8;
-constexpr int stream_keys(int TK) { return STREAM_WAVES * 16 * TK; }
-
+// Few query vectors (VT tiles of 16) on keys that a block holds at once: its scores stay in registers, and one pass over the keys is
+// all there is.  The keys are a stream's own segment; where several streams share a prefill segment, its maxima and sums are
+// there already (mass_stats) and what its masses need is left behind; where the stream is the only one (ALONE) they are the
+// block's as well, in front of the others.
 // a value combined over the 16 lanes of a quarter of the wave; every lane gets the result
 template <class Op>
 __device__ __forceinline__ float over_sixteen(float v, const Op &op)
@@ -430,16 +429,30 @@ __device__ __forceinline__ float over_sixteen(float v, const Op &op)
     return op(v, ror(v, std::integral_constant<int, 1>{}));
 }
 
-template <int D, int VT, int TK>
-__global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs a)
+template <int D, int VT, int TK, int W, bool ALONE>
+__global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 {
     constexpr int DK = D / 32, AHEAD = D == 64 ? (TK < 4 ? TK : 4) : 2, V = 16 * VT;
-    __shared__ __align__(16) float tops[STREAM_WAVES][V], sums[STREAM_WAVES][V], p_top[V], p_sum[V];
+    __shared__ __align__(16) float tops[W][V], sums[W][V], p_top[V], p_sum[V];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const Unit w(a, 0, 1, D);
-    // tiles of 16 keys: wave, wave + 8, ..; past the end: the last key
-    const auto key_of = [&](int t) { return (t * STREAM_WAVES + wave) * 16 + l16; };
-    const int last = max(w.keys - 1, 0);
+    // tiles of 16 keys: wave, wave + W, ..; first those of the prefill segment.  Past a segment's end: its last key.
+    const int p_tiles = ALONE ? (a.P + 15) / 16 : 0;
+    struct Key {
+        bool prefill, live;
+        int at;                                                      // in its segment
+    };
+    const auto key_of = [&](int t) {
+        const int tile = t * W + wave;
+        Key k;
+        k.prefill = ALONE && tile < p_tiles;
+        const int key = (k.prefill ? tile : tile - p_tiles) * 16 + l16, keys = k.prefill ? a.P : w.keys;
+        k.live = key < keys;
+        k.at = min(key, max(keys - 1, 0));
+        return k;
+    };
+    const uint16_t *const pk = ALONE ? a.k_prefill + (size_t)w.lh * a.P * D : nullptr;
+    float *const mass = a.mass + w.at, *const p_mass = ALONE ? a.mass_prefill + (size_t)w.lh * a.P : nullptr;
     // (vectors and what the prefill segment left come before the keys: loads return in their order)
     uint4 qf[VT][DK];
 #pragma unroll
@@ -452,25 +465,32 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     if (tid < V) {
         // this vector on the prefill segment
         float top = NEG_BIG, all = 0.f;
-        if (tid < w.vecs && a.P > 0) merge_parts(a.part + (size_t)w.lh * a.p_splits * a.vecs + own + tid, a.p_splits, a.vecs, top, all);
+        if (!ALONE && tid < w.vecs && a.P > 0) merge_parts(a.part + (size_t)w.lh * a.p_splits * a.vecs + own + tid, a.p_splits, a.vecs, top, all);
         p_top[tid] = top;
         p_sum[tid] = all;
     }
     uint4 kf[AHEAD][DK];
-    int at[TK];
+    int at[TK];                                                      // positions; a prefill segment's lie before all
     const auto ask = [&](int t) {
-        const int key = min(key_of(t), last);
+        const Key k = key_of(t);
+        const uint16_t *const kp = (k.prefill ? pk : w.k) + (size_t)k.at * D + 8 * lq;
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[t % AHEAD][kk] = *reinterpret_cast<const uint4 *>(w.k + (size_t)key * D + 8 * lq + 32 * kk);
+        for (int kk = 0; kk < DK; ++kk) kf[t % AHEAD][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
     };
 #pragma unroll
-    for (int t = 0; t < TK; ++t) at[t] = w.pos[min(key_of(t), last)];
+    for (int t = 0; t < TK; ++t) {
+        const Key k = key_of(t);
+        at[t] = (int)0x80000000;
+        if (!k.prefill) at[t] = w.pos[k.at];
+    }
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) ask(t);
-    float *const mass = a.mass + w.at;
     float old[TK];
 #pragma unroll
-    for (int t = 0; t < TK; ++t) old[t] = mass[min(key_of(t), last)];
+    for (int t = 0; t < TK; ++t) {
+        const Key k = key_of(t);
+        old[t] = (k.prefill ? p_mass : mass)[k.at];
+    }
     int pos[VT][4];
     float top[VT][4], sum[VT][4];
 #pragma unroll
@@ -485,7 +505,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     f32x4 sc[VT][TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t) {
-        const bool live = key_of(t) < w.keys;
+        const bool live = key_of(t).live;
 #pragma unroll
         for (int v = 0; v < VT; ++v) {
             sc[v][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -511,7 +531,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     for (int v = 0; v < VT; ++v) {
         f32x4 m = *reinterpret_cast<const f32x4 *>(&tops[0][16 * v + 4 * lq]);
 #pragma unroll
-        for (int i = 1; i < STREAM_WAVES; ++i) {
+        for (int i = 1; i < W; ++i) {
             const f32x4 o = *reinterpret_cast<const f32x4 *>(&tops[i][16 * v + 4 * lq]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], o[e]);
@@ -534,7 +554,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
     for (int v = 0; v < VT; ++v) {
         f32x4 all = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < STREAM_WAVES; ++i) all += *reinterpret_cast<const f32x4 *>(&sums[i][16 * v + 4 * lq]);
+        for (int i = 0; i < W; ++i) all += *reinterpret_cast<const f32x4 *>(&sums[i][16 * v + 4 * lq]);
         const f32x4 pt = *reinterpret_cast<const f32x4 *>(&p_top[16 * v + 4 * lq]), ps = *reinterpret_cast<const f32x4 *>(&p_sum[16 * v + 4 * lq]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -543,7 +563,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
             const float total = all[e] * here + ps[e] * __builtin_amdgcn_exp2f(pt[e] - m), inv = total > 0.f ? 1.f / total : total;      // (NaN stays)
             const bool counts = vec < w.vecs;
             factor[v][e] = counts ? here * inv : 0.f;
-            if (a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
+            if (!ALONE && a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
                 a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(m, counts ? inv : 0.f);
                 if (w.lh == 0) {
                     const int j = vec / a.G;
@@ -560,7 +580,8 @@ __global__ __launch_bounds__(64 * STREAM_WAVES) void mass_stream(const MassArgs 
 #pragma unroll
             for (int e = 0; e < 4; ++e) add += factor[v][e] != 0.f ? sc[v][t][e] * factor[v][e] : 0.f;
         add = over_quarters(add, [](float x, float y) { return x + y; });
-        if (lq == 0 && key_of(t) < w.keys) mass[key_of(t)] = a.decay * old[t] + add;
+        const Key k = key_of(t);
+        if (lq == 0 && k.live) (k.prefill ? p_mass : mass)[k.at] = a.decay * old[t] + add;
     }
 }
 
@@ -947,7 +968,8 @@ mlora_status check(const mlora_attention_mass *d)
 struct Plan {
     bool wide;
     int stream;                          // 0, or the key tiles of a wave in mass_stream
-    int stream_vecs;                     // its vector tiles
+    int stream_vecs, stream_waves;       // its vector tiles and waves
+    bool alone;                          // the prefill segment is the one stream's
     int p_tiles, s_tiles;                // query tiles of a block: prefill, stream segment
     int p_splits, s_splits, p_blocks, s_blocks;
     int key_tiles;                       // key tiles of a wave in mass_add
@@ -958,22 +980,37 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     const int G = d.n_q_heads / c.n_kv_heads;
     const long long lh = (long long)c.n_layers * c.n_kv_heads, own = (long long)N * G, all = own * c.n_streams;
     Plan p;
+    const auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
     // (a layer's query vectors are reached by 32-bit offsets)
     p.wide = d.scale > 0.f && own >= WIDE_OWN && d.n_q_heads <= 1024;
+    // One pass where a block holds the keys: up to 16 tiles in each of eight waves (9 with 17 to 32 vectors, whose scores take twice the
+    // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner.  A
+    // compute unit by itself draws little from memory, so it takes many blocks: 128 where it is the only launch (16 layers x 8
+    // heads, 2248 keys 16.7 us, in two passes 26; 32 blocks of 2000 keys 15.0 and 12.6) or the keys are few, 256 where
+    // it is the second of three, for streams that share a prefill segment (256 blocks 25.4 and 26.3 us, 128 blocks 24 and 20.4).
+    p.alone = d.len_prefill > 0 && c.n_streams == 1;
     p.stream_vecs = own <= 16 ? 1 : 2;
-    p.stream = p.wide || own > 32 || c.cap > stream_keys(own <= 16 ? 16 : 9) ? 0 : c.cap <= stream_keys(4) ? 4 : c.cap <= stream_keys(9) ? 9 : 16;
-    if (d.len_prefill > 0 && lh * c.n_streams < 256) p.stream = 0;
+    const long long key_tiles = ceil_div(c.cap, 16) + (p.alone ? ceil_div(d.len_prefill, 16) : 0), stream_blocks = lh * c.n_streams;
+    p.stream = 0;
+    p.stream_waves = 8;
+    const bool only = d.len_prefill == 0 || p.alone;
+    if (!p.wide && own <= 32 && (stream_blocks >= (only ? 128 : 256) || (only && key_tiles <= 8))) {
+        const int most = own <= 16 ? 16 : 9, most16 = own <= 16 ? 9 : 4;
+        if (key_tiles > 32 && key_tiles <= 16 * most16 && (stream_blocks <= 256 || key_tiles > 8 * most)) p.stream_waves = 16;
+        const int per_wave = (int)std::min(1000ll, ceil_div(key_tiles, p.stream_waves));
+        if (per_wave <= (p.stream_waves == 16 ? most16 : most)) p.stream = per_wave <= 4 ? 4 : per_wave <= 9 ? 9 : 16;
+    }
+    if (!p.stream) p.alone = false;
     const auto tiles_of = [&](long long vecs) { return vecs <= 16 ? 1 : 4; };
     p.s_tiles = own <= 16 ? 1 : 4;
     p.p_tiles = tiles_of(all);
-    const auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
-    const long long pt = d.len_prefill > 0 ? ceil_div(all, p.wide ? WIDE_OWN : 16 * p.p_tiles) : 0, st = ceil_div(own, p.wide ? WIDE_OWN : 16 * p.s_tiles);
+    const long long pt = d.len_prefill > 0 && !p.alone ? ceil_div(all, p.wide ? WIDE_OWN : 16 * p.p_tiles) : 0, st = ceil_div(own, p.wide ? WIDE_OWN : 16 * p.s_tiles);
     const long long blocks = std::max(1ll, lh * (pt + (p.stream ? 0 : c.n_streams * st))), want = std::max(1ll, ceil_div(512, blocks));
     const auto splits_of = [&](int keys) {
         const long long most = p.wide ? ceil_div(ceil_div(keys, WIDE_ROWS), 2) : ceil_div(ceil_div(keys, KC), 2 * MASS_WAVES);
         return (int)std::max(1ll, std::min({want, most, 32ll}));
     };
-    p.p_splits = d.len_prefill > 0 ? splits_of(d.len_prefill) : 0;
+    p.p_splits = d.len_prefill > 0 && !p.alone ? splits_of(d.len_prefill) : 0;
     p.s_splits = p.stream ? 0 : splits_of(c.cap);
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
@@ -1066,17 +1103,28 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
             mass_merge<<<dim3((unsigned)((lh * a.vecs + 31) / 32)), block, 0, s>>>(a);
             mass_add_wide<D><<<add_grid, block, 0, s>>>(a);
         } else if (p.stream) {
-            if (a.P > 0) narrow_stats();
-            const dim3 grid((unsigned)(lh * a.S)), wide_block(64 * STREAM_WAVES);
+            if (a.P > 0 && !p.alone) narrow_stats();
+            const auto stream_tiles = [&](auto vt, auto tk, auto waves) {
+                constexpr int VT = decltype(vt)::value, TK = decltype(tk)::value, W = decltype(waves)::value;
+                const dim3 grid((unsigned)(lh * a.S)), threads(64 * W);
+                if (p.alone) mass_stream<D, VT, TK, W, true><<<grid, threads, 0, s>>>(a);
+                else         mass_stream<D, VT, TK, W, false><<<grid, threads, 0, s>>>(a);
+            };
+            constexpr std::integral_constant<int, 2> two{};
+            constexpr std::integral_constant<int, 8> eight{};
+            constexpr std::integral_constant<int, 9> nine{};
+            constexpr std::integral_constant<int, 16> sixteen{};
             if (p.stream_vecs == 1) {
-                if (p.stream == 4)      mass_stream<D, 1, 4><<<grid, wide_block, 0, s>>>(a);
-                else if (p.stream == 9) mass_stream<D, 1, 9><<<grid, wide_block, 0, s>>>(a);
-                else                    mass_stream<D, 1, 16><<<grid, wide_block, 0, s>>>(a);
+                if (p.stream_waves == 16) p.stream == 4 ? stream_tiles(one, four, sixteen) : stream_tiles(one, nine, sixteen);
+                else if (p.stream == 4)   stream_tiles(one, four, eight);
+                else if (p.stream == 9)   stream_tiles(one, nine, eight);
+                else                      stream_tiles(one, sixteen, eight);
             } else {
-                if (p.stream == 4) mass_stream<D, 2, 4><<<grid, wide_block, 0, s>>>(a);
-                else               mass_stream<D, 2, 9><<<grid, wide_block, 0, s>>>(a);
+                if (p.stream_waves == 16) stream_tiles(two, four, sixteen);
+                else if (p.stream == 4)   stream_tiles(two, four, eight);
+                else                      stream_tiles(two, nine, eight);
             }
-            if (a.P > 0) {
+            if (a.P > 0 && !p.alone) {
                 if (p.key_tiles == 2) mass_add<D, 2, true><<<add_grid, block, 0, s>>>(a);
                 else                  mass_add<D, 4, true><<<add_grid, block, 0, s>>>(a);
             }

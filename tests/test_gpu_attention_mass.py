@@ -143,7 +143,7 @@ def test_a_long_segment(gpu):
     (64, 40, 8, [0, 2, 3, 5]), (128, 40, 8, [0, 2, 3]), (64, 530, 6, [0, 1, 2, 3]),
 ])
 def test_streams_in_one_pass_beside_a_prefill_segment(gpu, dim, cap, G, rows):
-    """From 256 heads of streams on: their segments are held by a block each (up to 2048 slots, and 1152 with more than 16 query
+    """From 256 heads of streams on (128 without the shared segment): their segments are held by a block each (up to 2048 slots, and 1152 with more than 16 query
     vectors), every number of slots per wave and both numbers of vector tiles; lists of all lengths, an empty stream."""
     L, S, H = (8, 8, 4) if cap < 100 else (16, 8, 2)
     n, rng = len(rows), np.random.default_rng(cap)
@@ -207,3 +207,42 @@ def test_scores_that_grow_along_the_keys(gpu):
             c["k"] = bf16(np.broadcast_to(ramp[:, None] / 8.0, (900, 64))[None, None, None])
             c["q"] = bf16(np.ones((1, R, 4, 64)) * 8.0)
             check(gpu, c, rows)
+
+
+@pytest.mark.parametrize("dim,cap,P,G,rows", [
+    (64, 30, 17, 4, [0, 2, 3]), (64, 200, 500, 4, [1]), (128, 100, 300, 2, [0, 1, 2, 3]), (64, 300, 2000, 2, [0, 3]), (128, 1000, 1100, 4, [2]),
+    (64, 100, 3900, 1, [0, 2, 3]), (64, 60, 40, 8, [0, 1, 2, 3]), (128, 300, 260, 8, [0, 1, 2]), (64, 900, 1000, 5, [0, 1, 2, 3]),
+])
+def test_one_stream_with_a_prompt_of_its_own_in_one_pass(gpu, dim, cap, P, G, rows):
+    """128 heads of one stream: a block holds the prefill segment and the stream's own, in eight and in sixteen waves."""
+    L, H = 32, 4
+    c = make(cap + P, L, 1, H, G, dim, cap, P, 5, [max(1, cap - 9)])
+    c["k"][:, 0, :, max(1, cap - 9):] = 0x7FC0
+    got, got_p = run(gpu, c, [rows + [-1]], 0.9)
+    wide = lambda a: bf16_bits_to_f32(a).astype(np.float64)   # noqa: E731
+    for l in range(0, L, 13):
+        part = {k: v[l:l + 1] if k in ("k", "mass", "slot_pos", "q", "k_prefill", "mass_prefill") else v for k, v in c.items()}
+        with np.errstate(invalid="ignore"):
+            want, shared = D.attention_mass(wide(part["k"]), part["mass"], part["slot_pos"], c["len"], c["next_pos"], wide(part["q"]), 5, [rows],
+                                            float(np.float32(c["scale"])), float(np.float32(0.9)), wide(part["k_prefill"]), part["mass_prefill"])
+        norm = lambda a: np.sqrt(np.where(np.isfinite(a), a * a, 0).sum(-1)).max()   # noqa: E731
+        d = (dim + 2) * 2.0 ** -23 * c["scale"] * norm(wide(part["q"])) * max(norm(wide(part["k"])), norm(wide(part["k_prefill"])))
+        rel = 2 * d + ((cap + P) ** 0.5 + 16) * 2.0 ** -23
+        for g, w, old in ((got[l:l + 1], want, part["mass"]), (got_p[l:l + 1], shared, part["mass_prefill"])):
+            assert np.all(np.abs(g - w) <= np.abs(w - 0.9 * old) * rel + (np.abs(old) + np.abs(w)) * 2 * 2.0 ** -24 + 1e-37), l
+
+
+@pytest.mark.parametrize("dim,cap,G,n", [(64, 500, 2, 3), (128, 1100, 4, 4), (64, 1700, 1, 2), (64, 700, 8, 3), (128, 1100, 8, 4), (64, 2048, 5, 3)])
+def test_streams_without_a_prompt_in_one_pass(gpu, dim, cap, G, n):
+    L, S, H = 16, 2, 4
+    c = make(cap + n, L, S, H, G, dim, cap, 0, 5, [cap, max(1, cap // 3)])
+    lists = [list(range(n)) + [-1], [2, -1] + [0] * (n - 1)]
+    got, _ = run(gpu, c, lists, 0.9)
+    wide = lambda a: bf16_bits_to_f32(a).astype(np.float64)   # noqa: E731
+    for l in (0, 15):
+        part = {k: v[l:l + 1] if k in ("k", "mass", "slot_pos", "q") else v for k, v in c.items()}
+        want, _ = D.attention_mass(wide(part["k"]), part["mass"], part["slot_pos"], c["len"], c["next_pos"], wide(part["q"]), 5, lists,
+                                   float(np.float32(c["scale"])), float(np.float32(0.9)))
+        norm = lambda a: np.sqrt((a * a).sum(-1)).max()   # noqa: E731
+        rel = 2 * (dim + 2) * 2.0 ** -23 * c["scale"] * norm(wide(part["q"])) * norm(wide(part["k"])) + (cap ** 0.5 + 16) * 2.0 ** -23
+        assert np.all(np.abs(got[l:l + 1] - want) <= np.abs(want - 0.9 * part["mass"]) * rel + (np.abs(part["mass"]) + np.abs(want)) * 2 * 2.0 ** -24 + 1e-37)

@@ -83,6 +83,14 @@ __device__ __forceinline__ float over_quarters(float v, const Op &op)
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// One of two arguments of the kernel, by its value: chosen by its place, the arguments would be copied to memory for it.
+template <class T>
+__device__ __forceinline__ T *either(bool first, T *a, T *b)
+{
+    asm("" : "+s"(a), "+s"(b));
+    return first ? a : b;
+}
+
 // What a block works on: a layer's and head's prefill segment or a stream's own, and a number within it.
 struct Unit {
     int lh, l, h, s, number;
@@ -112,7 +120,7 @@ struct Unit {
         newest -= n;
         vecs = prefill ? a.vecs : n * a.G;
         at = prefill ? (size_t)lh * a.P : (((size_t)l * a.S + s) * a.H + h) * a.cap;
-        k = (prefill ? a.k_prefill : a.k) + at * D;
+        k = either(prefill, a.k_prefill, a.k) + at * D;
         pos = a.slot_pos + at;
     }
     // place of query vector v's features in a.q, and its number over all streams; false: it does not count
@@ -127,18 +135,19 @@ struct Unit {
         q = q_at(a, l, h, st, row, g, D);
         return true;
     }
-    // the same where it may be any vector if v does not count
-    __device__ __forceinline__ size_t some_vector(const MassArgs &a, int v, int D) const
+    // the same in two steps, where it may be any vector if v does not count
+    __device__ __forceinline__ int listed_row(const MassArgs &a, int v) const
     {
-        const int j = v / a.G, g = v - j * a.G;
-        int st = s, row = j;
-        if (prefill) st = j / a.N, row = j - st * a.N;
-        if (a.rows) {
-            row = a.rows[(size_t)st * a.N + row];
-            row = row >= 0 && row < a.R ? row : 0;
-        }
+        const int j = v / a.G;
+        return a.rows ? a.rows[(prefill ? 0 : (size_t)s * a.N) + j] : prefill ? j % a.N : j;      // (of all streams, one behind the other)
+    }
+    __device__ __forceinline__ size_t some_vector(const MassArgs &a, int v, int row, int D) const
+    {
+        const int j = v / a.G, g = v - j * a.G, st = prefill ? j / a.N : s;
+        row = row >= 0 && row < a.R ? row : 0;
         return ((((size_t)l * a.S + st) * a.R + row) * a.H * a.G + h * a.G + g) * D;
     }
+    __device__ __forceinline__ size_t some_vector(const MassArgs &a, int v, int D) const { return some_vector(a, v, listed_row(a, v), D); }
 };
 
 // Maximum and sum of QT tiles of 16 query vectors over a share of the keys.
@@ -167,27 +176,31 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         }
         x.pos = w.prefill ? 0 : w.pos[min(k0 + (lane & 31), last)];
     };
-    // this lane's query vectors (B operands: lane (l16, lq) holds features 8 * lq .. of vector l16 of a tile)
+    // this lane's query vectors (B operands: lane (l16, lq) holds features 8 * lq .. of vector l16 of a tile).  Loads return in
+    // their order: the rows' places first, a chunk of keys on its way beside them, the vectors, and the other chunks behind, because
+    // the vectors are what all products need.
+    constexpr int AHEAD = D == 64 ? 4 : 2;                           // chunks on their way
+    Keys ring[AHEAD];
+    int c = z * MASS_WAVES + wave;
+    int listed_row[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) listed_row[t] = w.listed_row(a, min(v0 + 16 * t + l16, w.vecs - 1));
+    if (c < chunks) ask(ring[0], c);
     uint4 qf[QT][DK];
     float m[QT], sum[QT];
     int pos[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int v = min(v0 + 16 * t + l16, w.vecs - 1);
-        const size_t q = w.some_vector(a, v, D);
+        const size_t q = w.some_vector(a, v, listed_row[t], D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
         pos[t] = w.newest + v / a.G;
         m[t] = NEG_BIG;
         sum[t] = 0.f;
     }
-    // (the keys come after the vectors: loads return in their order, and these are what all products need.  With the keys
-    // first the products started after 9 us of a launch's 20.)
-    constexpr int AHEAD = D == 64 ? 4 : 2;                           // chunks on their way
-    Keys ring[AHEAD];
-    int c = z * MASS_WAVES + wave;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
+    for (int i = 1; i < AHEAD; ++i)
         if (c + i * stride < chunks) ask(ring[i], c + i * stride);
     const auto work = [&](const Keys &x, int c) {
         const int nk = min(KC, w.keys - c * KC);
@@ -347,7 +360,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     uint4 kf[KT][DK];
     int at[KT];
     float acc[KT], old[KT];
-    float *const mass = (w.prefill ? a.mass_prefill : a.mass) + w.at;
+    float *const mass = either(w.prefill, a.mass_prefill, a.mass) + w.at;
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
         const int key = min(k0 + 16 * t + l16, w.keys - 1);
@@ -939,7 +952,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     for (int t = 0; t < 2; ++t) {
         const float add = acc[t] + __shfl_xor(acc[t], 32);
         const int key = k0 + 32 * t + l32;
-        float *const to = (w.prefill ? a.mass_prefill : a.mass) + w.at + key;
+        float *const to = either(w.prefill, a.mass_prefill, a.mass) + w.at + key;
         if (lh2 == 0 && key < w.keys) *to = a.decay * *to + add;
     }
 }

@@ -83,13 +83,18 @@ __device__ __forceinline__ float over_quarters(float v, const Op &op)
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// One of two arguments of the kernel, by its value: chosen by its place, the arguments would be copied to memory for it.
+// One of two arguments of the kernel, by its value: chosen by its place, the arguments would be copied to memory for it.  The
+// compiler no longer sees that they are global memory: what comes from them is read and written by the calls below.
 template <class T>
 __device__ __forceinline__ T *either(bool first, T *a, T *b)
 {
     asm("" : "+s"(a), "+s"(b));
     return first ? a : b;
 }
+template <class T> using Global = __attribute__((address_space(1))) T;
+__device__ __forceinline__ u32x4 global_piece(const uint16_t *p) { return *(const Global<u32x4> *)p; }
+__device__ __forceinline__ float global_value(const float *p) { return *(const Global<float> *)p; }
+__device__ __forceinline__ void global_put(float *p, float v) { *(Global<float> *)p = v; }
 
 // What a block works on: a layer's and head's prefill segment or a stream's own, and a number within it.
 struct Unit {
@@ -172,7 +177,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         for (int j = 0; j < KC / 16; ++j) {
             const uint16_t *const kp = w.k + (size_t)min(k0 + 16 * j + l16, last) * D + 8 * lq;
 #pragma unroll
-            for (int kk = 0; kk < DK; ++kk) x.f[j][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
+            for (int kk = 0; kk < DK; ++kk) x.f[j][kk] = __builtin_bit_cast(uint4, global_piece(kp + 32 * kk));
         }
         x.pos = w.prefill ? 0 : w.pos[min(k0 + (lane & 31), last)];
     };
@@ -364,10 +369,10 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
         const int key = min(k0 + 16 * t + l16, w.keys - 1);
-        old[t] = mass[key];
+        old[t] = global_value(mass + key);
         const uint16_t *const kp = w.k + (size_t)key * D + 8 * lq;
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
+        for (int kk = 0; kk < DK; ++kk) kf[t][kk] = __builtin_bit_cast(uint4, global_piece(kp + 32 * kk));
         at[t] = w.prefill ? 0 : w.pos[key];
         acc[t] = 0.f;
     }
@@ -421,7 +426,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
     for (int t = 0; t < KT; ++t) {
         const float add = over_quarters(acc[t], [](float x, float y) { return x + y; });
         const int key = k0 + 16 * t + l16;
-        if (lq == 0 && key < w.keys) mass[key] = a.decay * old[t] + add;
+        if (lq == 0 && key < w.keys) global_put(mass + key, a.decay * old[t] + add);
     }
 }
 
@@ -488,7 +493,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
         const Key k = key_of(t);
         const uint16_t *const kp = (k.prefill ? pk : w.k) + (size_t)k.at * D + 8 * lq;
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[t % AHEAD][kk] = *reinterpret_cast<const uint4 *>(kp + 32 * kk);
+        for (int kk = 0; kk < DK; ++kk) kf[t % AHEAD][kk] = __builtin_bit_cast(uint4, global_piece(kp + 32 * kk));
     };
 #pragma unroll
     for (int t = 0; t < TK; ++t) {
@@ -502,7 +507,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 #pragma unroll
     for (int t = 0; t < TK; ++t) {
         const Key k = key_of(t);
-        old[t] = (k.prefill ? p_mass : mass)[k.at];
+        old[t] = global_value((k.prefill ? p_mass : mass) + k.at);
     }
     int pos[VT][4];
     float top[VT][4], sum[VT][4];
@@ -594,7 +599,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             for (int e = 0; e < 4; ++e) add += factor[v][e] != 0.f ? sc[v][t][e] * factor[v][e] : 0.f;
         add = over_quarters(add, [](float x, float y) { return x + y; });
         const Key k = key_of(t);
-        if (lq == 0 && k.live) (k.prefill ? p_mass : mass)[k.at] = a.decay * old[t] + add;
+        if (lq == 0 && k.live) global_put((k.prefill ? p_mass : mass) + k.at, a.decay * old[t] + add);
     }
 }
 
@@ -688,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
         const uint16_t *const rows = w.k + (size_t)next_k0 * D;
         const int last = w.keys - 1 - next_k0;
 #pragma unroll
-        for (int i = 0; i < St::PER; ++i) next[i] = *reinterpret_cast<const u32x4 *>(rows + (unsigned)(min(St::row(i), last) * D + St::piece() * 8));
+        for (int i = 0; i < St::PER; ++i) next[i] = global_piece(rows + (unsigned)(min(St::row(i), last) * D + St::piece() * 8));
         if (!w.prefill) next_pos = w.pos[next_k0 + min(lane, last)];
     };
     const auto put = [&](int buffer, int c) {
@@ -826,7 +831,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     for (int t = 0; t < 2; ++t) {
         const int key = min(k0 + 32 * t + l32, w.keys - 1);
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const u32x4 *>(w.k + (size_t)key * D + 16 * kk + 8 * lh2);
+        for (int kk = 0; kk < DK; ++kk) kf[t][kk] = global_piece(w.k + (size_t)key * D + 16 * kk + 8 * lh2);
         pos[t] = w.prefill ? 0 : w.pos[key];
         acc[t] = 0.f;
     }
@@ -953,7 +958,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
         const float add = acc[t] + __shfl_xor(acc[t], 32);
         const int key = k0 + 32 * t + l32;
         float *const to = either(w.prefill, a.mass_prefill, a.mass) + w.at + key;
-        if (lh2 == 0 && key < w.keys) *to = a.decay * *to + add;
+        if (lh2 == 0 && key < w.keys) global_put(to, a.decay * global_value(to) + add);
     }
 }
 

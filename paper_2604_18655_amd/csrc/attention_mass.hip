@@ -607,7 +607,10 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 // Many query vectors (a prompt's chunk): the side that a wave keeps is 64 vectors (or keys) in registers, the other passes by in
 // chunks of 64 rows that the block's waves share through LDS, on the 32x32x16 products.  A row's 16-byte pieces are
 // exchanged by its number, so that both the writes (rows side by side) and the reads (32 rows of one piece) use all banks.
-// Bound by the exponentials, 16 of a score's 24 cycles per 64 lanes: see the launch rule for what it measured.
+// Bound by the vector unit, at the clock that products and exponentials side by side leave it: a score costs a multiply-add, an
+// exponential (as long as three of them) and an addition, a tile of 32 x 32 scores half as long on the matrix unit.  512
+// rows on 16384 slots, 8 heads of 128 features, 4 query heads each: 76 us for the maxima and sums, 100 for the masses (67.6
+// GFLOP of products each: 0.89 and 0.68 PFLOP/s; a large library product 1.29).
 // ---------------------------------------------------------------------------------------------
 constexpr int WIDE_ROWS = 64;            // rows of a chunk
 constexpr int WIDE_OWN = 256;            // vectors or keys of a block
@@ -626,9 +629,9 @@ __device__ __forceinline__ void all_loaded() { __builtin_amdgcn_s_waitcnt(0x0F70
 
 // Scores of 32 rows of a chunk against what the wave keeps: element i of sc[t] is row 8 * (i / 4) + 4 * (lane / 32) + i % 4
 // against column 32 * t + lane % 32.  at[kk]: where the lane's pieces stand in the first half of the first buffer.  slice(i), i = 0 ..
-// 7, is an eighth of the vector work on the last 32 rows' scores; the two are written in turn and kept so, because the
-// matrix unit works beside the vector unit only if it is fed in between, and a chain of one exponential after the other
-// waits for each.
+// 15, is a share of the vector work on the last 32 rows' scores; product and slice are written in turn and kept so, because
+// the matrix unit works beside the vector unit only if it is fed in between (two products in a row, of which the
+// second waits for the first: maxima and sums of 2048 vectors on 16384 keys of 8 heads 80 us, in turn 76), and a chain of one exponential after the other waits for each.
 template <int D, int BUFFER, int HALF, class Slice>
 __device__ __forceinline__ void wide_scores(const u32x4 *chunks, const int (&at)[D / 16], const u32x4 (&own)[2][D / 16], f32x16 (&sc)[2], const Slice &slice)
 {
@@ -643,12 +646,13 @@ __device__ __forceinline__ void wide_scores(const u32x4 *chunks, const int (&at)
     for (int kk = 0; kk < DK; ++kk) {
         const uint4 now = f;
         if (kk + 1 < DK) f = piece(kk + 1);
-        sc[0] = mfma32(now, __builtin_bit_cast(uint4, own[0][kk]), sc[0]);
-        if (DK == 4) slice(2 * kk);
-        __builtin_amdgcn_sched_barrier(0);
-        sc[1] = mfma32(now, __builtin_bit_cast(uint4, own[1][kk]), sc[1]);
-        slice(DK == 4 ? 2 * kk + 1 : kk);
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            sc[t] = mfma32(now, __builtin_bit_cast(uint4, own[t][kk]), sc[t]);
+#pragma unroll
+            for (int i = 0; i < 8 / DK; ++i) slice((2 * kk + t) * (8 / DK) + i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 }
 
@@ -712,24 +716,21 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
             for (int t = 0; t < 2; ++t) sc[t][i] = p <= pos[t] ? sc[t][i] : -__builtin_inff();
         }
     };
-    // Sums relative to a maximum that may lie a little behind: the sum itself tells when it does too far.  A slice: four scores, and
-    // the sum of the slice before.
-    float more[2], e[4];
+    // Sums relative to a maximum that may lie a little behind: the sum itself tells when it does too far.  A slice: two scores, and the
+    // sum of the slice before.
+    float more[2], e[2];
     const auto slice_of = [&](const f32x16 (&sc)[2]) {
         return [&](int i) {
-            const int t = i / 4, first = i % 4 * 4;
-            float old[4];
+            const int t = i / 8, first = i % 8 * 2;
+            const float old = e[0] + e[1];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                old[u] = e[u];
-                e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][first + u], a.scale2, -m[t]));
-            }
-            if (i % 4 == 1) more[t] = (old[0] + old[1]) + (old[2] + old[3]);
-            else if (i > 0) more[(i - 1) / 4] += (old[0] + old[1]) + (old[2] + old[3]);
+            for (int u = 0; u < 2; ++u) e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][first + u], a.scale2, -m[t]));
+            if (i % 8 == 1) more[t] = old;
+            else if (i > 0) more[(i - 1) / 8] += old;
         };
     };
     const auto settle = [&](const f32x16 (&sc)[2]) {
-        more[1] += (e[0] + e[1]) + (e[2] + e[3]);
+        more[1] += e[0] + e[1];
         if (__any(more[0] > FAR || more[1] > FAR)) {                 // rare, but for the first chunk: once more
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -893,16 +894,16 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
             for (int t = 0; t < 2; ++t) sc[t][i] = pos[t] > p ? -__builtin_inff() : sc[t][i];
         }
     };
-    // A slice: four scores, and the weights of the slice before.  Maxima and sums come from LDS two slices ahead.
-    float e[4];
+    // A slice: two scores, and the weights of the slice before.  Maxima and sums come from LDS four slices ahead.
+    float e[2];
     f32x4 top, inv, old_inv = {0.f, 0.f, 0.f, 0.f}, top_next, inv_next;
     const auto slice_of = [&](const f32x16 (&sc)[2], int c, int half) {
         const float *const tops = &top_of[c & 3][32 * half + 4 * lh2], *const invs = &inv_of[c & 3][32 * half + 4 * lh2];
         top_next = *reinterpret_cast<const f32x4 *>(tops);
         inv_next = *reinterpret_cast<const f32x4 *>(invs);
         return [&, tops, invs](int i) {
-            const int g = i / 2, t = i % 2;
-            if (t == 0) {
+            const int g = i / 4, t = i / 2 % 2, first = i % 2 * 2;               // rows 8 * g + 4 * lh2 + first and the next one
+            if (i % 4 == 0) {
                 old_inv = inv;
                 top = top_next;
                 inv = inv_next;
@@ -911,21 +912,19 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
                     inv_next = *reinterpret_cast<const f32x4 *>(invs + 8 * g + 8);
                 }
             }
-            float old[4];
+            const float old[2] = {e[0], e[1]};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                old[u] = e[u];
-                e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][4 * g + u], a.scale2, -top[u]));
-            }
+            for (int u = 0; u < 2; ++u) e[u] = __builtin_amdgcn_exp2f(fmaf(sc[t][4 * g + first + u], a.scale2, -top[first + u]));
             if (i > 0) {
+                const int ot = (i - 1) / 2 % 2, of = (i - 1) % 2 * 2;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) acc[1 - t] = fmaf(old[u], t == 0 ? old_inv[u] : inv[u], acc[1 - t]);
+                for (int u = 0; u < 2; ++u) acc[ot] = fmaf(old[u], i % 4 == 0 ? old_inv[of + u] : inv[of + u], acc[ot]);
             }
         };
     };
     const auto settle = [&] {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) acc[1] = fmaf(e[u], inv[u], acc[1]);
+        for (int u = 0; u < 2; ++u) acc[1] = fmaf(e[u], inv[2 + u], acc[1]);
     };
     f32x16 x[2], y[2];
     if (chunks > 0) {

@@ -125,6 +125,8 @@ def attention_mass(k, mass, slot_pos, length, next_pos, q, R, rows, scale, decay
                     where = [t if kind == "p" else P + t for kind, t in see]
                     for g in range(G):
                         x = scale * (keys @ q[l, s * R + r, h * G + g])
+                        if x.max() == -np.inf:                   # (NaN is not)
+                            continue
                         e = np.exp(x - x.max())
                         got[where] += e / e.sum()
                 out[l, s, h, :live] = decay * out[l, s, h, :live] + got[P:]

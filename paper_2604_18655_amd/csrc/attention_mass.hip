@@ -2,9 +2,10 @@
 //
 //     mass[t] = decay * mass[t] + sum over rows and query heads of exp(s[row][t] - max) / sum,   s = scale q . k
 //
-// A weight needs its row's maximum and sum over all keys first, so there are two launches: mass_stats leaves the maximum and
+// A weight needs its row's maximum and sum over all keys first.  In general there are two launches: mass_stats leaves the maximum and
 // sum of every query vector over each block's share of the keys, mass_add makes the scores again, key by key.  (Kept
-// in between, the scores of a prompt's chunk would be gigabytes.)
+// in between, the scores of a prompt's chunk would be gigabytes.)  Many query vectors take the wide forms of both.  Where the
+// vectors are few and a block holds a stream's keys, mass_stream keeps the scores in registers and reads the keys once.
 //
 // Scores are products on the matrix units (16x16x32 bf16, fp32 accumulation).  A wave keeps one side in registers and its lanes
 // own it (a lane's columns: its query vectors in mass_stats, its keys in mass_add), and the other side passes by, so that
@@ -26,6 +27,7 @@ constexpr int MASS_WAVES = 4;
 constexpr int KC = 32;                   // keys of a chunk in mass_stats
 constexpr int BATCH = 512;               // query vectors whose maxima mass_add holds at a time
 constexpr float NEG_BIG = -1.0e30f;      // "no key seen yet"
+constexpr float NO_ROW = __builtin_inff();   // the maximum of a query vector that does not count: weights of 0
 constexpr float UNSEEN = -3.0e38f;       // score of a key that is not visible: exp2(UNSEEN - NEG_BIG) is 0
 constexpr float FAR = 1.0995e12f;        // 2^40: how far sums may grow above their maximum before they are scaled down
 
@@ -343,17 +345,17 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
                 const float2 row = a.rows_ml[(size_t)w.lh * a.vecs + v];
                 const int at_row = a.q_row[v];
                 const bool ok = at_row >= 0 && base + i < w.vecs;
-                top_of[i] = ok ? row.x : 1e30f;
+                top_of[i] = ok ? row.x : NO_ROW;
                 inv_of[i] = ok ? row.y : 0.f;
                 q_of[i] = a.q + (((size_t)w.l * a.S * a.R * a.H + w.h) * a.G + max(at_row, 0)) * D;
             } else {
                 size_t q;
                 int number;
                 const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
-                const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(1e30f, 0.f);
+                const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NO_ROW, 0.f);
                 top_of[i] = row.x;
                 inv_of[i] = row.y;
-                pos_of[i] = w.newest + v / a.G;
+                pos_of[i] = ok ? w.newest + v / a.G : (int)0x80000000;
                 q_of[i] = a.q + q;
             }
         }
@@ -377,6 +379,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
         acc[t] = 0.f;
     }
 
+    bool counted = false;                                            // any vector counts: without, a NaN key is no reason for a NaN
     for (int base = 0; base < w.vecs; base += BATCH) {
         const int here = min(BATCH, w.vecs - base), pad = (here + 15) / 16 * 16;
         if (base > 0) {
@@ -401,7 +404,8 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) qf[kk] = qn[kk];
             // (vectors that do not count are zeros: what their place holds may be NaN)
-            const bool bad = top_of[t0 + l16] >= 1e30f;
+            const bool bad = top_of[t0 + l16] == NO_ROW;
+            counted |= !__all(bad);
             if (__any(bad)) {
 #pragma unroll
                 for (int kk = 0; kk < DK; ++kk) qf[kk] = bad ? make_uint4(0, 0, 0, 0) : qf[kk];
@@ -414,17 +418,23 @@ __global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
 #pragma unroll
                 for (int kk = 0; kk < DK; ++kk) sc = mfma16(qf[kk], kf[t][kk], sc);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = __builtin_amdgcn_exp2f(fmaf(sc[e], a.scale2, -top[e]));
-                    if (masked) x = at[t] <= pos_of[t0 + 4 * lq + e] ? x : 0.f;
-                    acc[t] = fmaf(x, inv[e], acc[t]);
+                for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], a.scale2, -top[e]));
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float with = fmaf(sc[e], inv[e], acc[t]);
+                        acc[t] = at[t] > pos_of[t0 + 4 * lq + e] ? acc[t] : with;      // (a NaN row spoils what it sees, no more)
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t] = fmaf(sc[e], inv[e], acc[t]);
                 }
             }
         }
     }
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-        const float add = over_quarters(acc[t], [](float x, float y) { return x + y; });
+        const float add = counted ? over_quarters(acc[t], [](float x, float y) { return x + y; }) : 0.f;
         const int key = k0 + 16 * t + l16;
         if (lq == 0 && key < w.keys) global_put(mass + key, a.decay * old[t] + add);
     }
@@ -596,10 +606,30 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 #pragma unroll
         for (int v = 0; v < VT; ++v)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add += factor[v][e] != 0.f ? sc[v][t][e] * factor[v][e] : 0.f;
+            for (int e = 0; e < 4; ++e) add += factor[v][e] > 0.f ? sc[v][t][e] * factor[v][e] : 0.f;      // (not NaN: below)
         add = over_quarters(add, [](float x, float y) { return x + y; });
         const Key k = key_of(t);
         if (lq == 0 && k.live) global_put((k.prefill ? p_mass : mass) + k.at, a.decay * old[t] + add);
+    }
+    // a NaN row spoils the slots that it sees, no more
+    bool spoils = false;
+    int spoiled_to = (int)0x80000000;
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) spoils |= factor[v][e] != factor[v][e];
+    if (!__any(spoils)) return;
+    int first = 4 * lq;                                              // (positions anew: kept from above, they cost a block per compute unit)
+    asm volatile("" : "+v"(first));
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (factor[v][e] != factor[v][e]) spoiled_to = max(spoiled_to, w.newest + (16 * v + first + e) / a.G);
+#pragma unroll 1
+    for (int t = 0; t < TK; ++t) {                                   // (after the stores above: this wave's, to the same places)
+        const Key k = key_of(t);
+        if (spoils && k.live && (k.prefill || w.pos[k.at] <= spoiled_to)) global_put((k.prefill ? p_mass : mass) + k.at, __builtin_nanf(""));
     }
 }
 
@@ -609,8 +639,9 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 // exchanged by its number, so that both the writes (rows side by side) and the reads (32 rows of one piece) use all banks.
 // Bound by the vector unit, at the clock that products and exponentials side by side leave it: a score costs a multiply-add, an
 // exponential (as long as three of them) and an addition, a tile of 32 x 32 scores half as long on the matrix unit.  512
-// rows on 16384 slots, 8 heads of 128 features, 4 query heads each: 76 us for the maxima and sums, 100 for the masses (67.6
-// GFLOP of products each: 0.89 and 0.68 PFLOP/s; a large library product 1.29).
+// rows on 16384 slots, 8 heads of 128 features, 4 query heads each: 76 us for the maxima and sums, 86 for the masses (67.6
+// GFLOP of products each: 0.89 and 0.79 PFLOP/s; a large library product 1.29).  Chunks that a wave's side does not see
+// are passed over (the blocks of the last keys, where most are half seen or hidden, took 100 us).
 // ---------------------------------------------------------------------------------------------
 constexpr int WIDE_ROWS = 64;            // rows of a chunk
 constexpr int WIDE_OWN = 256;            // vectors or keys of a block
@@ -686,11 +717,11 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
     }
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) at[kk] = St::place(l32, 2 * kk + lh2);
-    const int first_pos = w.prefill ? 0 : w.newest + min(mine, w.vecs - 1) / a.G;
+    const int first_pos = w.prefill ? 0 : w.newest + min(mine, w.vecs - 1) / a.G, last_pos = w.prefill ? 0 : w.newest + min(mine + 63, w.vecs - 1) / a.G;
     const int chunks = (w.keys + WIDE_ROWS - 1) / WIDE_ROWS;
     u32x4 next[St::PER];
     int next_pos = 0, next_k0 = 0;
-    bool masked = false;                                             // the chunk holds keys that some of the wave's vectors do not see
+    bool masked = false, hidden = false;                             // the chunk holds keys that some of the wave's vectors do not see; no others
     // (what is loaded is not looked at here: that would wait for it)
     const auto ask = [&](int c) {
         next_k0 = min(c, chunks - 1) * WIDE_ROWS;
@@ -700,13 +731,15 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
         for (int i = 0; i < St::PER; ++i) next[i] = global_piece(rows + (unsigned)(min(St::row(i), last) * D + St::piece() * 8));
         if (!w.prefill) next_pos = w.pos[next_k0 + min(lane, last)];
     };
+    bool masked_next = false, hidden_next = false;
     const auto put = [&](int buffer, int c) {
 #pragma unroll
         for (int i = 0; i < St::PER; ++i) chunk[buffer * WIDE_ROWS * St::PIECES + St::place(St::row(i), St::piece())] = next[i];
         // (a prefill segment hides what lies past its end)
         const int p = next_k0 + lane < w.keys ? next_pos : 0x7FFFFFFF;
         if (tid < WIDE_ROWS) key_pos[c & 3][lane] = p;
-        return (bool)__any(p > first_pos);
+        masked_next = __any(p > first_pos);
+        hidden_next = __all(p > last_pos);
     };
     const auto hide = [&](f32x16 (&sc)[2], int c, int half) {
 #pragma unroll
@@ -748,10 +781,12 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
         sum[0] += more[0];
         sum[1] += more[1];
     };
-    f32x16 x[2], y[2];
+    f32x16 x[2], y[2] = {};
     if (chunks > 0) {
         ask(z);
-        masked = put(0, 0);
+        put(0, 0);
+        masked = masked_next;
+        hidden = hidden_next;
     }
     __syncthreads();
     all_loaded();
@@ -761,16 +796,21 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
     // half's (behind the last chunk: the last one again, of no use)
     const auto step = [&](auto buffer, int i) {
         constexpr int B = decltype(buffer)::value;
-        if (masked) hide(x, i, 0);
-        wide_scores<D, B, 1>(chunk, at, qf, y, slice_of(x));
-        settle(x);
-        const bool masked_next = put(B ^ 1, i + 1);
+        if (!hidden) {
+            if (masked) hide(x, i, 0);
+            wide_scores<D, B, 1>(chunk, at, qf, y, slice_of(x));
+            settle(x);
+        }
+        put(B ^ 1, i + 1);
         __syncthreads();
         ask(z + (i + 2) * splits);
-        if (masked) hide(y, i, 1);
+        if (!hidden || !hidden_next) {                               // (a hidden chunk's second half is what it was: all of it is hidden here)
+            if (masked) hide(y, i, 1);
+            wide_scores<D, B ^ 1, 0>(chunk, at, qf, x, slice_of(y));
+            settle(y);
+        }
         masked = masked_next;
-        wide_scores<D, B ^ 1, 0>(chunk, at, qf, x, slice_of(y));
-        settle(y);
+        hidden = hidden_next;
     };
     const int mine_chunks = z < chunks ? (chunks - z + splits - 1) / splits : 0;
     for (int i = 0; i < mine_chunks; i += 2) {
@@ -807,7 +847,7 @@ __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
         top = high;
     }
     if (i >= all || lane != 0) return;
-    a.rows_ml[i] = ok ? make_float2(top, sum > 0.f ? 1.f / sum : sum) : make_float2(1e30f, 0.f);      // (a row that sees nothing adds nothing; NaN stays)
+    a.rows_ml[i] = ok ? make_float2(top, sum > 0.f ? 1.f / sum : sum) : make_float2(NO_ROW, 0.f);      // (a row that sees nothing adds nothing; NaN stays)
     if (lh == 0) a.q_row[number] = ok ? (s * a.R + (a.rows ? a.rows[j] : j - s * a.N)) * a.H * a.G + number - j * a.G : -1;
 }
 
@@ -820,9 +860,12 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     __shared__ u32x4 chunk[2 * WIDE_ROWS * St::PIECES];
     __shared__ __align__(16) float top_of[4][WIDE_ROWS], inv_of[4][WIDE_ROWS];
     __shared__ __align__(16) int pos_of[4][WIDE_ROWS];
+    __shared__ int counted;                                          // any vector counts: without, a NaN key is no reason for a NaN
+    __shared__ long long spoiled_to;                                 // NaN rows spoil the slots that they see, no more: the last position
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh2 = lane >> 5;
     const Unit w(a, a.p_tiles, a.s_tiles, D);
     if (w.number * WIDE_OWN >= w.keys) return;
+    if (tid == 0) counted = 0, spoiled_to = -(1ll << 40);            // (the first wave's alone, until the last chunk has gone by)
     const int k0 = w.number * WIDE_OWN + wave * 64;
 
     u32x4 kf[2][DK];
@@ -839,6 +882,13 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) at[kk] = St::place(l32, 2 * kk + lh2);
     const bool any_hidden = !w.prefill && __any(pos[0] > w.newest || pos[1] > w.newest);          // from the first listed row, at least
+    // the wave's keys are hidden from a chunk's rows, all of them
+    const auto hidden_from = [&](int c) {
+        if (!any_hidden) return false;
+        const int last_pos = w.newest + min(c * WIDE_ROWS + WIDE_ROWS - 1, w.vecs - 1) / a.G;
+        return (bool)__all(pos[0] > last_pos && pos[1] > last_pos);
+    };
+    bool hidden = hidden_from(0);
     const int chunks = (w.vecs + WIDE_ROWS - 1) / WIDE_ROWS;
     const float2 *const ml = a.rows_ml + (size_t)w.lh * a.vecs + (w.prefill ? 0 : w.s * a.N * a.G);
     const int *const q_row = a.q_row + (w.prefill ? 0 : w.s * a.N * a.G);
@@ -879,9 +929,14 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
         for (int i = 0; i < St::PER; ++i) chunk[buffer * WIDE_ROWS * St::PIECES + St::place(St::row(i), St::piece())] = next[i];
         if (tid < WIDE_ROWS) {
             const bool past = next_v0 + lane >= w.vecs;
-            top_of[c & 3][lane] = past ? 1e30f : next_ml.x;
-            inv_of[c & 3][lane] = past ? 0.f : next_ml.y;
-            pos_of[c & 3][lane] = w.newest + (next_v0 + lane) / a.G;
+            top_of[c & 3][lane] = past ? NO_ROW : next_ml.x;
+            const int p = w.newest + (next_v0 + lane) / a.G;
+            const bool spoils = !past && next_ml.y != next_ml.y;
+            inv_of[c & 3][lane] = past || spoils ? 0.f : next_ml.y;
+            const bool counts = !past && next_ml.x != NO_ROW;
+            pos_of[c & 3][lane] = counts ? p : (int)0x80000000;
+            if (counts) counted = 1;
+            if (spoils) atomicMax(&spoiled_to, w.prefill ? 1ll << 40 : (long long)p);
         }
     };
     const auto hide = [&](f32x16 (&sc)[2], int c, int half) {
@@ -926,7 +981,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
 #pragma unroll
         for (int u = 0; u < 2; ++u) acc[1] = fmaf(e[u], inv[2 + u], acc[1]);
     };
-    f32x16 x[2], y[2];
+    f32x16 x[2], y[2] = {};
     if (chunks > 0) {
         find(0);
         ask(0);
@@ -938,15 +993,21 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     wide_scores<D, 0, 0>(chunk, at, kf, x, [](int) {});
     const auto step = [&](auto buffer, int c) {                      // (see mass_stats_wide)
         constexpr int B = decltype(buffer)::value;
-        if (any_hidden) hide(x, c, 0);
-        wide_scores<D, B, 1>(chunk, at, kf, y, slice_of(x, c, 0));
-        settle();
+        const bool hidden_next = hidden_from(c + 1);
+        if (!hidden) {
+            if (any_hidden) hide(x, c, 0);
+            wide_scores<D, B, 1>(chunk, at, kf, y, slice_of(x, c, 0));
+            settle();
+        }
         put(B ^ 1, c + 1);
         __syncthreads();
         ask(c + 2);
-        if (any_hidden) hide(y, c, 1);
-        wide_scores<D, B ^ 1, 0>(chunk, at, kf, x, slice_of(y, c, 1));
-        settle();
+        if (!hidden || !hidden_next) {                               // (see mass_stats_wide)
+            if (any_hidden) hide(y, c, 1);
+            wide_scores<D, B ^ 1, 0>(chunk, at, kf, x, slice_of(y, c, 1));
+            settle();
+        }
+        hidden = hidden_next;
     };
     for (int c = 0; c < chunks; c += 2) {
         step(std::integral_constant<int, 0>{}, c);
@@ -954,7 +1015,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const float add = acc[t] + __shfl_xor(acc[t], 32);
+        const float sum = acc[t] + __shfl_xor(acc[t], 32), add = pos[t] <= spoiled_to ? __builtin_nanf("") : counted ? sum : 0.f;
         const int key = k0 + 32 * t + l32;
         float *const to = either(w.prefill, a.mass_prefill, a.mass) + w.at + key;
         if (lh2 == 0 && key < w.keys) global_put(to, a.decay * global_value(to) + add);

@@ -246,3 +246,57 @@ def test_streams_without_a_prompt_in_one_pass(gpu, dim, cap, G, n):
         norm = lambda a: np.sqrt((a * a).sum(-1)).max()   # noqa: E731
         rel = 2 * (dim + 2) * 2.0 ** -23 * c["scale"] * norm(wide(part["q"])) * norm(wide(part["k"])) + (cap ** 0.5 + 16) * 2.0 ** -23
         assert np.all(np.abs(got[l:l + 1] - want) <= np.abs(want - 0.9 * part["mass"]) * rel + (np.abs(part["mass"]) + np.abs(want)) * 2 * 2.0 ** -24 + 1e-37)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_hidden_chunks_of_many_rows(gpu, dim):
+    """A prompt that is all chunk: half of all scores are hidden.  A row with NaN spoils what it sees, and nothing ahead of it."""
+    R = 330
+    c = make(19, 1, 1, 2, 3, dim, R, 0, R, [R], ordered=True)
+    check(gpu, c, None, 0.9)
+    c["q"][:, 100] = 0x7FC0
+    got, _ = check(gpu, c, None, 0.9)
+    assert np.all(np.isnan(got[:, 0, :, :101])) and np.all(np.isfinite(got[:, 0, :, 101:]))
+    shuffled = make(20, 1, 2, 1, 3, dim, 700, 0, 150, [700, 400])
+    check(gpu, shuffled, None, 0.9)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("L,S,H,G,cap,P,R", [
+    (1, 2, 2, 4, 90, 0, 7),                                      # the keys in one block: one pass
+    (1, 1, 1, 3, 60, 50, 5),
+    (1, 2, 2, 4, 150, 70, 12),                                   # maxima and sums by themselves
+    (2, 1, 1, 2, 4500, 0, 4),
+    (1, 2, 1, 2, 200, 140, 150),                                 # the wide products
+    (8, 16, 2, 2, 80, 70, 6),                                    # one pass after a shared segment's maxima
+])
+def test_rows_and_keys_that_are_not_finite(gpu, dim, L, S, H, G, cap, P, R):
+    """The definition's answer, element for element: a NaN row spoils the slots that it sees; a NaN key what its rows see; scores that are
+    all minus infinity count for nothing, plus infinity makes NaN."""
+    def fresh():
+        return make(21, L, S, H, G, dim, cap, P, R, [cap, cap - 2, *[cap - s % 3 for s in range(S)]][:S], ordered=True)
+    c = fresh()
+    c["q"][:, R // 2] = 0x7FC0                                   # stream 0, a row in the middle
+    got, got_p = check(gpu, c, None, 0.9)
+    assert np.all(np.isnan(got[:, 0, :, :cap - R + R // 2 + 1])) and np.all(np.isfinite(got[:, 0, :, cap - R + R // 2 + 1:]))
+    assert np.all(np.isfinite(got[:, 1:][~np.isnan(c["mass"][:, 1:])])) and (got_p is None or np.all(np.isnan(got_p)))
+    c = fresh()
+    c["k"][:, 0, :, cap - 2] = 0x7FC0                            # what only the two newest rows of stream 0 see
+    got, _ = check(gpu, c, None, 0.9)
+    assert np.all(np.isnan(got[:, 0]))
+    c["slot_pos"][:, 0, :, cap - 2] = cap + 5                    # nobody does
+    got, _ = check(gpu, c, None, 0.9)
+    assert np.all(np.isfinite(got[:, 0]))
+    if P:
+        c["k_prefill"][:, :, P // 2] = 0x7FC0                    # of a shared segment: a slot for which no row is there
+        c["q"][:] = 0x7FC0
+        got, got_p = check(gpu, c, [[-1] * R] * S, 0.9)
+        assert np.array_equal(got_p, np.float32(0.9) * c["mass_prefill"])
+    for sign in (0xFF80, 0x7F80):
+        c = fresh()
+        c["k"][..., 0] = 0x3F80
+        if P:
+            c["k_prefill"][..., 0] = 0x3F80
+        c["q"][:, R - 1, :, 0] = sign                            # the newest row of stream 0: all scores infinite
+        got, _ = check(gpu, c, None, 0.9)
+        assert np.all(np.isfinite(got[:, 0]) if sign == 0xFF80 else np.isnan(got[:, 0]))

@@ -4,9 +4,9 @@
 // stream, so counts and biases come from memory once, and new tokens enter the counts where they are read: no atomics, and
 // no second launch.  Rows are dealt out to the block's waves, a wave asks for several at once, and everything that is looked up
 // for a row or a token goes through LDS once: a wave that went through all 30 rows of a draft tree by itself, and looked
-// masks and path tokens up in memory, spent its time waiting (8 streams, 128256 tokens: 60 us, now 31: 4.1 TB/s).  What a stream's counts and biases do to a token is the same in all its rows: one of two factors and
-// a sum, made once (1 / repetition is rounded, which adds half a step to a logit); a token of a row's own path is looked up
-// again, which is rare.  Rows of an odd vocabulary start anywhere: 16-byte accesses at their element's alignment.
+// masks and path tokens up in memory, spent its time waiting (8 streams, 128256 tokens: 60 us, now 31: 4.1 TB/s).  What a
+// stream's counts and biases do to a token is the same in all its rows: one of two factors and a sum, made once (1 /
+// repetition is rounded, which adds half a step to a logit); a token of a row's own path is looked up again, which is rare.  Rows of an odd vocabulary start anywhere: 16-byte accesses at their element's alignment.
 #include <algorithm>
 #include <type_traits>
 

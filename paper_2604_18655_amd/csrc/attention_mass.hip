@@ -100,19 +100,40 @@ __device__ __forceinline__ void global_put(float *p, float v) { *(Global<float> 
 
 // What a block works on: a layer's and head's prefill segment or a stream's own, and a number within it.
 struct Unit {
-    int lh, l, h, s, number;
+    int lh, l, h, s;
+    int number;                          // of a tile of keys (the masses)
+    int tile, z;                         // of query vectors, and which share of the keys (maxima and sums)
     bool prefill;
     int n, newest;                       // listed rows of the stream, and the position of the first one
     int vecs, keys;                      // query vectors and keys
     const uint16_t *k;
     const int *pos;
     size_t at;                           // of the segment's first slot
+    // Blocks that share keys (a unit's tiles of query vectors) stand eight apart, on one die: its second-level cache has the
+    // keys for all of them.
+    __device__ __forceinline__ Unit(const MassArgs &a, int D)
+    {
+        int b = (int)blockIdx.x;
+        const int heads = a.L * a.H, shared = heads * a.p_blocks;
+        prefill = b < shared;
+        if (!prefill) b -= shared;
+        const int splits = prefill ? a.p_splits : a.s_splits, tiles = (prefill ? a.p_blocks : a.s_blocks) / splits;
+        const int units = heads * splits * (prefill ? 1 : a.S);
+        const int group = b / (8 * tiles), at_group = b - group * 8 * tiles, width = min(8, units - 8 * group);
+        tile = at_group / width;
+        int unit = 8 * group + at_group - tile * width;
+        z = unit % splits;
+        unit /= splits;
+        lh = prefill ? unit : unit / a.S;
+        s = prefill ? 0 : unit - lh * a.S;
+        number = 0;
+        rest(a, D);
+    }
     __device__ __forceinline__ Unit(const MassArgs &a, int p_blocks, int s_blocks, int D)
     {
         const int per_head = p_blocks + a.S * s_blocks;
         lh = (int)blockIdx.x / per_head;
-        l = lh / a.H;
-        h = lh - l * a.H;
+        tile = z = 0;
         number = (int)blockIdx.x - lh * per_head;
         prefill = number < p_blocks;
         s = 0;
@@ -121,6 +142,12 @@ struct Unit {
             s = number / s_blocks;
             number -= s * s_blocks;
         }
+        rest(a, D);
+    }
+    __device__ __forceinline__ void rest(const MassArgs &a, int D)
+    {
+        l = lh / a.H;
+        h = lh - l * a.H;
         keys = prefill ? a.P : max(0, min(a.len[s], a.cap));         // (asked for before the list is looked at)
         newest = prefill ? 0 : a.next_pos[s];
         n = prefill ? 0 : listed(a, s);
@@ -163,7 +190,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
 {
     constexpr int DK = D / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.number / splits, z = w.number - tile * splits;
+    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.tile, z = w.z;
     const int v0 = tile * QT * 16;
     if (v0 >= w.vecs) return;
 
@@ -294,7 +321,7 @@ template <int D, int PT, int QT>
 __global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
 {
     __shared__ float2 ml[MASS_WAVES][128];
-    const Unit w(a, a.p_blocks, a.s_blocks, D);
+    const Unit w(a, D);
     if (PT != QT && w.prefill) stats_tiles<D, PT>(a, w, ml);
     else                       stats_tiles<D, QT>(a, w, ml);
 }
@@ -696,8 +723,8 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
     __shared__ u32x4 chunk[2 * WIDE_ROWS * St::PIECES];
     __shared__ __align__(16) int key_pos[4][WIDE_ROWS];              // (read while the next but one is written)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh2 = lane >> 5;
-    const Unit w(a, a.p_blocks, a.s_blocks, D);
-    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.number / splits, z = w.number - tile * splits;
+    const Unit w(a, D);
+    const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.tile, z = w.z;
     const int v0 = tile * WIDE_OWN;
     if (v0 >= w.vecs) return;
     const int mine = v0 + wave * 64;                                 // first vector of the wave

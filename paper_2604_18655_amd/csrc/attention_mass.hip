@@ -44,6 +44,7 @@ struct MassArgs {
     int vecs;                            // S * N * G
     int p_splits, s_splits;              // blocks that share the keys of a query tile: prefill, stream segment
     int p_blocks, s_blocks;              // blocks of a layer and head: prefill; one stream (mass_stats)
+    int p_per, s_per;                    // tiles of 16 query vectors of a block (mass_stats)
     int p_tiles, s_tiles;                // the same (mass_add)
     float scale2, decay;                 // scale2 = scale * log2(e)
 };
@@ -191,7 +192,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
     constexpr int DK = D / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lq = lane >> 4;
     const int splits = w.prefill ? a.p_splits : a.s_splits, tile = w.tile, z = w.z;
-    const int v0 = tile * QT * 16;
+    const int per = w.prefill ? a.p_per : a.s_per, v0 = tile * per * 16, v_end = min(w.vecs, v0 + per * 16);
     if (v0 >= w.vecs) return;
 
     // keys as A operands (past the end: the last key), some chunks ahead of the one that is worked on
@@ -241,7 +242,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         const bool masked = nk < KC || (!w.prefill && __any(x.pos > w.newest));
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            if (QT > 1 && v0 + 16 * t >= w.vecs) break;
+            if (QT > 1 && v0 + 16 * t >= v_end) break;
             f32x4 sc[KC / 16];
 #pragma unroll
             for (int j = 0; j < KC / 16; ++j) {
@@ -306,7 +307,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
     }
     __syncthreads();
     const int v = v0 + (int)threadIdx.x;
-    if (threadIdx.x < QT * 16 && v < w.vecs) {
+    if (threadIdx.x < QT * 16 && v < v_end) {
         float top = NEG_BIG, all = 0.f;
 #pragma unroll
         for (int i = 0; i < MASS_WAVES; ++i) top = fmaxf(top, ml[i][threadIdx.x].x);
@@ -1077,6 +1078,7 @@ struct Plan {
     bool alone;                          // the prefill segment is the one stream's
     int p_tiles, s_tiles;                // query tiles of a block: prefill, stream segment
     int p_splits, s_splits, p_blocks, s_blocks;
+    int p_per, s_per;                    // query tiles of a block, evenly: 6 tiles are 3 and 3, not 4 and 2
     int key_tiles;                       // key tiles of a wave in mass_add
 };
 Plan plan_of(const mlora_attention_mass &d, int N)
@@ -1117,6 +1119,8 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     };
     p.p_splits = d.len_prefill > 0 && !p.alone ? splits_of(d.len_prefill) : 0;
     p.s_splits = p.stream ? 0 : splits_of(c.cap);
+    p.p_per = (int)ceil_div(ceil_div(all, 16), std::max(1ll, pt));
+    p.s_per = (int)ceil_div(ceil_div(own, 16), std::max(1ll, st));
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
     const int many = 4, keys = MASS_WAVES * 16 * many;
@@ -1179,6 +1183,8 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
     a.vecs = a.S * N * a.G;
     a.p_splits = p.p_splits;
     a.s_splits = p.s_splits;
+    a.p_per = p.p_per;
+    a.s_per = p.s_per;
     a.p_blocks = p.p_blocks;
     a.s_blocks = p.s_blocks;
     a.scale2 = d->scale * 1.44269504088896340736f;

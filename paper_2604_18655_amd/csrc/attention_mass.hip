@@ -240,54 +240,63 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
     const auto work = [&](const Keys &x, int c) {
         const int nk = min(KC, w.keys - c * KC);
         const bool masked = nk < KC || (!w.prefill && __any(x.pos > w.newest));
+        const float factor = masked ? 1.f : a.scale2;                // of scores (hidden ones: minus infinity, at any scale)
+        // (all tiles side by side, whether their vectors count or not: one after the other, each waits for its products)
+        f32x4 sc[QT][KC / 16];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            if (QT > 1 && v0 + 16 * t >= v_end) break;
-            f32x4 sc[KC / 16];
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int j = 0; j < KC / 16; ++j) {
-                sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                sc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < DK; ++kk) sc[j] = mfma16(x.f[j][kk], qf[t][kk], sc[j]);
+                for (int kk = 0; kk < DK; ++kk) sc[t][j] = mfma16(x.f[j][kk], qf[t][kk], sc[t][j]);
             }
-            unsigned see = ~0u;                                      // a bit per score
-            if (masked) {
-                see = 0;
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < KC / 16; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = 16 * j + 4 * lq + e;
+                    const int key_pos = __shfl(x.pos, key);          // (all lanes: before any condition)
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+                        sc[t][j][e] = key < nk && (w.prefill || key_pos <= pos[t]) ? sc[t][j][e] * a.scale2 : -__builtin_inff();
+                }
+        }
+        // Sums relative to maxima that may lie behind: the sums themselves tell when one does too far (the first chunk, and rarely
+        // another), and they are made again.
+        float add[QT], most;
+        const auto take = [&](float by) {
+            most = 0.f;
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                float of[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < KC / 16; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = 16 * j + 4 * lq + e;
-                        const int key_pos = __shfl(x.pos, key);      // (all lanes: before any condition)
-                        see |= key < nk && (w.prefill || key_pos <= pos[t]) ? 1u << (4 * j + e) : 0u;
-                    }
+                    for (int e = 0; e < 4; ++e) of[e & 1] += __builtin_amdgcn_exp2f(fmaf(sc[t][j][e], by, -m[t]));
+                add[t] = of[0] + of[1];
+                most = fmaxf(most, add[t]);
             }
-            // sums relative to a maximum that may lie behind: the sum itself tells when it does too far
-            float add[2] = {0.f, 0.f};
-            const auto take = [&](bool all) {
+        };
+        take(factor);
+        if (__any(most > FAR)) {
+            float by = factor;
+            asm volatile("" : "+v"(by));                             // (products that only this path needs are made here)
 #pragma unroll
-                for (int j = 0; j < KC / 16; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(sc[j][e], a.scale2, -m[t]));
-                        add[j & 1] += all || see >> (4 * j + e) & 1 ? p : 0.f;
-                    }
-            };
-            if (!masked) take(true);
-            else         take(false);
-            if (__any(add[0] + add[1] > FAR)) {                      // (the first chunk, and rarely another)
+            for (int t = 0; t < QT; ++t) {
                 float top = m[t];
 #pragma unroll
                 for (int j = 0; j < KC / 16; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, see >> (4 * j + e) & 1 ? sc[j][e] * a.scale2 : UNSEEN);
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[t][j][e] * by);
                 sum[t] *= __builtin_amdgcn_exp2f(m[t] - top);
                 m[t] = top;
-                add[0] = add[1] = 0.f;
-                take(false);
             }
-            sum[t] += add[0] + add[1];
+            take(by);
         }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sum[t] += add[t];
     };
     while (c < chunks) {
 #pragma unroll
@@ -319,7 +328,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
 }
 
 template <int D, int PT, int QT>
-__global__ __launch_bounds__(64 * MASS_WAVES) void mass_stats(const MassArgs a)
+__global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_stats(const MassArgs a)
 {
     __shared__ float2 ml[MASS_WAVES][128];
     const Unit w(a, D);
@@ -355,7 +364,7 @@ __device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int numbe
 // One block: KT tiles of 16 keys per wave against all query vectors that may see them.  TABLE: their maxima, sums and places have been
 // written down (mass_stream).
 template <int D, int KT, bool TABLE>
-__global__ __launch_bounds__(64 * MASS_WAVES) void mass_add(const MassArgs a)
+__global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
 {
     constexpr int DK = D / 32, KEYS = MASS_WAVES * KT * 16;
     __shared__ __align__(16) float top_of[BATCH], inv_of[BATCH];
@@ -1204,10 +1213,13 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
             mass_stats<D, decltype(prefill_tiles)::value, decltype(stream_tiles)::value><<<stats_grid, block, 0, s>>>(a);
         };
         constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 2> two{};
+        constexpr std::integral_constant<int, 3> three{};
         constexpr std::integral_constant<int, 4> four{};
         const auto narrow_stats = [&] {
-            if (p.s_tiles == 1) p.p_tiles == 1 ? stats(one, one) : stats(four, one);
-            else                stats(four, four);
+            const int per = p.s_tiles == 1 ? p.p_per : std::max(p.p_per, p.s_per);
+            const auto tiles = [&](auto q) { p.s_tiles == 1 ? stats(q, one) : stats(q, q); };
+            per <= 1 ? tiles(one) : per == 2 ? tiles(two) : per == 3 ? tiles(three) : tiles(four);
         };
         if (p.wide) {
             mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
@@ -1221,7 +1233,6 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
                 if (p.alone) mass_stream<D, VT, TK, W, true><<<grid, threads, 0, s>>>(a);
                 else         mass_stream<D, VT, TK, W, false><<<grid, threads, 0, s>>>(a);
             };
-            constexpr std::integral_constant<int, 2> two{};
             constexpr std::integral_constant<int, 8> eight{};
             constexpr std::integral_constant<int, 9> nine{};
             constexpr std::integral_constant<int, 16> sixteen{};

@@ -47,7 +47,13 @@ struct MassArgs {
     int p_per, s_per;                    // tiles of 16 query vectors of a block (mass_stats)
     int p_tiles, s_tiles;                // the same (mass_add)
     float scale2, decay;                 // scale2 = scale * log2(e)
+    float per_group, per_stream;         // 1 / G, 1 / N
 };
+
+// v / G and j / N in whole numbers (v < 2^16, j and N <= 2^12 and a little): (v + 1/2) / G lies 1 / 2G or more from the next whole number,
+// farther than its roundings reach.  An integer division takes thirty instructions, in front of every look-up.
+__device__ __forceinline__ int row_of(const MassArgs &a, int v) { return (int)(((float)v + 0.5f) * a.per_group); }
+__device__ __forceinline__ int stream_of(const MassArgs &a, int j) { return (int)(((float)j + 0.5f) * a.per_stream); }
 
 // listed rows of stream s that count; every wave finds it by itself
 __device__ __forceinline__ int listed(const MassArgs &a, int s)
@@ -161,9 +167,9 @@ struct Unit {
     // place of query vector v's features in a.q, and its number over all streams; false: it does not count
     __device__ __forceinline__ bool vector(const MassArgs &a, int v, int D, size_t &q, int &number_of) const
     {
-        const int j = v / a.G, g = v - j * a.G;
+        const int j = row_of(a, v), g = v - j * a.G;
         int st = s, row = j;
-        if (prefill) st = j / a.N, row = j - st * a.N;
+        if (prefill) st = stream_of(a, j), row = j - st * a.N;
         number_of = (st * a.N + row) * a.G + g;
         q = 0;
         if (prefill && !counts(a, st, row)) return false;
@@ -173,12 +179,12 @@ struct Unit {
     // the same in two steps, where it may be any vector if v does not count
     __device__ __forceinline__ int listed_row(const MassArgs &a, int v) const
     {
-        const int j = v / a.G;
-        return a.rows ? a.rows[(prefill ? 0 : (size_t)s * a.N) + j] : prefill ? j % a.N : j;      // (of all streams, one behind the other)
+        const int j = row_of(a, v);
+        return a.rows ? a.rows[(prefill ? 0 : (size_t)s * a.N) + j] : prefill ? j - stream_of(a, j) * a.N : j;      // (of all streams, one behind the other)
     }
     __device__ __forceinline__ size_t some_vector(const MassArgs &a, int v, int row, int D) const
     {
-        const int j = v / a.G, g = v - j * a.G, st = prefill ? j / a.N : s;
+        const int j = row_of(a, v), g = v - j * a.G, st = prefill ? stream_of(a, j) : s;
         row = row >= 0 && row < a.R ? row : 0;
         return ((((size_t)l * a.S + st) * a.R + row) * a.H * a.G + h * a.G + g) * D;
     }
@@ -230,7 +236,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
         const size_t q = w.some_vector(a, v, listed_row[t], D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
-        pos[t] = w.newest + v / a.G;
+        pos[t] = w.newest + row_of(a, v);
         m[t] = NEG_BIG;
         sum[t] = 0.f;
     }
@@ -392,7 +398,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
                 const float2 row = ok ? whole_row(a, w.lh, number) : make_float2(NO_ROW, 0.f);
                 top_of[i] = row.x;
                 inv_of[i] = row.y;
-                pos_of[i] = ok ? w.newest + v / a.G : (int)0x80000000;
+                pos_of[i] = ok ? w.newest + row_of(a, v) : (int)0x80000000;
                 q_of[i] = a.q + q;
             }
         }
@@ -562,7 +568,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
     for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            pos[v][e] = w.newest + (16 * v + 4 * lq + e) / a.G;
+            pos[v][e] = w.newest + row_of(a, 16 * v + 4 * lq + e);
             top[v][e] = NEG_BIG;
             sum[v][e] = 0.f;
         }
@@ -631,7 +637,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             if (!ALONE && a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
                 a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(m, counts ? inv : 0.f);
                 if (w.lh == 0) {
-                    const int j = vec / a.G;
+                    const int j = row_of(a, vec);
                     a.q_row[own + vec] = counts ? (w.s * a.R + (a.rows ? a.rows[(size_t)w.s * a.N + j] : j)) * a.H * a.G + vec - j * a.G : -1;
                 }
             }
@@ -662,7 +668,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
     for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (factor[v][e] != factor[v][e]) spoiled_to = max(spoiled_to, w.newest + (16 * v + first + e) / a.G);
+            if (factor[v][e] != factor[v][e]) spoiled_to = max(spoiled_to, w.newest + row_of(a, 16 * v + first + e));
 #pragma unroll 1
     for (int t = 0; t < TK; ++t) {                                   // (after the stores above: this wave's, to the same places)
         const Key k = key_of(t);
@@ -748,13 +754,13 @@ __global__ __launch_bounds__(256, 2) void mass_stats_wide(const MassArgs a)
         const size_t q = w.some_vector(a, v, D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[t][kk] = *reinterpret_cast<const u32x4 *>(a.q + q + 16 * kk + 8 * lh2);
-        pos[t] = w.prefill ? 0 : w.newest + v / a.G;
+        pos[t] = w.prefill ? 0 : w.newest + row_of(a, v);
         m[t] = NEG_BIG;
         sum[t] = 0.f;
     }
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) at[kk] = St::place(l32, 2 * kk + lh2);
-    const int first_pos = w.prefill ? 0 : w.newest + min(mine, w.vecs - 1) / a.G, last_pos = w.prefill ? 0 : w.newest + min(mine + 63, w.vecs - 1) / a.G;
+    const int first_pos = w.prefill ? 0 : w.newest + row_of(a, min(mine, w.vecs - 1)), last_pos = w.prefill ? 0 : w.newest + row_of(a, min(mine + 63, w.vecs - 1));
     const int chunks = (w.keys + WIDE_ROWS - 1) / WIDE_ROWS;
     u32x4 next[St::PER];
     int next_pos = 0, next_k0 = 0;
@@ -872,7 +878,7 @@ __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
     const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 8, all = (long long)a.L * a.H * a.vecs;
     const int lane = (int)threadIdx.x % 8;
     const long long at = i < all ? i : all - 1;
-    const int lh = (int)(at / a.vecs), number = (int)(at - (long long)lh * a.vecs), j = number / a.G, s = j / a.N, splits = a.p_splits + a.s_splits;
+    const int lh = (int)(at / a.vecs), number = (int)(at - (long long)lh * a.vecs), j = row_of(a, number), s = stream_of(a, j), splits = a.p_splits + a.s_splits;
     float top = NEG_BIG, sum = 0.f;
     if (lane < splits)
         merge_parts(a.part + ((size_t)lh * splits + lane) * a.vecs + number, (splits - lane + 7) / 8, 8 * a.vecs, top, sum);
@@ -922,7 +928,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     // the wave's keys are hidden from a chunk's rows, all of them
     const auto hidden_from = [&](int c) {
         if (!any_hidden) return false;
-        const int last_pos = w.newest + min(c * WIDE_ROWS + WIDE_ROWS - 1, w.vecs - 1) / a.G;
+        const int last_pos = w.newest + row_of(a, min(c * WIDE_ROWS + WIDE_ROWS - 1, w.vecs - 1));
         return (bool)__all(pos[0] > last_pos && pos[1] > last_pos);
     };
     bool hidden = hidden_from(0);
@@ -967,7 +973,7 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
         if (tid < WIDE_ROWS) {
             const bool past = next_v0 + lane >= w.vecs;
             top_of[c & 3][lane] = past ? NO_ROW : next_ml.x;
-            const int p = w.newest + (next_v0 + lane) / a.G;
+            const int p = w.newest + row_of(a, next_v0 + lane);
             const bool spoils = !past && next_ml.y != next_ml.y;
             inv_of[c & 3][lane] = past || spoils ? 0.f : next_ml.y;
             const bool counts = !past && next_ml.x != NO_ROW;
@@ -1191,6 +1197,8 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
     a.P = d->len_prefill;
     a.vecs = a.S * N * a.G;
     a.p_splits = p.p_splits;
+    a.per_group = 1.f / (float)a.G;
+    a.per_stream = 1.f / (float)a.N;
     a.s_splits = p.s_splits;
     a.p_per = p.p_per;
     a.s_per = p.s_per;

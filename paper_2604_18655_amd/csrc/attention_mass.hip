@@ -503,7 +503,7 @@ __device__ __forceinline__ float over_sixteen(float v, const Op &op)
 template <int D, int VT, int TK, int W, bool ALONE>
 __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 {
-    constexpr int DK = D / 32, AHEAD = D == 64 ? (TK < 4 ? TK : 4) : 2, V = 16 * VT;
+    constexpr int DK = D / 32, AHEAD = D == 64 ? (TK < 4 ? TK : 4) : 2, V = 16 * VT, GROUPS = (TK + 3) / 4;
     __shared__ __align__(16) float tops[W][V], sums[W][V], p_top[V], p_sum[V];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const Unit w(a, 0, 1, D);
@@ -521,6 +521,10 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
         k.live = key < keys;
         k.at = min(key, max(keys - 1, 0));
         return k;
+    };
+    const auto tile_lives = [&](int t) {
+        const int tile = t * W + wave;
+        return ALONE && tile < p_tiles ? true : (tile - p_tiles) * 16 < w.keys;
     };
     const uint16_t *const pk = ALONE ? a.k_prefill + (size_t)w.lh * a.P * D : nullptr;
     float *const mass = a.mass + w.at, *const p_mass = ALONE ? a.mass_prefill + (size_t)w.lh * a.P : nullptr;
@@ -556,11 +560,12 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
     }
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) ask(t);
-    float old[TK];
+    // Masses: a quarter of the wave takes one of four tiles.
+    float old[GROUPS];
 #pragma unroll
-    for (int t = 0; t < TK; ++t) {
-        const Key k = key_of(t);
-        old[t] = global_value((k.prefill ? p_mass : mass) + k.at);
+    for (int g = 0; g < GROUPS; ++g) {
+        const Key k = key_of(4 * g + lq);
+        old[g] = global_value((k.prefill ? p_mass : mass) + k.at);
     }
     int pos[VT][4];
     float top[VT][4], sum[VT][4];
@@ -568,25 +573,42 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
     for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            pos[v][e] = w.newest + row_of(a, 16 * v + 4 * lq + e);
+            const int vec = 16 * v + 4 * lq + e;
+            pos[v][e] = vec < w.vecs ? w.newest + row_of(a, vec) : (int)0x80000000;
             top[v][e] = NEG_BIG;
             sum[v][e] = 0.f;
         }
-    // scores: element e of sc[v][t] is vector 16 * v + 4 * lq + e against key l16 of tile t
+    // (vectors that do not count are zeros: what their place holds may be NaN)
+    if (w.vecs < V) {
+#pragma unroll
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+            for (int kk = 0; kk < DK; ++kk) qf[v][kk] = 16 * v + l16 < w.vecs ? qf[v][kk] : make_uint4(0, 0, 0, 0);
+    }
+    // Scores, not yet scaled: element e of sc[v][t] is vector 16 * v + 4 * lq + e against key l16 of tile t; hidden ones are minus
+    // infinity.  Tiles past the end are left out (their keys are asked for all the same: fewer loads on some ways make the
+    // compiler wait for more on all).
     f32x4 sc[VT][TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t) {
-        const bool live = key_of(t).live;
+        if (tile_lives(t)) {
 #pragma unroll
-        for (int v = 0; v < VT; ++v) {
-            sc[v][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int v = 0; v < VT; ++v) {
+                sc[v][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kk = 0; kk < DK; ++kk) sc[v][t] = mfma16(qf[v][kk], kf[t % AHEAD][kk], sc[v][t]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sc[v][t][e] = live && at[t] <= pos[v][e] ? sc[v][t][e] * a.scale2 : UNSEEN;
-                top[v][e] = fmaxf(top[v][e], sc[v][t][e]);
+                for (int kk = 0; kk < DK; ++kk) sc[v][t] = mfma16(qf[v][kk], kf[t % AHEAD][kk], sc[v][t]);
             }
+            const int key_pos = key_of(t).live ? at[t] : 0x7FFFFFFF;
+            if (__any(key_pos > w.newest)) {
+#pragma unroll
+                for (int v = 0; v < VT; ++v)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[v][t][e] = key_pos <= pos[v][e] ? sc[v][t][e] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int v = 0; v < VT; ++v)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top[v][e] = fmaxf(top[v][e], sc[v][t][e]);
         }
         if (t + AHEAD < TK) ask(t + AHEAD);
     }
@@ -608,19 +630,29 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], o[e]);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            top[v][e] = m[e];
+        for (int e = 0; e < 4; ++e) top[v][e] = m[e] * a.scale2;
+    }
 #pragma unroll
-            for (int t = 0; t < TK; ++t) {
-                sc[v][t][e] = __builtin_amdgcn_exp2f(sc[v][t][e] - m[e]);
+    for (int t = 0; t < TK; ++t) {
+        if (!tile_lives(t)) continue;
+#pragma unroll
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sc[v][t][e] = __builtin_amdgcn_exp2f(fmaf(sc[v][t][e], a.scale2, -top[v][e]));
                 sum[v][e] += sc[v][t][e];
             }
+    }
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
             sum[v][e] = over_sixteen(sum[v][e], [](float x, float y) { return x + y; });
             if (l16 == 0) sums[wave][16 * v + 4 * lq + e] = sum[v][e];
         }
-    }
     __syncthreads();
     float factor[VT][4];                                             // of a vector's weights
+    bool spoils[VT][4];                                              // a NaN row spoils the slots that it sees, no more: below
 #pragma unroll
     for (int v = 0; v < VT; ++v) {
         f32x4 all = {0.f, 0.f, 0.f, 0.f};
@@ -634,6 +666,8 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             const float total = all[e] * here + ps[e] * __builtin_amdgcn_exp2f(pt[e] - m), inv = total > 0.f ? 1.f / total : total;      // (NaN stays)
             const bool counts = vec < w.vecs;
             factor[v][e] = counts ? here * inv : 0.f;
+            spoils[v][e] = factor[v][e] != factor[v][e];
+            if (spoils[v][e]) factor[v][e] = 0.f;
             if (!ALONE && a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
                 a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(m, counts ? inv : 0.f);
                 if (w.lh == 0) {
@@ -644,35 +678,39 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
         }
     }
 #pragma unroll
-    for (int t = 0; t < TK; ++t) {
-        float add = 0.f;
+    for (int g = 0; g < GROUPS; ++g) {
+        float mine = 0.f;
 #pragma unroll
-        for (int v = 0; v < VT; ++v)
+        for (int t = 4 * g; t < TK && t < 4 * g + 4; ++t) {
+            if (!tile_lives(t)) continue;
+            float add = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add += factor[v][e] > 0.f ? sc[v][t][e] * factor[v][e] : 0.f;      // (not NaN: below)
-        add = over_quarters(add, [](float x, float y) { return x + y; });
-        const Key k = key_of(t);
-        if (lq == 0 && k.live) global_put((k.prefill ? p_mass : mass) + k.at, a.decay * old[t] + add);
+            for (int v = 0; v < VT; ++v)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) add = fmaf(sc[v][t][e], factor[v][e], add);
+            add = over_quarters(add, [](float x, float y) { return x + y; });
+            mine = lq == t - 4 * g ? add : mine;
+        }
+        const Key k = key_of(4 * g + lq);
+        if (k.live && 4 * g + lq < TK) global_put((k.prefill ? p_mass : mass) + k.at, a.decay * old[g] + (w.vecs > 0 ? mine : 0.f));
     }
-    // a NaN row spoils the slots that it sees, no more
-    bool spoils = false;
-    int spoiled_to = (int)0x80000000;
+    bool any_spoils = false;
 #pragma unroll
     for (int v = 0; v < VT; ++v)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) spoils |= factor[v][e] != factor[v][e];
-    if (!__any(spoils)) return;
-    int first = 4 * lq;                                              // (positions anew: kept from above, they cost a block per compute unit)
+        for (int e = 0; e < 4; ++e) any_spoils |= spoils[v][e];
+    if (!__any(any_spoils)) return;
+    int first = 4 * lq, spoiled_to = (int)0x80000000;                // (positions anew: kept from above, they cost a block per compute unit)
     asm volatile("" : "+v"(first));
 #pragma unroll
     for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (factor[v][e] != factor[v][e]) spoiled_to = max(spoiled_to, w.newest + row_of(a, 16 * v + first + e));
+            if (spoils[v][e]) spoiled_to = max(spoiled_to, w.newest + row_of(a, 16 * v + first + e));
 #pragma unroll 1
     for (int t = 0; t < TK; ++t) {                                   // (after the stores above: this wave's, to the same places)
         const Key k = key_of(t);
-        if (spoils && k.live && (k.prefill || w.pos[k.at] <= spoiled_to)) global_put((k.prefill ? p_mass : mass) + k.at, __builtin_nanf(""));
+        if (any_spoils && k.live && (k.prefill || w.pos[k.at] <= spoiled_to)) global_put((k.prefill ? p_mass : mass) + k.at, __builtin_nanf(""));
     }
 }
 
@@ -1116,7 +1154,7 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     p.stream = 0;
     p.stream_waves = 8;
     const bool only = d.len_prefill == 0 || p.alone;
-    if (!p.wide && own <= 32 && (stream_blocks >= (only ? 128 : 256) || (only && key_tiles <= 8))) {
+    if (!p.wide && d.scale > 0.f && own <= 32 && (stream_blocks >= (only ? 128 : 256) || (only && key_tiles <= 8))) {
         const int most = own <= 16 ? 16 : 9, most16 = own <= 16 ? 9 : 4;
         if (key_tiles > 32 && key_tiles <= 16 * most16 && (stream_blocks <= 256 || key_tiles > 8 * most)) p.stream_waves = 16;
         const int per_wave = (int)std::min(1000ll, ceil_div(key_tiles, p.stream_waves));

@@ -439,7 +439,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
         const auto ask = [&](int t0) {
             const uint16_t *const qp = q_of[min(t0, pad - 16) + l16] + 8 * lq;
 #pragma unroll
-            for (int kk = 0; kk < DK; ++kk) qn[kk] = *reinterpret_cast<const uint4 *>(qp + 32 * kk);
+            for (int kk = 0; kk < DK; ++kk) qn[kk] = __builtin_bit_cast(uint4, global_piece(qp + 32 * kk));
         };
         ask(0);
         for (int t0 = 0; t0 < pad; t0 += 16) {

@@ -1144,17 +1144,20 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     // (a layer's query vectors are reached by 32-bit offsets)
     p.wide = d.scale > 0.f && own >= WIDE_OWN && d.n_q_heads <= 1024;
     // One pass where a block holds the keys: up to 16 tiles in each of eight waves (9 with 17 to 32 vectors, whose scores take twice the
-    // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner.  A
-    // compute unit by itself draws little from memory, so it takes many blocks: 128 where it is the only launch (16 layers x 8
-    // heads, 2248 keys 16.7 us, in two passes 26; 32 blocks of 2000 keys 15.0 and 12.6) or the keys are few, 256 where
-    // it is the second of three, for streams that share a prefill segment (256 blocks 25.4 and 26.3 us, 128 blocks 24 and 20.4).
+    // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner.  As
+    // the only launch it is always taken up to 64 tiles (32 with more vectors): 1000 keys on 1 or 32 blocks 8.5 and 8.8 us, in
+    // two passes 10.5 and 12.0; 300 keys 5.6 and 9.8.  Beyond, a compute unit by itself draws too little from memory, so it
+    // takes blocks: one per feature (32 blocks of 2000 keys of 64 features 13.1 and 12.7 us, 64 blocks 12.3 and 16.3; 48 blocks of
+    // 1900 keys 14.5 and 13.8, 64 blocks 14.2 and 14.9).  As the second of three launches, for streams that share a
+    // prefill segment, 256 blocks (256 blocks 24.6 and 25.7 us, 192 blocks 24.0 and 22.7).
     p.alone = d.len_prefill > 0 && c.n_streams == 1;
     p.stream_vecs = own <= 16 ? 1 : 2;
     const long long key_tiles = ceil_div(c.cap, 16) + (p.alone ? ceil_div(d.len_prefill, 16) : 0), stream_blocks = lh * c.n_streams;
     p.stream = 0;
     p.stream_waves = 8;
     const bool only = d.len_prefill == 0 || p.alone;
-    if (!p.wide && d.scale > 0.f && own <= 32 && (stream_blocks >= (only ? 128 : 256) || (only && key_tiles <= 8))) {
+    const int few = own <= 16 ? 64 : 32;
+    if (!p.wide && d.scale > 0.f && own <= 32 && (only ? key_tiles <= few || stream_blocks >= c.head_dim : stream_blocks >= 256)) {
         const int most = own <= 16 ? 16 : 9, most16 = own <= 16 ? 9 : 4;
         if (key_tiles > 32 && key_tiles <= 16 * most16 && (stream_blocks <= 256 || key_tiles > 8 * most)) p.stream_waves = 16;
         const int per_wave = (int)std::min(1000ll, ceil_div(key_tiles, p.stream_waves));

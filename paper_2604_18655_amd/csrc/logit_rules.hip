@@ -4,7 +4,7 @@
 // stream, so counts and biases come from memory once, and new tokens enter the counts where they are read: no atomics, and
 // no second launch.  Rows are dealt out to the block's waves, a wave asks for several at once, and everything that is looked up
 // for a row or a token goes through LDS once: a wave that went through all 30 rows of a draft tree by itself, and looked
-// masks and path tokens up in memory, spent its time waiting (8 streams, 128256 tokens: 60 us, now 31: 4.1 TB/s).  What a
+// masks and path tokens up in memory, spent its time waiting (8 streams, 128256 tokens: 60 us, now 27: 4.8 TB/s).  What a
 // stream's counts and biases do to a token is the same in all its rows: one of two factors and a sum, made once (1 /
 // repetition is rounded, which adds half a step to a logit); a token of a row's own path is looked up again, which is rare.  Rows of an odd vocabulary start anywhere: 16-byte accesses at their element's alignment.
 #include <algorithm>
@@ -55,12 +55,18 @@ template <> struct RulesPack<float> {
         return __uint_as_float(x);
     }
 };
+// PAST: by the caches
+template <bool PAST>
 __device__ __forceinline__ void rules_store(uint16_t *at, const float (&z)[RULES_V])
 {
-    *reinterpret_cast<u32x4_any *>(at) = u32x4_any{pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7])};
+    const u32x4_any x = {pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7])};
+    if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_any *>(at));
+    else                *reinterpret_cast<u32x4_any *>(at) = x;
 }
+template <bool PAST>
 __device__ __forceinline__ void rules_store(float *at, const float (&z)[RULES_V])
 {
+    static_assert(!PAST, "(see the launch)");
     typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
     *reinterpret_cast<f32x4_any *>(at) = f32x4_any{z[0], z[1], z[2], z[3]};
     *reinterpret_cast<f32x4_any *>(at + 4) = f32x4_any{z[4], z[5], z[6], z[7]};
@@ -89,7 +95,7 @@ __device__ __forceinline__ float rules_mask(float z, int allowed, int i)
 
 // A block takes 512 tokens of a stream, eight per lane, its waves every blockDim / 64-th row.  Where the vocabulary ends inside a
 // lane's eight, they are the last eight and the first of them the lane before's: it stores its own only.
-template <class T, int AHEAD>
+template <class T, int AHEAD, bool PAST>
 __global__ __launch_bounds__(512) void logit_rules(const RulesArgs a)
 {
     __shared__ unsigned long long path[MLORA_RULES_MAX_ROWS], same[MLORA_RULES_MAX_ROWS];
@@ -226,7 +232,7 @@ __global__ __launch_bounds__(512) void logit_rules(const RulesArgs a)
 #pragma unroll
             for (int e = 0; e < RULES_V; ++e) z[e] = rules_mask(z[e], bits[u], e);
             if (first == 0) {
-                rules_store(out + r * V, z);
+                rules_store<PAST>(out + r * V, z);
             } else {
 #pragma unroll
                 for (int e = 1; e < RULES_V; ++e)
@@ -334,13 +340,20 @@ extern "C" mlora_status mlora_logit_rules_apply(const mlora_logit_rules *d, cons
         // block per compute unit (us: 30 rows in 63 blocks 8.7 and 8.0, in 2008 31 and 33; 7 rows in 1004 blocks, one wave 9.3, two 7.8).
         const int most = (long long)tiles * a.S <= 256 ? 8 : 4, waves = a.R <= 4 ? a.R : std::min(most, (a.R + 3) / 4);
         const dim3 grid((unsigned)tiles, (unsigned)a.S), block(64u * (unsigned)waves);
-        const auto go = [&](auto ahead) {
+        // bf16 results of their own that outgrow the second-level caches (8 x 4 MB) go past them: 8 streams x 30 rows x 128256 tokens
+        // 33.0 -> 26.6 us, with the draft step that reads them 51.5 -> 46.6 (with a plain copy of them 52.6 -> 57.4); of 64000
+        // tokens 17.5 -> 16.9, 33.7 -> 32.3.  In place 26.9 -> 27.7, and fp32 with the draft step 78.3 -> 80.2: not those.
+        const bool past = out != logits && size == 2 && (double)a.S * a.R * a.V * 2 > (double)(32 << 20);
+        const auto go = [&](auto ahead, auto by) {
             constexpr int AHEAD = decltype(ahead)::value;
-            if (size == 2) logit_rules<uint16_t, AHEAD><<<grid, block, 0, s>>>(a);
-            else           logit_rules<float, AHEAD><<<grid, block, 0, s>>>(a);
+            constexpr bool PAST = decltype(by)::value;
+            if (PAST || size == 2) logit_rules<uint16_t, AHEAD, PAST><<<grid, block, 0, s>>>(a);
+            else                   logit_rules<float, AHEAD, false><<<grid, block, 0, s>>>(a);
         };
-        if (a.R <= 4) go(std::integral_constant<int, 1>{});
-        else          go(std::integral_constant<int, 4>{});
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 4> four{};
+        if (past) a.R <= 4 ? go(one, std::true_type{}) : go(four, std::true_type{});
+        else      a.R <= 4 ? go(one, std::false_type{}) : go(four, std::false_type{});
     }
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }

@@ -117,3 +117,39 @@ def test_repeated_calls_give_the_same_bits(gpu):
     a, _ = run(gpu, c, False)
     b, _ = run(gpu, c, False)
     assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("S,R,V", [(4, 3, 1400003), (3, 30, 187000), (3, 30, 187001)])
+def test_results_that_outgrow_the_caches(gpu, S, R, V, bf16):
+    """More than 32 MiB of results in a buffer of their own: the same bits as in place, which the definition checks; and the
+    definition on the first and last tokens, which take part in no sum over others."""
+    lib, _, torch = gpu
+    assert S * R * V * 2 > 32 << 20
+    c = case(40, S, R, min(R, 9), V, 2)
+    dev = lambda a: torch.from_numpy(a.view(np.int32) if a.dtype == np.uint32 else a).cuda()   # noqa: E731
+    z = dev(c["z"]).to(torch.bfloat16 if bf16 else torch.float32)
+    results, counted = [], []
+    for in_place in (False, True):
+        given = {n: dev(c[n]) for n in NAMES}
+        rules = lib.LogitRules(S, R, c["T"], V, lib.Y_BF16 if bf16 else lib.Y_FP32, dev(c["parent"]), **given)
+        x = z.clone()
+        out = x if in_place else torch.full_like(x, 5.0)
+        rules.run(x, dev(c["tokens"]), out, new_tokens=dev(c["new"]))
+        torch.cuda.synchronize()
+        results.append(out)
+        counted.append(given["counts"])
+    bits = torch.int16 if bf16 else torch.int32
+    assert torch.equal(results[0].view(bits), results[1].view(bits)) and torch.equal(counted[0], counted[1])
+    for part in (slice(0, 64), slice((V - 40) // 32 * 32, V)):
+        kw = {n: c[n] for n in NAMES}
+        kw["counts"], kw["bias"] = c["counts"][:, part], c["bias"][:, part]
+        kw["masks"] = c["masks"][:, part.start // 32:part.stop // 32 + 1]
+        tokens = [[t - part.start for t in row] for row in c["tokens"].tolist()]
+        new = [[t - part.start for t in row] for row in c["new"].tolist()]
+        want, _ = D.logit_rules(z[:, part].double().cpu().numpy(), S, R, c["T"], c["parent"], tokens, new, **kw)
+        got = results[0][:, part].double().cpu().numpy()
+        size = np.abs(z[:, part].double().cpu().numpy()) * 2 + (4 + 2 + R) * 1.0 + 1 + np.abs(c["bias"][:, part]).max()
+        with np.errstate(invalid="ignore"):
+            same = (got == want) | (np.abs(got - want) <= size * 4 * 2.0 ** -24 + (np.abs(want) * 2.0 ** -8 if bf16 else 0))
+        assert np.all(same), np.argwhere(~same)[:3].tolist()

@@ -11,9 +11,9 @@
 // tickets per stream).
 //
 // A compression into a large cache is bound by its copy: 128 heads of 16384 slots with 128 features to 2048 slots, 268 MB read and written:
-// 14.4 us to find the slots, a block per head (dependent passes over 64 KB of ranks in registers), and 54 us to copy them, by
-// blocks all over the card (5.0 TB/s; stores that pass the caches by: 60 -> 54).  Up to COPY_ROWS slots a head the
-// block that found them copies them as well (15 heads of 1003 slots: 7.7 us a call).
+// 14.4 us to find the slots, a block per head (dependent passes over 64 KB of ranks in registers), and 52 us to copy them, by
+// blocks all over the card (5.2 TB/s).  Up to COPY_ROWS slots a head the block that found them copies them as well (15
+// heads of 1003 slots: 7.7 us a call).
 #include <algorithm>
 #include <type_traits>
 
@@ -436,8 +436,9 @@ struct CompressArgs {
 
 // One head's slots, all of them found: AT_ONCE rows of keys and of values side by side, AHEAD times.  from_slot(j) is the slot of
 // row j, the same for all lanes of a row; j counts from the first row of `to`.
-// STREAM: past the caches, where there is more of it than they hold.
-template <int D, int LANES, bool STREAM, class From>
+// PAST: read past the caches.  (Written past them, the call takes as long, and the attention that reads the copies next longer: 16
+// layers' compression and attention 250 us instead of 238.)
+template <int D, int LANES, bool PAST, class From>
 __device__ __forceinline__ void copy_rows(const CompressArgs &a, size_t from, size_t to, int rows, int lane, const From &from_slot)
 {
     constexpr int PIECES = D / 8, AT_ONCE = LANES / PIECES, AHEAD = 4;
@@ -450,14 +451,13 @@ __device__ __forceinline__ void copy_rows(const CompressArgs &a, size_t from, si
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + u * AT_ONCE + row, src = from_slot(j);
             const u32x4 *const kp = ks + (size_t)src * PIECES, *const vp = vs + (size_t)src * PIECES;
-            if (j < rows) kv[u] = STREAM ? __builtin_nontemporal_load(kp) : *kp, vv[u] = STREAM ? __builtin_nontemporal_load(vp) : *vp;
+            if (j < rows) kv[u] = PAST ? __builtin_nontemporal_load(kp) : *kp, vv[u] = PAST ? __builtin_nontemporal_load(vp) : *vp;
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + u * AT_ONCE + row;
             if (j >= rows) continue;
-            if (STREAM) __builtin_nontemporal_store(kv[u], kt + (size_t)j * PIECES), __builtin_nontemporal_store(vv[u], vt + (size_t)j * PIECES);
-            else        kt[(size_t)j * PIECES] = kv[u], vt[(size_t)j * PIECES] = vv[u];
+            kt[(size_t)j * PIECES] = kv[u], vt[(size_t)j * PIECES] = vv[u];
         }
     }
 }
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(THREADS) void cache_select(const CompressArgs a)
 }
 
 // A wave copies 64 slots of a head.
-template <int D>
+template <int D, bool PAST>
 __global__ __launch_bounds__(256) void cache_gather(const CompressArgs a)
 {
     const int runs = (a.budget + 63) / 64, lane = threadIdx.x & 63;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) void cache_gather(const CompressArgs a)
         a.to.mass[to + lane] = a.from.mass[from + slot];
         a.to.slot_pos[to + lane] = a.from.slot_pos[from + slot];
     }
-    copy_rows<D, 64, true>(a, from, to, __popcll(__ballot(slot >= 0)), lane, [&](int j) { return __shfl(slot, j); });
+    copy_rows<D, 64, PAST>(a, from, to, __popcll(__ballot(slot >= 0)), lane, [&](int j) { return __shfl(slot, j); });
 }
 
 mlora_status check(const mlora_stream_cache *c)
@@ -605,8 +605,12 @@ mlora_status mlora_stream_cache_compress(const mlora_stream_cache *from, const m
     };
     if (budget > COPY_ROWS) {
         select(std::integral_constant<int, 0>{});
-        if (from->head_dim == 64) cache_gather<64><<<gather, dim3(256), 0, s>>>(a);
-        else                      cache_gather<128><<<gather, dim3(256), 0, s>>>(a);
+        // From 128 MB read and copied on, half of the memory-side cache, what is read goes past the caches, which leaves them to the
+        // copies: 128 heads of 16384 slots with 128 features to 2048, 268 MB, 75 -> 66 us, with a reader of the copies 140 -> 128;
+        // 96 heads 62 -> 51 and 109 -> 97; 64 heads, 134 MB, 46 to 40 -> 40; to 700 of 8192, 92 MB, 31 -> 33.
+        const bool past = (double)heads * budget * from->head_dim * 8 >= (double)(128 << 20);
+        if (from->head_dim == 64) past ? cache_gather<64, true><<<gather, dim3(256), 0, s>>>(a) : cache_gather<64, false><<<gather, dim3(256), 0, s>>>(a);
+        else                      past ? cache_gather<128, true><<<gather, dim3(256), 0, s>>>(a) : cache_gather<128, false><<<gather, dim3(256), 0, s>>>(a);
     } else {
         if (from->head_dim == 64) select(std::integral_constant<int, 64>{});
         else                      select(std::integral_constant<int, 128>{});

@@ -1179,8 +1179,8 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     };
     p.p_splits = d.len_prefill > 0 && !p.alone ? splits_of(d.len_prefill) : 0;
     p.s_splits = p.stream ? 0 : splits_of(c.cap);
-    p.p_per = (int)ceil_div(ceil_div(all, 16), std::max(1ll, pt));
-    p.s_per = (int)ceil_div(ceil_div(own, 16), std::max(1ll, st));
+    p.p_per = pt > 0 ? (int)ceil_div(ceil_div(all, 16), pt) : 1;
+    p.s_per = p.stream ? 1 : (int)ceil_div(ceil_div(own, 16), st);
     p.p_blocks = (int)(pt * p.p_splits);
     p.s_blocks = (int)(st * p.s_splits);
     const int many = 4, keys = MASS_WAVES * 16 * many;
@@ -1270,8 +1270,8 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
         constexpr std::integral_constant<int, 3> three{};
         constexpr std::integral_constant<int, 4> four{};
         const auto narrow_stats = [&] {
-            const int per = p.s_tiles == 1 ? p.p_per : std::max(p.p_per, p.s_per);
-            const auto tiles = [&](auto q) { p.s_tiles == 1 ? stats(q, one) : stats(q, q); };
+            const int per = std::max(p.p_per, p.s_per);
+            const auto tiles = [&](auto q) { p.s_per == 1 ? stats(q, one) : stats(q, q); };
             per <= 1 ? tiles(one) : per == 2 ? tiles(two) : per == 3 ? tiles(three) : tiles(four);
         };
         if (p.wide) {

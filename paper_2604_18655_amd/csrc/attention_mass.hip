@@ -342,6 +342,19 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_stats(const MassArgs 
     else                       stats_tiles<D, QT>(a, w, ml);
 }
 
+// a value combined over the 16 lanes of a quarter of the wave; every lane gets the result
+template <class Op>
+__device__ __forceinline__ float over_sixteen(float v, const Op &op)
+{
+    const auto ror = [](float x, auto n) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(n)::value, 0xF, 0xF, false));
+    };
+    v = op(v, ror(v, std::integral_constant<int, 8>{}));
+    v = op(v, ror(v, std::integral_constant<int, 4>{}));
+    v = op(v, ror(v, std::integral_constant<int, 2>{}));
+    return op(v, ror(v, std::integral_constant<int, 1>{}));
+}
+
 // maximum and sum over what blocks left, four trips at a time
 __device__ __forceinline__ void merge_parts(const float2 *part, int n, int stride, float &top, float &all)
 {
@@ -382,6 +395,31 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
     const int k0 = w.number * KEYS + wave * KT * 16;
 
     const auto look_up = [&](int base, int pad) {
+        if constexpr (!TABLE) {
+            // Few vectors, of which many blocks had a share: sixteen lanes take turns with what these left, sixteen vectors at a time, where
+            // that is fewer trips than a lane by itself makes, four parts at a time (one row on 2176 keys, nine parts: 5.6 -> 5.0 us;
+            // three on 12000, both launches: 21.0 -> 16.3).
+            const int splits = a.p_splits + a.s_splits;
+            if (pad < 4 * splits) {
+                for (int i = tid >> 4; i < pad; i += 4 * MASS_WAVES) {
+                    size_t q;
+                    int number;
+                    const int v = min(base + i, w.vecs - 1);
+                    const bool ok = w.vector(a, v, D, q, number) && base + i < w.vecs;
+                    float top = NEG_BIG, all = 0.f;
+                    if (l16 < splits) merge_parts(a.part + ((size_t)w.lh * splits + l16) * a.vecs + number, (splits - l16 + 15) / 16, 16 * a.vecs, top, all);
+                    const float most = over_sixteen(top, [](float x, float y) { return fmaxf(x, y); });
+                    all = over_sixteen(all * __builtin_amdgcn_exp2f(top - most), [](float x, float y) { return x + y; });
+                    if (l16 == 0) {
+                        top_of[i] = ok ? most : NO_ROW;
+                        inv_of[i] = !ok ? 0.f : all > 0.f ? 1.f / all : all;
+                        pos_of[i] = ok ? w.newest + row_of(a, v) : (int)0x80000000;
+                        q_of[i] = a.q + q;
+                    }
+                }
+                return;
+            }
+        }
         for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
             const int v = min(base + i, w.vecs - 1);
             if constexpr (TABLE) {
@@ -487,19 +525,6 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
 // all there is.  The keys are a stream's own segment; where several streams share a prefill segment, its maxima and sums are
 // there already (mass_stats) and what its masses need is left behind; where the stream is the only one (ALONE) they are the
 // block's as well, in front of the others.
-// a value combined over the 16 lanes of a quarter of the wave; every lane gets the result
-template <class Op>
-__device__ __forceinline__ float over_sixteen(float v, const Op &op)
-{
-    const auto ror = [](float x, auto n) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(n)::value, 0xF, 0xF, false));
-    };
-    v = op(v, ror(v, std::integral_constant<int, 8>{}));
-    v = op(v, ror(v, std::integral_constant<int, 4>{}));
-    v = op(v, ror(v, std::integral_constant<int, 2>{}));
-    return op(v, ror(v, std::integral_constant<int, 1>{}));
-}
-
 template <int D, int VT, int TK, int W, bool ALONE>
 __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
 {

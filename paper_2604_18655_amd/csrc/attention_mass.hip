@@ -1174,11 +1174,12 @@ Plan plan_of(const mlora_attention_mass &d, int N)
           && (double)lh * ((double)c.cap * own * c.n_streams + (double)d.len_prefill * all) * own >= (double)(1 << 29);
     // One pass where a block holds the keys: up to 16 tiles in each of eight waves (9 with 17 to 32 vectors, whose scores take twice the
     // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner.  As
-    // the only launch it is always taken up to 64 tiles (32 with more vectors): 1000 keys on 1 or 32 blocks 8.5 and 8.8 us, in
-    // two passes 10.5 and 12.0; 300 keys 5.6 and 9.8.  Beyond, a compute unit by itself draws too little from memory, so it
-    // takes blocks: one per feature (32 blocks of 2000 keys of 64 features 13.1 and 12.7 us, 64 blocks 12.3 and 16.3; 48 blocks of
-    // 1900 keys 14.5 and 13.8, 64 blocks 14.2 and 14.9).  As the second of three launches, for streams that share a
-    // prefill segment, 256 blocks (256 blocks 24.6 and 25.7 us, 192 blocks 24.0 and 22.7).
+    // the only launch it is always taken up to 64 tiles (32 with more vectors): 1000 keys on 8 or 32 blocks 8.6 and 8.5 us, in
+    // two passes 11.5 and 11.3; 300 keys 5.6 and 9.8.  Beyond, a compute unit by itself draws too little from memory, so it
+    // takes blocks: one per feature (32 blocks of 2000 keys of 64 features 11.8 and 11.5 us, 64 blocks 12.2 and 14.3; 64 blocks of
+    // 1900 keys 14.6 and 14.1, 96 blocks 14.7 and 17.9; 64 blocks of 1800 keys of 128 features 18.8 and 19.8, 128 blocks 18.8
+    // and 31.3).  As the second of three launches, for streams that share a prefill segment, 256 blocks (256 blocks 24.4 and
+    // 25.8 us, 192 blocks 23.6 and 22.8).
     p.alone = d.len_prefill > 0 && c.n_streams == 1;
     p.stream_vecs = own <= 16 ? 1 : 2;
     const long long key_tiles = ceil_div(c.cap, 16) + (p.alone ? ceil_div(d.len_prefill, 16) : 0), stream_blocks = lh * c.n_streams;

@@ -143,7 +143,7 @@ def test_a_long_segment(gpu):
     (64, 40, 8, [0, 2, 3, 5]), (128, 40, 8, [0, 2, 3]), (64, 530, 6, [0, 1, 2, 3]),
 ])
 def test_streams_in_one_pass_beside_a_prefill_segment(gpu, dim, cap, G, rows):
-    """From 256 heads of streams on (128 without the shared segment): their segments are held by a block each (up to 2048 slots, and 1152 with more than 16 query
+    """From 256 heads of streams on, their segments are held by a block each (up to 2048 slots, and 1152 with more than 16 query
     vectors), every number of slots per wave and both numbers of vector tiles; lists of all lengths, an empty stream."""
     L, S, H = (8, 8, 4) if cap < 100 else (16, 8, 2)
     n, rng = len(rows), np.random.default_rng(cap)
@@ -187,7 +187,7 @@ def test_any_sign_of_the_scale(gpu, scale):
 
 
 def test_many_listed_rows_of_several_streams(gpu):
-    """The wide products with lists: rows that do not count, with NaN where they stand, and a shared segment."""
+    """Lists of all lengths: rows that do not count, with NaN where they stand, and a shared segment."""
     rng = np.random.default_rng(16)
     R = 70
     lists = [sorted(rng.permutation(R)[:64].tolist()), sorted(rng.permutation(R)[:40].tolist()) + [-1] * 24, [-1] * 64]

@@ -28,7 +28,6 @@ constexpr int KC = 32;                   // keys of a chunk in mass_stats
 constexpr int BATCH = 512;               // query vectors whose maxima mass_add holds at a time
 constexpr float NEG_BIG = -1.0e30f;      // "no key seen yet"
 constexpr float NO_ROW = __builtin_inff();   // the maximum of a query vector that does not count: weights of 0
-constexpr float UNSEEN = -3.0e38f;       // score of a key that is not visible: exp2(UNSEEN - NEG_BIG) is 0
 constexpr float FAR = 1.0995e12f;        // 2^40: how far sums may grow above their maximum before they are scaled down
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -37,15 +36,15 @@ struct MassArgs {
     const uint16_t *q, *k, *k_prefill;
     float *mass, *mass_prefill;
     const int *slot_pos, *len, *next_pos, *rows;
-    float2 *rows_ml;                     // wide calls: [L * H][vecs], maximum and 1 / sum
-    int *q_row;                          // wide calls: [vecs], vector of a.q of a layer's first head (of its query heads), -1: does not count
+    float2 *rows_ml;                     // wide calls, and mass_stream beside a prefill segment: [L * H][vecs], maximum and 1 / sum
+    int *q_row;                          // the same calls: [vecs], vector of a.q of a layer's first head (of its query heads), -1: does not count
     float2 *part;                        // [L * H][p_splits + s_splits][vecs]: maximum (of scores in units of log 2) and sum
     int L, S, H, G, R, N, cap, P;        // N: listed rows of a stream
     int vecs;                            // S * N * G
     int p_splits, s_splits;              // blocks that share the keys of a query tile: prefill, stream segment
     int p_blocks, s_blocks;              // blocks of a layer and head: prefill; one stream (mass_stats)
     int p_per, s_per;                    // tiles of 16 query vectors of a block (mass_stats)
-    int p_tiles, s_tiles;                // the same (mass_add)
+    int p_tiles, s_tiles;                // blocks of a layer and head: prefill; one stream (mass_add)
     float scale2, decay;                 // scale2 = scale * log2(e)
     float per_group, per_stream;         // 1 / G, 1 / N
 };
@@ -755,7 +754,6 @@ constexpr int WIDE_OWN = 256;            // vectors or keys of a block
 template <int D>
 struct Stage {
     static constexpr int PIECES = D / 8, PER = WIDE_ROWS * PIECES / 256;            // pieces of a row, of a thread
-    static constexpr int BYTES = WIDE_ROWS * D * 2;
     static __device__ __forceinline__ int row(int i) { return (i * 256 + (int)threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return (int)threadIdx.x % PIECES; }
     static __device__ __forceinline__ int place(int row, int piece) { return row * PIECES + (piece ^ (D == 128 ? row & 15 : row >> 1 & 7)); }

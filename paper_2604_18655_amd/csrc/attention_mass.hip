@@ -381,14 +381,15 @@ __device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int numbe
 
 // One block: KT tiles of 16 keys per wave against all query vectors that may see them.  TABLE: their maxima, sums and places have been
 // written down (mass_stream).
-template <int D, int KT, bool TABLE>
-__global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
+// SHARE: as many waves have the same keys, and take every SHARE-th tile of vectors each.
+template <int D, int KT, bool TABLE, int SHARE>
+__global__ __launch_bounds__(64 * MASS_WAVES * SHARE, 2) void mass_add(const MassArgs a)
 {
     constexpr int DK = D / 32, KEYS = MASS_WAVES * KT * 16;
     __shared__ __align__(16) float top_of[BATCH], inv_of[BATCH];
     __shared__ int pos_of[BATCH];
     __shared__ const uint16_t *q_of[BATCH];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, all_waves = __builtin_amdgcn_readfirstlane(tid >> 6), wave = all_waves % MASS_WAVES, share = all_waves / MASS_WAVES, l16 = lane & 15, lq = lane >> 4;
     const Unit w(a, a.p_tiles, a.s_tiles, D);
     if (w.number * KEYS >= w.keys) return;
     const int k0 = w.number * KEYS + wave * KT * 16;
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
             // three on 12000, both launches: 21.0 -> 16.3).
             const int splits = a.p_splits + a.s_splits;
             if (pad < 4 * splits) {
-                for (int i = tid >> 4; i < pad; i += 4 * MASS_WAVES) {
+                for (int i = tid >> 4; i < pad; i += 4 * MASS_WAVES * SHARE) {
                     size_t q;
                     int number;
                     const int v = min(base + i, w.vecs - 1);
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
                 return;
             }
         }
-        for (int i = tid; i < pad; i += 64 * MASS_WAVES) {
+        for (int i = tid; i < pad; i += 64 * MASS_WAVES * SHARE) {
             const int v = min(base + i, w.vecs - 1);
             if constexpr (TABLE) {
                 const float2 row = a.rows_ml[(size_t)w.lh * a.vecs + v];
@@ -478,8 +479,8 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) qn[kk] = __builtin_bit_cast(uint4, global_piece(qp + 32 * kk));
         };
-        ask(0);
-        for (int t0 = 0; t0 < pad; t0 += 16) {
+        ask(16 * share);
+        for (int t0 = 16 * share; t0 < pad; t0 += 16 * SHARE) {
             uint4 qf[DK];
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) qf[kk] = qn[kk];
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
 #pragma unroll
                 for (int kk = 0; kk < DK; ++kk) qf[kk] = bad ? make_uint4(0, 0, 0, 0) : qf[kk];
             }
-            ask(t0 + 16);
+            ask(t0 + 16 * SHARE);
             const f32x4 top = *reinterpret_cast<const f32x4 *>(top_of + t0 + 4 * lq), inv = *reinterpret_cast<const f32x4 *>(inv_of + t0 + 4 * lq);
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
@@ -512,9 +513,21 @@ __global__ __launch_bounds__(64 * MASS_WAVES, 2) void mass_add(const MassArgs a)
             }
         }
     }
+    __shared__ float others[SHARE > 1 ? SHARE - 1 : 1][MASS_WAVES][KT][16];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-        const float add = counted ? over_quarters(acc[t], [](float x, float y) { return x + y; }) : 0.f;
+        acc[t] = counted ? over_quarters(acc[t], [](float x, float y) { return x + y; }) : 0.f;
+        if (SHARE > 1 && share > 0 && lq == 0) others[share - 1][wave][t][l16] = acc[t];
+    }
+    if (SHARE > 1) {
+        __syncthreads();
+        if (share > 0) return;
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        float add = acc[t];
+#pragma unroll
+        for (int i = 1; i < SHARE; ++i) add += others[i - 1][wave][t][l16];
         const int key = k0 + 16 * t + l16;
         if (lq == 0 && key < w.keys) global_put(mass + key, a.decay * old[t] + add);
     }
@@ -1156,6 +1169,7 @@ struct Plan {
     int p_splits, s_splits, p_blocks, s_blocks;
     int p_per, s_per;                    // query tiles of a block, evenly: 6 tiles are 3 and 3, not 4 and 2
     int key_tiles;                       // key tiles of a wave in mass_add
+    int share;                           // waves of it that share keys
 };
 Plan plan_of(const mlora_attention_mass &d, int N)
 {
@@ -1209,6 +1223,10 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     p.s_blocks = (int)(st * p.s_splits);
     const int many = 4, keys = MASS_WAVES * 16 * many;
     p.key_tiles = lh * (ceil_div(d.len_prefill, keys) + (p.stream ? 0 : c.n_streams * ceil_div(c.cap, keys))) < 512 ? 2 : many;
+    // Few blocks with many vectors of 64 features are bound by the vectors' turns: two waves share keys and take turns (one head, 256
+    // vectors on 400 slots 16.8 -> 15.2 us, 400 vectors 21.1 -> 17.1; 128 vectors 15.1 and 15.1, 64 vectors 11.6 and 12.2; of 128
+    // features, whose keys are loaded twice for it, 256 vectors 20.2 and 21.0; four waves: 15.5 and 17.6 of the first two).
+    p.share = p.key_tiles == 2 && c.head_dim == 64 && (d.len_prefill > 0 ? all : own) >= 256 ? 2 : 1;
     return p;
 }
 int listed_rows(const mlora_attention_mass &d, int n_rows) { return n_rows > 0 ? n_rows : d.rows_per_stream; }
@@ -1298,6 +1316,16 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
             const auto tiles = [&](auto q) { p.s_per == 1 ? stats(q, one) : stats(q, q); };
             per <= 1 ? tiles(one) : per == 2 ? tiles(two) : per == 3 ? tiles(three) : tiles(four);
         };
+        const auto add_masses = [&](auto table) {
+            constexpr bool TABLE = decltype(table)::value;
+            if (p.key_tiles == 4) {
+                mass_add<D, 4, TABLE, 1><<<add_grid, block, 0, s>>>(a);
+            } else if (p.share == 1) {
+                mass_add<D, 2, TABLE, 1><<<add_grid, block, 0, s>>>(a);
+            } else if constexpr (D == 64) {
+                mass_add<D, 2, TABLE, 2><<<add_grid, dim3(2 * 64 * MASS_WAVES), 0, s>>>(a);
+            }
+        };
         if (p.wide) {
             mass_stats_wide<D><<<stats_grid, block, 0, s>>>(a);
             mass_merge<<<dim3((unsigned)((lh * a.vecs + 31) / 32)), block, 0, s>>>(a);
@@ -1324,13 +1352,11 @@ mlora_status mlora_attention_mass_add(const mlora_attention_mass *d, const void 
                 else                      stream_tiles(two, nine, eight);
             }
             if (a.P > 0 && !p.alone) {
-                if (p.key_tiles == 2) mass_add<D, 2, true><<<add_grid, block, 0, s>>>(a);
-                else                  mass_add<D, 4, true><<<add_grid, block, 0, s>>>(a);
+                add_masses(std::true_type{});
             }
         } else {
             narrow_stats();
-            if (p.key_tiles == 2) mass_add<D, 2, false><<<add_grid, block, 0, s>>>(a);
-            else                  mass_add<D, 4, false><<<add_grid, block, 0, s>>>(a);
+            add_masses(std::false_type{});
         }
     };
     if (c.head_dim == 64) all(std::integral_constant<int, 64>{});

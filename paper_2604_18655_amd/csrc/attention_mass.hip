@@ -370,13 +370,19 @@ __device__ __forceinline__ void merge_parts(const float2 *part, int n, int strid
         }
     }
 }
-// maximum and 1 / sum of a query vector over all blocks that looked at its keys; a row that sees nothing: 0
+// Maximum and 1 / sum of a row that counts; of one that sees nothing: 0.  Where the sum is NaN, 1 / sum is all that matters, and the
+// maximum may be plus infinity, NO_ROW: it is not handed on.
+__device__ __forceinline__ float2 counting_row(float top, float all)
+{
+    return make_float2(all == all ? top : 0.f, all > 0.f ? 1.f / all : all);
+}
+// the same of a query vector over all blocks that looked at its keys
 __device__ __forceinline__ float2 whole_row(const MassArgs &a, int lh, int number)
 {
     const int splits = a.p_splits + a.s_splits;
     float top = NEG_BIG, all = 0.f;
     merge_parts(a.part + (size_t)lh * splits * a.vecs + number, splits, a.vecs, top, all);
-    return make_float2(top, all > 0.f ? 1.f / all : all);            // (NaN stays)
+    return counting_row(top, all);
 }
 
 // One block: KT tiles of 16 keys per wave against all query vectors that may see them.  TABLE: their maxima, sums and places have been
@@ -411,8 +417,9 @@ __global__ __launch_bounds__(64 * MASS_WAVES * SHARE, 2) void mass_add(const Mas
                     const float most = over_sixteen(top, [](float x, float y) { return fmaxf(x, y); });
                     all = over_sixteen(all * __builtin_amdgcn_exp2f(top - most), [](float x, float y) { return x + y; });
                     if (l16 == 0) {
-                        top_of[i] = ok ? most : NO_ROW;
-                        inv_of[i] = !ok ? 0.f : all > 0.f ? 1.f / all : all;
+                        const float2 row = counting_row(most, all);
+                        top_of[i] = ok ? row.x : NO_ROW;
+                        inv_of[i] = ok ? row.y : 0.f;
                         pos_of[i] = ok ? w.newest + row_of(a, v) : (int)0x80000000;
                         q_of[i] = a.q + q;
                     }
@@ -706,7 +713,7 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             spoils[v][e] = factor[v][e] != factor[v][e];
             if (spoils[v][e]) factor[v][e] = 0.f;
             if (!ALONE && a.P > 0 && wave == 0 && l16 == 0 && vec < a.N * a.G) {
-                a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(m, counts ? inv : 0.f);
+                a.rows_ml[(size_t)w.lh * a.vecs + own + vec] = make_float2(inv == inv ? m : 0.f, counts ? inv : 0.f);      // (see counting_row)
                 if (w.lh == 0) {
                     const int j = row_of(a, vec);
                     a.q_row[own + vec] = counts ? (w.s * a.R + (a.rows ? a.rows[(size_t)w.s * a.N + j] : j)) * a.H * a.G + vec - j * a.G : -1;
@@ -964,7 +971,7 @@ __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
         top = high;
     }
     if (i >= all || lane != 0) return;
-    a.rows_ml[i] = ok ? make_float2(top, sum > 0.f ? 1.f / sum : sum) : make_float2(NO_ROW, 0.f);      // (a row that sees nothing adds nothing; NaN stays)
+    a.rows_ml[i] = ok ? counting_row(top, sum) : make_float2(NO_ROW, 0.f);
     if (lh == 0) a.q_row[number] = ok ? (s * a.R + (a.rows ? a.rows[j] : j - s * a.N)) * a.H * a.G + number - j * a.G : -1;
 }
 

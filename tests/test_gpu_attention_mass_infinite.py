@@ -1,0 +1,45 @@
+"""Attention weights of rows and keys with infinite features, in every form of the call.  A row that meets a score of plus infinity makes
+NaN of what it sees, whether other rows count or not; a key whose scores are all minus infinity receives nothing, whatever
+stands in the places of rows that do not count.  Bounds as in tests/test_gpu_attention_mass.py."""
+import numpy as np
+import pytest
+
+import test_gpu_attention_mass as T
+
+pytestmark = pytest.mark.gpu
+
+INF, MINUS_INF, ONE, NAN = 0x7F80, 0xFF80, 0x3F80, 0x7FC0
+
+
+def with_ones(c):
+    """Feature 0 is one in all rows and keys."""
+    for name in ("q", "k", "k_prefill"):
+        if c[name] is not None:
+            c[name][..., 0] = ONE
+    return c
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("L,S,H,G,cap,P,rows", [
+    (1, 1, 2, 1, 1100, 0, [[0]]),                                 # maxima and sums by themselves
+    (1, 2, 2, 4, 150, 70, [[1, -1], [-1, 0]]),
+    (8, 16, 2, 2, 80, 70, [[0, 1]] + [[-1, -1]] * 15),            # one pass, then the shared segment's masses
+    (1, 1, 2, 4, 90, 0, [[0]]),                                   # one pass
+    (1, 1, 1, 3, 60, 50, [[0, 1]]),
+])
+def test_only_rows_of_infinite_scores(gpu, dim, L, S, H, G, cap, P, rows):
+    c = with_ones(T.make(41 + dim, L, S, H, G, dim, cap, P, 2, [cap] * S, ordered=True))
+    c["q"][:, :, :, 0] = INF
+    got, got_p = T.check(gpu, c, rows, 0.9)
+    n = sum(r >= 0 for r in rows[0])
+    assert np.all(np.isnan(got[:, 0, :, :cap])) and n and (got_p is None or np.all(np.isnan(got_p)))
+    assert all(np.all(np.isfinite(got[:, s])) for s in range(1, S))
+
+
+def test_infinite_scores_in_one_of_two_waves_that_share_keys(gpu):
+    """280 vectors of 64 features on 400 slots: two waves take turns with the tiles of 16 vectors."""
+    for odd in (0, 1):
+        c = with_ones(T.make(43, 1, 1, 1, 4, 64, 400, 0, 70, [400], ordered=True))
+        c["q"][:, [r for r in range(70) if r // 4 % 2 == odd], :, 0] = INF
+        got, _ = T.check(gpu, c, None, 0.9)
+        assert np.all(np.isnan(got[0, 0, 0, :331]))

@@ -37,7 +37,8 @@ struct MassArgs {
     float *mass, *mass_prefill;
     const int *slot_pos, *len, *next_pos, *rows;
     float2 *rows_ml;                     // wide calls, and mass_stream beside a prefill segment: [L * H][vecs], maximum and 1 / sum
-    int *q_row;                          // the same calls: [vecs], vector of a.q of a layer's first head (of its query heads), -1: does not count
+    int *q_row;                          // the same calls: [vecs], vector of a.q of a layer's first head (of its query heads); negative: does
+                                         // not count (in wide calls ~ the place of a vector that does)
     float2 *part;                        // [L * H][p_splits + s_splits][vecs]: maximum (of scores in units of log 2) and sum
     int L, S, H, G, R, N, cap, P;        // N: listed rows of a stream
     int vecs;                            // S * N * G
@@ -480,9 +481,15 @@ __global__ __launch_bounds__(64 * MASS_WAVES * SHARE, 2) void mass_add(const Mas
         for (int t = 0; t < KT; ++t) masked |= !w.prefill && at[t] > w.newest;
         masked = __any(masked);
         // query vectors as A operands, a tile ahead: element e of a score belongs to vector 4 * lq + e
+        // (in the place of one that does not count, another of the tile: it has no weight, but zeros times an infinite key would be NaN,
+        // which a vector that sees the key makes of it by itself)
         uint4 qn[DK];
+        unsigned counting_next;                                      // a bit for each of the tile's that counts
         const auto ask = [&](int t0) {
-            const uint16_t *const qp = q_of[min(t0, pad - 16) + l16] + 8 * lq;
+            const int first = min(t0, pad - 16);
+            counting_next = (unsigned)__ballot(top_of[first + l16] != NO_ROW) & 0xFFFFu;
+            const int from = counting_next >> l16 & 1 || !counting_next ? l16 : __ffs(counting_next) - 1;
+            const uint16_t *const qp = q_of[first + from] + 8 * lq;
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) qn[kk] = __builtin_bit_cast(uint4, global_piece(qp + 32 * kk));
         };
@@ -491,14 +498,10 @@ __global__ __launch_bounds__(64 * MASS_WAVES * SHARE, 2) void mass_add(const Mas
             uint4 qf[DK];
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) qf[kk] = qn[kk];
-            // (vectors that do not count are zeros: what their place holds may be NaN)
-            const bool bad = top_of[t0 + l16] == NO_ROW;
-            counted |= !__all(bad);
-            if (__any(bad)) {
-#pragma unroll
-                for (int kk = 0; kk < DK; ++kk) qf[kk] = bad ? make_uint4(0, 0, 0, 0) : qf[kk];
-            }
+            const bool none = counting_next == 0;
             ask(t0 + 16 * SHARE);
+            if (none) continue;
+            counted = true;
             const f32x4 top = *reinterpret_cast<const f32x4 *>(top_of + t0 + 4 * lq), inv = *reinterpret_cast<const f32x4 *>(inv_of + t0 + 4 * lq);
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
@@ -572,11 +575,12 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
     };
     const uint16_t *const pk = ALONE ? a.k_prefill + (size_t)w.lh * a.P * D : nullptr;
     float *const mass = a.mass + w.at, *const p_mass = ALONE ? a.mass_prefill + (size_t)w.lh * a.P : nullptr;
-    // (vectors and what the prefill segment left come before the keys: loads return in their order)
+    // (vectors and what the prefill segment left come before the keys: loads return in their order.  In the place of a vector
+    // that does not count stands the last one that does: without weight, but zeros times an infinite key would be NaN.)
     uint4 qf[VT][DK];
 #pragma unroll
     for (int v = 0; v < VT; ++v) {
-        const size_t q = w.some_vector(a, min(16 * v + l16, a.N * a.G - 1), D);
+        const size_t q = w.some_vector(a, min(16 * v + l16, max(w.vecs, 1) - 1), D);
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk) qf[v][kk] = *reinterpret_cast<const uint4 *>(a.q + q + 8 * lq + 32 * kk);
     }
@@ -622,13 +626,6 @@ __global__ __launch_bounds__(64 * W) void mass_stream(const MassArgs a)
             top[v][e] = NEG_BIG;
             sum[v][e] = 0.f;
         }
-    // (vectors that do not count are zeros: what their place holds may be NaN)
-    if (w.vecs < V) {
-#pragma unroll
-        for (int v = 0; v < VT; ++v)
-#pragma unroll
-            for (int kk = 0; kk < DK; ++kk) qf[v][kk] = 16 * v + l16 < w.vecs ? qf[v][kk] : make_uint4(0, 0, 0, 0);
-    }
     // Scores, not yet scaled: element e of sc[v][t] is vector 16 * v + 4 * lq + e against key l16 of tile t; hidden ones are minus
     // infinity.  Tiles past the end are left out (their keys are asked for all the same: fewer loads on some ways make the
     // compiler wait for more on all).
@@ -959,7 +956,8 @@ __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
     const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 8, all = (long long)a.L * a.H * a.vecs;
     const int lane = (int)threadIdx.x % 8;
     const long long at = i < all ? i : all - 1;
-    const int lh = (int)(at / a.vecs), number = (int)(at - (long long)lh * a.vecs), j = row_of(a, number), s = stream_of(a, j), splits = a.p_splits + a.s_splits;
+    const int lh = (int)(at / a.vecs), number = (int)(at - (long long)lh * a.vecs), j = row_of(a, number), splits = a.p_splits + a.s_splits;
+    int s = stream_of(a, j);
     float top = NEG_BIG, sum = 0.f;
     if (lane < splits)
         merge_parts(a.part + ((size_t)lh * splits + lane) * a.vecs + number, (splits - lane + 7) / 8, 8 * a.vecs, top, sum);
@@ -972,7 +970,22 @@ __global__ __launch_bounds__(256) void mass_merge(const MassArgs a)
     }
     if (i >= all || lane != 0) return;
     a.rows_ml[i] = ok ? counting_row(top, sum) : make_float2(NO_ROW, 0.f);
-    if (lh == 0) a.q_row[number] = ok ? (s * a.R + (a.rows ? a.rows[j] : j - s * a.N)) * a.H * a.G + number - j * a.G : -1;
+    if (lh == 0) {
+        int row = a.rows ? a.rows[j] : j - s * a.N;
+        if (!ok) {
+            // another row that counts, of this stream or of the next one that has any (or none does: any row)
+            int t = s;
+            for (int i = 0; i < a.S; ++i) {
+                row = a.rows[(size_t)t * a.N];
+                if (row >= 0 && row < a.R) break;
+                row = 0;
+                t = t + 1 < a.S ? t + 1 : 0;
+            }
+            s = t;
+        }
+        const int at = (s * a.R + row) * a.H * a.G + number - j * a.G;
+        a.q_row[number] = ok ? at : ~at;
+    }
 }
 
 // 256 keys of a segment against all query vectors that may see them.
@@ -1020,7 +1033,6 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     u32x4 next[St::PER];
     float2 next_ml = make_float2(0.f, 0.f);
     int rows[St::PER], next_v0 = 0;                                  // where the next chunk's rows stand: a chunk ahead of them
-    unsigned bad = 0;                                                // a bit for each of the chunk's that does not count
     // (what is loaded is not looked at here: that would wait for it)
     const auto find = [&](int c) {
 #pragma unroll
@@ -1028,27 +1040,15 @@ __global__ __launch_bounds__(256, 2) void mass_add_wide(const MassArgs a)
     };
     const auto ask = [&](int c) {
         next_v0 = c * WIDE_ROWS;
-        int any = next_v0 + WIDE_ROWS > w.vecs ? -1 : 0;
+        // (in the place of a row that does not count, one that does, and past the end the last: without weight, but zeros times an
+        // infinite key would be NaN)
 #pragma unroll
-        for (int i = 0; i < St::PER; ++i) {
-            any |= rows[i];
-            next[i] = *reinterpret_cast<const u32x4 *>(q + ((unsigned)max(rows[i], 0) * D + St::piece() * 8));
-        }
-        bad = 0;
-        if (__any(any < 0)) {
-#pragma unroll
-            for (int i = 0; i < St::PER; ++i) bad |= rows[i] < 0 || next_v0 + St::row(i) >= w.vecs ? 1u << i : 0u;
-        }
+        for (int i = 0; i < St::PER; ++i)
+            next[i] = *reinterpret_cast<const u32x4 *>(q + ((unsigned)max(rows[i], ~rows[i]) * D + St::piece() * 8));
         find(c + 1);
         next_ml = ml[(unsigned)min(next_v0 + lane, w.vecs - 1)];
     };
     const auto put = [&](int buffer, int c) {
-        // (rows that do not count are zeros: what their place holds may be NaN)
-        if (__any(bad != 0)) {
-#pragma unroll
-            for (int i = 0; i < St::PER; ++i)
-                if (bad >> i & 1) next[i] = u32x4{0, 0, 0, 0};
-        }
 #pragma unroll
         for (int i = 0; i < St::PER; ++i) chunk[buffer * WIDE_ROWS * St::PIECES + St::place(St::row(i), St::piece())] = next[i];
         if (tid < WIDE_ROWS) {

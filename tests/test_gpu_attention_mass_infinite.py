@@ -43,3 +43,32 @@ def test_infinite_scores_in_one_of_two_waves_that_share_keys(gpu):
         c["q"][:, [r for r in range(70) if r // 4 % 2 == odd], :, 0] = INF
         got, _ = T.check(gpu, c, None, 0.9)
         assert np.all(np.isnan(got[0, 0, 0, :331]))
+
+
+@pytest.mark.parametrize("dim,L,S,H,G,cap,P,R,n", [
+    (64, 1, 2, 2, 4, 90, 0, 3, None), (128, 1, 2, 2, 5, 90, 0, 4, None),          # one pass
+    (64, 1, 1, 1, 3, 60, 50, 3, None), (128, 1, 1, 2, 3, 60, 50, 3, None),
+    (64, 1, 2, 2, 4, 150, 70, 11, None), (128, 1, 2, 2, 4, 150, 70, 11, None),    # maxima and sums by themselves
+    (64, 1, 3, 2, 4, 150, 70, 11, 7), (128, 2, 1, 1, 2, 4500, 0, 4, None),
+    (64, 8, 16, 2, 2, 80, 70, 6, 3), (128, 8, 16, 2, 2, 80, 70, 6, 3),            # one pass, then the shared segment's masses
+    (64, 1, 1, 1, 4, 400, 0, 70, None),                                           # two waves share keys
+    (64, 1, 1, 4, 8, 500, 0, 190, None), (128, 1, 1, 2, 4, 500, 0, 190, None),    # the wide products
+    (128, 4, 3, 2, 4, 300, 130, 70, 64), (64, 4, 3, 4, 8, 300, 130, 70, 64),
+])
+def test_keys_of_minus_infinity_beside_rows_that_do_not_count(gpu, dim, L, S, H, G, cap, P, R, n):
+    c = with_ones(T.make(44 + dim, L, S, H, G, dim, cap, P, R, [cap] * S, ordered=True))
+    plain = {"k": c["k"].copy(), "k_prefill": None if P == 0 else c["k_prefill"].copy()}
+    rows = None
+    if n is not None:                                              # lists of all lengths, one of them empty
+        rows = [(list(range(R))[R - n:][:k] + [-1] * n)[:n] for k in ([n, n // 2 + 1, 0, 1] * S)[:S]]
+        unlisted = [s * R + r for s in range(S) for r in range(R) if r not in rows[s]]
+        c["q"][:, unlisted] = NAN
+    dead = [1, 17, min(33, cap - R - 1)]                           # seen by every row
+    c["k"][:, :, :, dead, 0] = MINUS_INF
+    if P:
+        c["k_prefill"][:, :, [0, P - 1], 0] = MINUS_INF
+    got, got_p = T.check(gpu, c, rows, 0.9)
+    assert np.all(np.isfinite(got)) and np.array_equal(got[..., dead], np.float32(0.9) * c["mass"][..., dead])
+    if P:
+        assert np.all(np.isfinite(got_p)) and np.array_equal(got_p[..., [0, P - 1]], np.float32(0.9) * c["mass_prefill"][..., [0, P - 1]])
+    assert not np.array_equal(plain["k"], c["k"])

@@ -578,7 +578,7 @@ def _call_buffer(t, where: str, itemsize: int, n: int) -> None:
 class Rope:
     """Rotary positions (mlora_rope): `rot` of head_dim features turn, in pairs of the half or the interleaved layout, by
     frequencies that are plain, divided by factor (linear), of a larger base (base) or stretched where they turn fewer than
-    low..high times within context positions (turns).  Keeps the device table of the frequencies."""
+    low..high times within context positions (turns).  Keeps the table of the frequencies, on the device where it is to be used."""
 
     def __init__(self, head_dim: int, rot: int, layout: int = ROPE_HALF, scaling: int = ROPE_PLAIN, theta: float = 10000.0,
                  factor: float = 1.0, low: float = 1.0, high: float = 4.0, context: float = 8192.0, device="cuda:0"):
@@ -591,6 +591,7 @@ class Rope:
 
     def rows(self, M: int, rows_per_stream: Optional[int], base, offset) -> _RopeRowsStruct:
         R = int(M if rows_per_stream is None else rows_per_stream)
+        _buffer(self.quarter_turns, "rope frequencies", 8)
         if base is not None:
             _buffer(base, "rope base", 4, n=M // max(1, R))
         if offset is not None:
@@ -742,6 +743,8 @@ class AttentionMass:
         if rows is not None:
             listed = rows.numel() // self.streams
             _call_buffer(rows, where, 4, self.streams * listed)
+        if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+            raise MloraError(_EINVAL, where)
         st = self.fn(self.ref, q.data_ptr(), None if rows is None else rows.data_ptr(), listed,
                      None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
                      _stream() if stream is None else stream)

@@ -1,0 +1,71 @@
+"""What the Python side of the decoding loop's calls refuses before the library sees a pointer (no GPU: tensors that say they
+are on the device, and a library that records its calls)."""
+import pytest
+import torch
+
+import paper_2604_18655_amd as lib
+from paper_2604_18655_amd import binding as B
+
+EINVAL, ESHAPE = -1, -2
+
+
+class OnDevice:
+    """A tensor that says it is device memory."""
+
+    def __init__(self, t):
+        self.t = t
+
+    is_cuda = True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def dev(*shape, dtype=torch.int32):
+    return OnDevice(torch.zeros(shape, dtype=dtype))
+
+
+def refused(make, status=EINVAL):
+    with pytest.raises(lib.MloraError) as e:
+        make()
+    assert e.value.status == status
+
+
+def a_cache(**kw):
+    L, S, H, cap, D = 1, 2, 3, 8, 64
+    t = dict(k=dev(L, S, H, cap, D, dtype=torch.bfloat16), v=dev(L, S, H, cap, D, dtype=torch.bfloat16), mass=dev(L, S, H, cap, dtype=torch.float32),
+             slot_pos=dev(L, S, H, cap), len=dev(S), next_pos=dev(S))
+    t.update(kw)
+    return lib.StreamCache(*(t[n] for n in ("k", "v", "mass", "slot_pos", "len", "next_pos")))
+
+
+def recorder(calls):
+    def call(*args):
+        calls.append(args)
+        return 0
+    return call
+
+
+def a_mass(cache=None, **kw):
+    op = lib.AttentionMass(cache or a_cache(), 6, 4, 0.125, **kw)
+    calls = []
+    op.fn = recorder(calls)
+    return op, calls
+
+
+def test_frequencies_on_the_host_are_refused():
+    r = lib.Rope(64, 64, device="cpu")
+    refused(lambda: r.rows(4, None, None, None))
+    refused(lambda: lib.RopeTables(r, dev(4, 32, dtype=torch.float32), dev(4, 32, dtype=torch.float32), 4))
+    refused(lambda: lib.RopePlan(r, [], 4, lib.Y_FP32))
+
+
+def test_workspaces_on_the_host_or_with_gaps_are_refused():
+    op, calls = a_mass()
+    q = dev(1, 8, 6, 64, dtype=torch.bfloat16)
+    for ws in (torch.zeros(1 << 16, dtype=torch.uint8), OnDevice(torch.zeros(1, dtype=torch.uint8).expand(1 << 16)),
+               OnDevice(torch.zeros(1 << 17, dtype=torch.uint8)[::2])):
+        refused(lambda: op.run(q, None, ws, stream=0))
+    assert not calls
+    op.run(q, None, dev(1 << 16, dtype=torch.uint8), stream=0)
+    assert len(calls) == 1

@@ -32,7 +32,7 @@ class DecoderLayerStep:
                  h, rope_cos, rope_sin, row_adapter, M: int, eps: float = 1e-5, h_sq=None, q=None):
         """proj_*: binding.Proj on the device; attention: descriptor whose k_new / v_new are the
         tensors this step writes k and v to; h bf16 [M][hidden] (int16 tensor); rope tables fp32
-        [M][32]; q: where the rotated queries go (a tensor of its own if None)."""
+        [M][32]; q: where the rotated queries go, bf16 [M][columns of proj_q] (a tensor of its own if None)."""
         dev = h.device
         hidden, ffn = proj_q.K, proj_gate_up.N // 2
         i16 = lambda n: torch.empty((M, n), dtype=torch.int16, device=dev)
@@ -42,6 +42,11 @@ class DecoderLayerStep:
         self.h_sq = h_sq                                 # [M][parts] from the previous layer, or None
         self.sq2 = torch.empty((M, parts), dtype=torch.float32, device=dev)
         self.out_sq = torch.empty((M, parts), dtype=torch.float32, device=dev)
+        if q is not None and (q.device != dev or q.element_size() != 2 or q.is_floating_point() and q.dtype != torch.bfloat16
+                              or not q.is_contiguous()):
+            raise B.MloraError(B._EINVAL, "decoder layer's queries")
+        if q is not None and q.numel() != M * proj_q.N:
+            raise B.MloraError(B._ESHAPE, "decoder layer's queries")
         self.q = i16(proj_q.N) if q is None else q
         self.k_new, self.v_new = attention.keep[7], attention.keep[8]
         self.attn = i16(proj_q.N)

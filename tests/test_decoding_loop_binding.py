@@ -69,3 +69,19 @@ def test_workspaces_on_the_host_or_with_gaps_are_refused():
     assert not calls
     op.run(q, None, dev(1 << 16, dtype=torch.uint8), stream=0)
     assert len(calls) == 1
+
+
+def test_a_place_for_the_queries_of_another_size_is_refused():
+    from paper_2604_18655_amd.decoder import DecoderLayerStep
+    M, hidden = 6, 128
+    proj = lambda K, N: lib.Proj(K, N, 32, torch.zeros(16, dtype=torch.uint8))   # noqa: E731
+    projs = [proj(hidden, 128), proj(hidden, 64), proj(hidden, 64), proj(128, hidden), proj(hidden, 256), proj(128, hidden)]
+    i32, i16 = (lambda *s: torch.zeros(s, dtype=torch.int32)), (lambda *s: torch.zeros(s, dtype=torch.int16))   # noqa: E731
+    attention = lib.TreeAttention(2, 1, 64, 1, M, 0.125, None, None, None, None, None, None, None, i16(M, 64), i16(M, 64), i32(M),
+                                  torch.zeros(M, dtype=torch.uint8), 0, 0, 0)
+    table = torch.zeros(M, 32)
+    step = lambda q: DecoderLayerStep(*projs, attention, i16(M, hidden), table, table, None, M, q=q)   # noqa: E731
+    for q, status in ((i16(M - 1, 128), ESHAPE), (i16(M, 64), ESHAPE), (i16(128, M).t(), EINVAL), (torch.zeros((M, 128)), EINVAL), (i16(M, 128).to("meta"), EINVAL)):
+        refused(lambda: step(q), status)
+    mine = i16(M, 128)
+    assert step(mine).q is mine and step(None).q.shape == (M, 128)

@@ -693,6 +693,8 @@ class StreamCache:
         if rows is not None:
             listed = rows.numel() // self.streams
             _call_buffer(rows, where, 4, self.streams * listed)
+            if listed == 0:                              # (its pointer is null: all rows)
+                raise MloraError(_ESHAPE, where)
         st = self.append_fn(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
                             None if rows is None else rows.data_ptr(), listed, budget, sink, recent,
                             _stream() if stream is None else stream)
@@ -743,6 +745,8 @@ class AttentionMass:
         if rows is not None:
             listed = rows.numel() // self.streams
             _call_buffer(rows, where, 4, self.streams * listed)
+            if listed == 0:                              # (its pointer is null: all rows)
+                raise MloraError(_ESHAPE, where)
         if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
             raise MloraError(_EINVAL, where)
         st = self.fn(self.ref, q.data_ptr(), None if rows is None else rows.data_ptr(), listed,

@@ -85,3 +85,17 @@ def test_a_place_for_the_queries_of_another_size_is_refused():
         refused(lambda: step(q), status)
     mine = i16(M, 128)
     assert step(mine).q is mine and step(None).q.shape == (M, 128)
+
+
+def test_lists_without_entries_are_refused():
+    """Their pointer is null, which would mean all rows."""
+    c, calls = a_cache(), []
+    c.append_fn = recorder(calls)
+    new = [dev(1, 8, 3, 64, dtype=torch.bfloat16) for _ in range(2)]
+    refused(lambda: c.append(*new, 4, dev(2, 0), 8, stream=0), ESHAPE)
+    op, mass_calls = a_mass(c)
+    refused(lambda: op.run(dev(1, 8, 6, 64, dtype=torch.bfloat16), dev(2, 0), dev(1 << 16, dtype=torch.uint8), stream=0), ESHAPE)
+    assert not calls and not mass_calls
+    c.append(*new, 4, None, 8, stream=0)
+    c.append(*new, 4, dev(2, 3), 8, stream=0)
+    assert [x[4] is None for x in calls] == [True, False] and calls[1][5] == 3

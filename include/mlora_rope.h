@@ -50,7 +50,7 @@ typedef struct {
 mlora_status mlora_rope_frequencies(const mlora_rope *r, double *quarter_turns);
 
 typedef struct {
-    int32_t M;                      /* rows: 0 .. MLORA_ROPE_MAX_ROWS, a multiple of rows_per_stream */
+    int32_t M;                      /* rows: 0 .. MLORA_ROPE_MAX_ROWS, a multiple of rows_per_stream; 0: tensors may be NULL, nothing is launched */
     int32_t rows_per_stream;
     const int32_t *base;            /* device int32 [M / rows_per_stream], or NULL */
     const int32_t *offset;          /* device int32 [rows_per_stream], or NULL */

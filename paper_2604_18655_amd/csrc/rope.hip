@@ -251,7 +251,7 @@ mlora_status mlora_rope_tables(const mlora_rope *r, const mlora_rope_rows *rows,
 {
     const mlora_status st = check(r, rows);
     if (st != MLORA_OK) return st;
-    if (!cos_out || !sin_out) return MLORA_EINVAL;
+    if (rows->M > 0 && (!cos_out || !sin_out)) return MLORA_EINVAL;
     if ((reinterpret_cast<uintptr_t>(cos_out) | reinterpret_cast<uintptr_t>(sin_out)) & 3u) return MLORA_EALIGN;
     if (rows->M == 0) return MLORA_OK;
     const RopeRows a = rows_of(r, rows);
@@ -277,11 +277,11 @@ mlora_status mlora_rope_apply(const mlora_rope *r, const mlora_rope_rows *rows, 
     int units = 0;
     for (int i = 0; i < n_tensors; ++i) {
         const mlora_rope_tensor &t = tensors[i];
-        if (!t.x || !t.y) return MLORA_EINVAL;
+        if (rows->M > 0 && (!t.x || !t.y)) return MLORA_EINVAL;
         if (t.heads < 1 || t.heads > 4096) return MLORA_ESHAPE;
         if (t.x_row < 0 || t.x_head < 0 || t.y_row < 0 || t.y_head < 0) return MLORA_ESHAPE;
         if ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.y)) & (unsigned)(size - 1)) return MLORA_EALIGN;
-        if (t.x == t.y && (t.x_row != t.y_row || t.x_head != t.y_head)) return MLORA_EINVAL;
+        if (rows->M > 0 && t.x == t.y && (t.x_row != t.y_row || t.x_head != t.y_head)) return MLORA_EINVAL;
         RopeMove &m = a.t[i];
         m.x = t.x;
         m.y = t.y;

@@ -99,3 +99,15 @@ def test_lists_without_entries_are_refused():
     c.append(*new, 4, None, 8, stream=0)
     c.append(*new, 4, dev(2, 3), 8, stream=0)
     assert [x[4] is None for x in calls] == [True, False] and calls[1][5] == 3
+
+
+def test_a_rotation_of_no_rows():
+    """Tensors without elements have null pointers; nothing is launched, as the header says of M = 0."""
+    r = lib.Rope(64, 32, device="cpu")
+    r.quarter_turns = OnDevice(r.quarter_turns)
+    none = lambda *shape: dev(0, *shape, dtype=torch.float32)   # noqa: E731
+    lib.RopeTables(r, none(16), none(16), 0).run(stream=0)
+    lib.RopePlan(r, [lib.RopeTensor(none(2, 64), none(2, 64))], 0, lib.Y_FP32).run(stream=0)
+    lib.RopePlan(r, [lib.RopeTensor(none(2, 64), none(2, 64))], 0, lib.Y_FP32, rows_per_stream=4, base=dev(0), offset=dev(4)).run(stream=0)
+    rows = B._RopeRowsStruct(4, 4, None, None, 0x3000)
+    assert lib.load_library().mlora_rope_tables(r.struct, rows, None, None, None) == EINVAL

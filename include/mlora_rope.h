@@ -61,7 +61,8 @@ typedef struct {
 mlora_status mlora_rope_tables(const mlora_rope *r, const mlora_rope_rows *rows, float *cos_out, float *sin_out, void *stream);
 
 /* One tensor of a call: element (m, head, e) of x lies at m * x_row + head * x_head + e (strides in elements, not negative).  y may be
- * x itself with the same strides, and otherwise overlaps no tensor of the call.  rotate 0: the rows are copied. */
+ * x itself with the same strides, and otherwise overlaps no tensor of the call; its rows and heads do not overlap each other (x's may).
+ * rotate 0: the rows are copied. */
 typedef struct {
     const void *x;
     void *y;

@@ -282,6 +282,7 @@ mlora_status mlora_rope_apply(const mlora_rope *r, const mlora_rope_rows *rows, 
         if (t.x_row < 0 || t.x_head < 0 || t.y_row < 0 || t.y_head < 0) return MLORA_ESHAPE;
         if ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.y)) & (unsigned)(size - 1)) return MLORA_EALIGN;
         if (rows->M > 0 && t.x == t.y && (t.x_row != t.y_row || t.x_head != t.y_head)) return MLORA_EINVAL;
+        if ((rows->M > 1 && t.y_row < dim) || (rows->M > 0 && t.heads > 1 && t.y_head < dim)) return MLORA_EINVAL;
         RopeMove &m = a.t[i];
         m.x = t.x;
         m.y = t.y;

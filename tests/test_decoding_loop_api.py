@@ -188,3 +188,18 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
         lib.Rope(64, 63, device="cpu")
     meta = lambda t: t.to("meta")   # noqa: E731  (a device tensor's shape checks cannot run without a device)
     refused(lambda: lib.StreamCache(*(meta(t) for t in (k, k, f(1, 2, 3, 8), i(1, 2, 3, 8), i(2), i(2)))))
+
+
+def test_rotated_rows_or_heads_that_overlap_are_refused():
+    """y with a stride of less than a head is written by several blocks at once."""
+    cdll = lib.load_library()
+
+    def apply(M=8, heads=8, **kw):
+        f = dict(x=0x10000, y=0x20000, x_row=0, x_head=0, y_row=512, y_head=64, heads=heads, rotate=1)
+        f.update(kw)
+        rows = B._RopeRowsStruct(M, max(1, M), None, None, 0x3000)
+        return cdll.mlora_rope_apply(C.byref(rope()), C.byref(rows), (B._RopeTensorStruct * 1)(B._RopeTensorStruct(**f)), 1, 0, 0, None)
+
+    for bad in (dict(y_row=0), dict(y_row=63), dict(y_head=0), dict(y_head=63), dict(y_row=0, M=2, heads=1), dict(x=0x20000, y_row=0, x_head=64)):
+        assert apply(**bad) == EINVAL, bad
+    assert apply(M=0, y_row=0) == OK

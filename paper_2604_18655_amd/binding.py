@@ -560,19 +560,46 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS = 0, 1, 2, 3
 _EINVAL, _ESHAPE = -1, -2
 
 
-def _buffer(t, where: str, itemsize: int, shape=None, n: Optional[int] = None) -> None:
-    """Refuses what is no dense device tensor of elements of this size, of this shape or number of elements."""
-    if not t.is_cuda or t.element_size() != itemsize or not t.is_contiguous():
+class _Kind:
+    """Types that a buffer's elements may have, by name; `last` is the one that was met last."""
+
+    def __init__(self, itemsize: int, *names: str):
+        self.itemsize, self.names, self.last = itemsize, {"torch." + n for n in names}, None
+
+    def takes(self, dtype) -> bool:
+        if dtype is not self.last:
+            if str(dtype) not in self.names:
+                return False
+            self.last = dtype
+        return True
+
+
+_AS_BF16 = _Kind(2, "bfloat16", "int16", "uint16")       # (or their patterns)
+_AS_FP32, _AS_FP64 = _Kind(4, "float32"), _Kind(8, "float64")
+_AS_INT32 = _Kind(4, "int32", "uint32")
+
+
+def _buffer(t, where: str, kind: _Kind, shape=None, n: Optional[int] = None) -> None:
+    """Refuses what is no dense device tensor of elements of this kind, of this shape or number of elements."""
+    if not t.is_cuda or not kind.takes(t.dtype) or not t.is_contiguous():
         raise MloraError(_EINVAL, where)
     if (shape is not None and tuple(t.shape) != tuple(shape)) or (n is not None and t.numel() != n):
         raise MloraError(_ESHAPE, where)
 
 
-def _call_buffer(t, where: str, itemsize: int, n: int) -> None:
-    """_buffer for what changes from call to call: one look at the bytes, and the reason only if they are wrong."""
-    if t.nbytes != itemsize * n or not t.is_contiguous() or not t.is_cuda:
-        _buffer(t, where, itemsize, n=n)
-        raise MloraError(_EINVAL, where)
+def _call_buffer(t, where: str, kind: _Kind, n: int) -> None:
+    """_buffer for what changes from call to call: one look, and the reason only if something is wrong or new."""
+    if t.nbytes != kind.itemsize * n or t.dtype is not kind.last or not t.is_contiguous() or not t.is_cuda:
+        _buffer(t, where, kind, n=n)
+
+
+def _call_list(t, where: str, streams: int) -> int:
+    """Entries per stream of an int32 list [streams][n]."""
+    size = t.nbytes
+    n = size // (4 * streams)
+    if size != 4 * streams * n or t.dtype is not _AS_INT32.last or not t.is_contiguous() or not t.is_cuda:
+        _buffer(t, where, _AS_INT32, n=streams * n)
+    return n
 
 
 class Rope:
@@ -591,11 +618,11 @@ class Rope:
 
     def rows(self, M: int, rows_per_stream: Optional[int], base, offset) -> _RopeRowsStruct:
         R = int(M if rows_per_stream is None else rows_per_stream)
-        _buffer(self.quarter_turns, "rope frequencies", 8)
+        _buffer(self.quarter_turns, "rope frequencies", _AS_FP64)
         if base is not None:
-            _buffer(base, "rope base", 4, n=M // max(1, R))
+            _buffer(base, "rope base", _AS_INT32, n=M // max(1, R))
         if offset is not None:
-            _buffer(offset, "rope offset", 4, n=R)
+            _buffer(offset, "rope offset", _AS_INT32, n=R)
         return _RopeRowsStruct(int(M), max(1, R), _ptr(base), _ptr(offset), _ptr(self.quarter_turns))
 
 
@@ -604,7 +631,7 @@ class RopeTables:
 
     def __init__(self, rope: Rope, cos, sin, M: int, rows_per_stream: Optional[int] = None, base=None, offset=None):
         for t in (cos, sin):
-            _buffer(t, "mlora_rope_tables", 4, n=M * (rope.struct.rot // 2))
+            _buffer(t, "mlora_rope_tables", _AS_FP32, n=M * (rope.struct.rot // 2))
         self.keep = (rope, cos, sin, base, offset)
         self.rows = rope.rows(M, rows_per_stream, base, offset)
         self.args = (C.byref(rope.struct), C.byref(self.rows), _ptr(cos), _ptr(sin))
@@ -639,7 +666,7 @@ class RopePlan:
         for t in tensors:
             if t.x.shape[0] != M or t.x.shape[2] != rope.struct.head_dim:
                 raise MloraError(_ESHAPE, "mlora_rope_apply")
-            if t.x.element_size() != (2 if dtype == Y_BF16 else 4):
+            if not (_AS_BF16 if dtype == Y_BF16 else _AS_FP32).takes(t.x.dtype):
                 raise MloraError(_EINVAL, "mlora_rope_apply")
         self.keep = (rope, list(tensors), base, offset)
         self.rows = rope.rows(M, rows_per_stream, base, offset)
@@ -664,11 +691,11 @@ class StreamCache:
             raise MloraError(_ESHAPE, "stream cache")
         L, S, H, cap, D = (int(x) for x in k.shape)
         for t in (k, v):
-            _buffer(t, "stream cache", 2, (L, S, H, cap, D))
-        for t in (mass, slot_pos):
-            _buffer(t, "stream cache", 4, (L, S, H, cap))
+            _buffer(t, "stream cache", _AS_BF16, (L, S, H, cap, D))
+        _buffer(mass, "stream cache", _AS_FP32, (L, S, H, cap))
+        _buffer(slot_pos, "stream cache", _AS_INT32, (L, S, H, cap))
         for t in (len, next_pos):
-            _buffer(t, "stream cache", 4, (S,))
+            _buffer(t, "stream cache", _AS_INT32, (S,))
         self.k, self.v, self.mass, self.slot_pos, self.len, self.next_pos = k, v, mass, slot_pos, len, next_pos
         self.tickets = torch.zeros((S, 32), dtype=torch.int32).to(k.device)  # (an upload: done when it returns)
         self.shape = (L, S, H, cap, D)
@@ -685,14 +712,14 @@ class StreamCache:
         caches; beyond the budget they take the slots of the lowest rank."""
         where = "mlora_stream_cache_append"
         size = self.row_bytes * rows_per_stream
-        if (k_new.nbytes != size or v_new.nbytes != size or not k_new.is_contiguous() or not v_new.is_contiguous()
+        if (k_new.nbytes != size or v_new.nbytes != size or k_new.dtype is not _AS_BF16.last
+                or v_new.dtype is not _AS_BF16.last or not k_new.is_contiguous() or not v_new.is_contiguous()
                 or not k_new.is_cuda or not v_new.is_cuda):
             for t in (k_new, v_new):
-                _call_buffer(t, where, 2, size // 2)
+                _call_buffer(t, where, _AS_BF16, size // 2)
         listed = 0
         if rows is not None:
-            listed = rows.numel() // self.streams
-            _call_buffer(rows, where, 4, self.streams * listed)
+            listed = _call_list(rows, where, self.streams)
             if listed == 0:                              # (its pointer is null: all rows)
                 raise MloraError(_ESHAPE, where)
         st = self.append_fn(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
@@ -705,7 +732,7 @@ class StreamCache:
                  stream: Optional[int] = None) -> None:
         """The slots of the highest rank, at most budget, to the front of another cache; kept int32 [L][S][H][budget]
         tells which (-1 beyond)."""
-        _call_buffer(kept, "mlora_stream_cache_compress", 4, self.heads * budget)
+        _call_buffer(kept, "mlora_stream_cache_compress", _AS_INT32, self.heads * budget)
         st = self.compress_fn(self.ref, to.ref, kept.data_ptr(), budget, sink, recent,
                               _stream() if stream is None else stream)
         if st != 0:
@@ -722,10 +749,10 @@ class AttentionMass:
         P = 0
         if k_prefill is not None:
             P = int(k_prefill.shape[2]) if k_prefill.dim() == 4 else -1
-            _buffer(k_prefill, "attention mass", 2, (L, H, P, D))
+            _buffer(k_prefill, "attention mass", _AS_BF16, (L, H, P, D))
             if mass_prefill is None:
                 raise MloraError(_EINVAL, "attention mass")
-            _buffer(mass_prefill, "attention mass", 4, (L, H, P))
+            _buffer(mass_prefill, "attention mass", _AS_FP32, (L, H, P))
         self.keep = (cache, k_prefill, mass_prefill)
         self.streams, self.q_elements = S, L * S * int(rows_per_stream) * int(n_q_heads) * D
         self.struct = _AttentionMassStruct(cache.struct, int(n_q_heads), int(rows_per_stream), float(scale),
@@ -740,11 +767,10 @@ class AttentionMass:
     def run(self, q, rows, workspace, stream: Optional[int] = None) -> None:
         """q bf16 [L][S * rows_per_stream][n_q_heads][head_dim], rows int32 [S][n] or None (all)."""
         where = "mlora_attention_mass_add"
-        _call_buffer(q, where, 2, self.q_elements)
+        _call_buffer(q, where, _AS_BF16, self.q_elements)
         listed = 0
         if rows is not None:
-            listed = rows.numel() // self.streams
-            _call_buffer(rows, where, 4, self.streams * listed)
+            listed = _call_list(rows, where, self.streams)
             if listed == 0:                              # (its pointer is null: all rows)
                 raise MloraError(_ESHAPE, where)
         if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
@@ -765,22 +791,22 @@ class LogitRules:
                  mask_row=None):
         S, R, T, V = int(n_streams), int(rows_per_stream), int(tokens_per_stream), int(vocab)
         where = "logit rules"
-        _buffer(parent, where, 4, n=S * R)
+        _buffer(parent, where, _AS_INT32, n=S * R)
         if counts is not None:
-            _buffer(counts, where, 4, (S, V))
+            _buffer(counts, where, _AS_INT32, (S, V))
         for t in (repetition, frequency, presence):
             if t is not None:
-                _buffer(t, where, 4, n=S)
+                _buffer(t, where, _AS_FP32, n=S)
         if (bias is None) != (bias_row is None) or (masks is None) != (mask_row is None):
             raise MloraError(_EINVAL, where)
         if bias is not None:
-            _buffer(bias, where, 4, (bias.shape[0], V))
-            _buffer(bias_row, where, 4, n=S)
+            _buffer(bias, where, _AS_FP32, (bias.shape[0], V))
+            _buffer(bias_row, where, _AS_INT32, n=S)
         if masks is not None:
-            _buffer(masks, where, 4, (masks.shape[0], (V + 31) // 32))
-            _buffer(mask_row, where, 4, n=S * R)
+            _buffer(masks, where, _AS_INT32, (masks.shape[0], (V + 31) // 32))
+            _buffer(mask_row, where, _AS_INT32, n=S * R)
         self.keep = (parent, counts, repetition, frequency, presence, bias, bias_row, masks, mask_row)
-        self.streams, self.tokens, self.logits, self.itemsize = S, S * T, S * R * V, 2 if logits_dtype == Y_BF16 else 4
+        self.streams, self.tokens, self.logits, self.kind = S, S * T, S * R * V, _AS_BF16 if logits_dtype == Y_BF16 else _AS_FP32
         self.struct = _LogitRulesStruct(S, R, T, V, int(logits_dtype), _ptr(parent), _ptr(counts), _ptr(repetition),
                                         _ptr(frequency), _ptr(presence), _ptr(bias), _ptr(bias_row),
                                         0 if bias is None else int(bias.shape[0]), _ptr(masks), _ptr(mask_row),
@@ -791,17 +817,16 @@ class LogitRules:
     def run(self, logits, tokens, out, new_tokens=None, stream: Optional[int] = None) -> None:
         """logits [S * R][V] -> out (may be logits itself); tokens int32 [S][T]; new_tokens int32 [S][n]: counted first."""
         where = "mlora_logit_rules_apply"
-        size = self.itemsize * self.logits
-        if (logits.nbytes != size or out.nbytes != size or tokens.nbytes != 4 * self.tokens or not logits.is_contiguous()
+        kind = self.kind
+        size, dtype = kind.itemsize * self.logits, kind.last
+        if (logits.nbytes != size or out.nbytes != size or tokens.nbytes != 4 * self.tokens or logits.dtype is not dtype
+                or out.dtype is not dtype or tokens.dtype is not _AS_INT32.last or not logits.is_contiguous()
                 or not out.is_contiguous() or not tokens.is_contiguous() or not logits.is_cuda or not out.is_cuda
                 or not tokens.is_cuda):
-            _call_buffer(logits, where, self.itemsize, self.logits)
-            _call_buffer(out, where, self.itemsize, self.logits)
-            _call_buffer(tokens, where, 4, self.tokens)
-        fresh = 0
-        if new_tokens is not None:
-            fresh = new_tokens.numel() // self.streams
-            _call_buffer(new_tokens, where, 4, self.streams * fresh)
+            _call_buffer(logits, where, kind, self.logits)
+            _call_buffer(out, where, kind, self.logits)
+            _call_buffer(tokens, where, _AS_INT32, self.tokens)
+        fresh = 0 if new_tokens is None else _call_list(new_tokens, where, self.streams)
         st = self.fn(self.ref, logits.data_ptr(), tokens.data_ptr(), new_tokens.data_ptr() if fresh else None, fresh,
                      out.data_ptr(), _stream() if stream is None else stream)
         if st != 0:

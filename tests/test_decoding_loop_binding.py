@@ -111,3 +111,59 @@ def test_a_rotation_of_no_rows():
     lib.RopePlan(r, [lib.RopeTensor(none(2, 64), none(2, 64))], 0, lib.Y_FP32, rows_per_stream=4, base=dev(0), offset=dev(4)).run(stream=0)
     rows = B._RopeRowsStruct(4, 4, None, None, 0x3000)
     assert lib.load_library().mlora_rope_tables(r.struct, rows, None, None, None) == EINVAL
+
+
+def test_elements_of_another_type_of_the_same_size_are_refused():
+    bf16, f32, i32, f16, i16 = torch.bfloat16, torch.float32, torch.int32, torch.float16, torch.int16
+    on = lambda shape, dtype: dev(*shape, dtype=dtype)   # noqa: E731
+    for kw in (dict(k=f16), dict(v=f16), dict(mass=i32), dict(slot_pos=f32), dict(len=f32), dict(next_pos=f32)):
+        (name, dtype), shapes = next(iter(kw.items())), dict(k=(1, 2, 3, 8, 64), v=(1, 2, 3, 8, 64), mass=(1, 2, 3, 8), slot_pos=(1, 2, 3, 8), len=(2,), next_pos=(2,))
+        refused(lambda: a_cache(**{name: on(shapes[name], dtype)}))
+    a_cache(k=on((1, 2, 3, 8, 64), i16))
+    c, calls = a_cache(), []
+    c.append_fn = c.compress_fn = recorder(calls)
+    new = on((1, 8, 3, 64), bf16)
+    refused(lambda: c.append(new, on((1, 8, 3, 64), f16), 4, None, 8, stream=0))
+    refused(lambda: c.append(on((1, 8, 3, 64), f16), new, 4, None, 8, stream=0))
+    refused(lambda: c.append(new, new, 4, on((2, 3), f32), 8, stream=0))
+    refused(lambda: c.append(new, new, 4, on((2, 3), torch.int64), 8, stream=0))
+    refused(lambda: c.append(new, new, 4, on((7,), i32), 8, stream=0), ESHAPE)
+    refused(lambda: c.compress(a_cache(), on((1, 2, 3, 5), f32), 5, stream=0))
+    ws = on((1 << 16,), torch.uint8)
+    op, mass_calls = a_mass(c)
+    refused(lambda: op.run(on((1, 8, 6, 64), f16), None, ws, stream=0))
+    refused(lambda: op.run(on((1, 8, 6, 64), bf16), on((2, 3), f32), ws, stream=0))
+    refused(lambda: a_mass(c, k_prefill=on((1, 3, 9, 64), f16), mass_prefill=on((1, 3, 9), f32)))
+    refused(lambda: a_mass(c, k_prefill=on((1, 3, 9, 64), bf16), mass_prefill=on((1, 3, 9), i32)))
+    assert not calls and not mass_calls
+    c.append(on((1, 8, 3, 64), i16), new, 4, on((2, 3), i32), 8, stream=0)
+    op.run(on((1, 8, 6, 64), i16), None, ws, stream=0)
+    assert len(calls) == 1 and calls[0][5] == 3 and len(mass_calls) == 1
+
+    r = lib.Rope(64, 64, device="cpu")
+    r.quarter_turns = OnDevice(r.quarter_turns)
+    table, x = on((4, 32), f32), on((4, 2, 64), f16)
+    refused(lambda: lib.RopeTables(r, table, on((4, 32), i32), 4))
+    refused(lambda: lib.RopeTables(r, table, table, 4, base=on((1,), f32)))
+    refused(lambda: lib.RopeTables(r, table, table, 4, offset=on((4,), f32)))
+    refused(lambda: lib.RopePlan(r, [lib.RopeTensor(x, x)], 4, lib.Y_BF16))
+    refused(lambda: lib.RopePlan(r, [lib.RopeTensor(on((4, 2, 64), i32), on((4, 2, 64), i32))], 4, lib.Y_FP32))
+    lib.RopePlan(r, [lib.RopeTensor(on((4, 2, 64), bf16), on((4, 2, 64), bf16))], 4, lib.Y_BF16)
+
+    given = dict(counts=on((2, 40), i32), repetition=on((2,), f32), bias=on((1, 40), f32), bias_row=on((2,), i32), masks=on((1, 2), i32), mask_row=on((6,), i32))
+    other = dict(counts=f32, repetition=i32, bias=i32, bias_row=f32, masks=f32, mask_row=f32)
+    rules = lambda y=lib.Y_BF16, **kw: lib.LogitRules(2, 3, 2, 40, y, on((6,), i32), **dict(given, **kw))   # noqa: E731
+    for name, dtype in other.items():
+        refused(lambda: rules(**{name: on(tuple(given[name].shape), dtype)}))
+    op, calls = rules(), []
+    op.fn = recorder(calls)
+    z, tokens = on((6, 40), bf16), on((2, 2), i32)
+    for args in ((on((6, 40), f16), tokens, z), (z, tokens, on((6, 40), f16)), (z, on((2, 2), f32), z), (z, on((2, 1), torch.int64), z),
+                 (z, tokens, z, on((2, 3), f32))):
+        refused(lambda: op.run(*args, stream=0))
+    assert not calls
+    op.run(z, tokens, z, on((2, 3), i32), stream=0)
+    op.run(z, tokens, z, on((2, 0), i32), stream=0)
+    assert [x[4] for x in calls] == [3, 0]
+    op = rules(lib.Y_FP32)
+    refused(lambda: op.run(on((6, 40), i32), tokens, on((6, 40), i32), stream=0))

@@ -31,6 +31,8 @@ class DecodingLoop:
         arguments of binding.LogitRules (counts and parent are made here).  Stream caches have room for `budget` slots."""
         L, S, m = len(layers), int(n_streams), int(forecast.shape[0])
         self.T, self.R = B.ds2d_rows(branch, m)
+        if budget < m + 1 or sink < 0 or recent < 0:     # (a step appends up to m + 1 rows)
+            raise B.MloraError(B._ESHAPE, "decoding loop")
         parent, is_forecast, _ = B.ds2d_layout(branch, m)
         M, V, hidden = S * self.R, head.N, head.K
         kv, heads = layers[0][1].N // HEAD_DIM, layers[0][0].N // HEAD_DIM

@@ -167,3 +167,22 @@ def test_elements_of_another_type_of_the_same_size_are_refused():
     assert [x[4] for x in calls] == [3, 0]
     op = rules(lib.Y_FP32)
     refused(lambda: op.run(on((6, 40), i32), tokens, on((6, 40), i32), stream=0))
+
+
+def loop_of(**kw):
+    """Arguments that fit each other, but for what the caller changes.  Nothing here is on a device."""
+    from paper_2604_18655_amd.decoding import DecodingLoop
+    bits = lambda *shape: torch.zeros(shape, dtype=torch.int16)   # noqa: E731
+    sizes = dict(q=(128, 256), k=(128, 64), v=(128, 64), o=(256, 128), gate_up=(128, 512), down=(256, 128), head=(128, 300))
+    second = {n[1:]: kw.pop(n) for n in list(kw) if n.startswith("_")}
+    proj = lambda n, over=(): lib.Proj(*dict(sizes, **dict(over))[n], 32, None)   # noqa: E731
+    layers = [[proj(n) for n in list(sizes)[:6]], [proj(n, second) for n in list(sizes)[:6]]]
+    args = dict(layers=layers, head=proj("head", {k: kw.pop(k) for k in ("head",) if k in kw}), embedding=bits(300, 128), forecast=bits(2, 128), n_streams=3,
+                branch=(3, 2), budget=24)
+    args.update(kw)
+    return DecodingLoop(**args)
+
+
+@pytest.mark.parametrize("bad", [dict(budget=2), dict(sink=-1), dict(recent=-1)])
+def test_a_budget_below_a_step_is_refused(bad):
+    refused(lambda: loop_of(**bad), ESHAPE)

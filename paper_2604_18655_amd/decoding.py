@@ -22,6 +22,22 @@ from .decoder import DecoderLayerStep
 HEAD_DIM = 64                                            # the fused projections turn heads of 64 features
 
 
+def _fitting(layers, head, embedding, forecast, k_prefill, v_prefill) -> None:
+    """Refuses parts of a loop that do not fit each other: what a call writes or reads has the size of another part's."""
+    hidden, wide, narrow = head.K, 0, 0
+    ok = len(layers) > 0 and embedding.dim() == 2 and forecast.dim() == 2
+    ok = ok and embedding.shape[0] >= head.N and embedding.shape[1] == forecast.shape[1] == hidden
+    for q, k, v, o, gate_up, down in layers:
+        wide, narrow = wide or q.N, narrow or k.N
+        ok = ok and q.K == k.K == v.K == gate_up.K == o.N == down.N == hidden and q.N == o.K == wide and k.N == v.N == narrow
+        ok = ok and wide % HEAD_DIM == narrow % HEAD_DIM == 0 and gate_up.N == 2 * down.K
+    ok = ok and (k_prefill is None) == (v_prefill is None)
+    if not ok:
+        raise B.MloraError(B._ESHAPE, "decoding loop")
+    for t in () if k_prefill is None else (k_prefill, v_prefill):
+        B._buffer(t, "decoding loop", B._AS_BF16, (len(layers), narrow // HEAD_DIM, k_prefill.shape[2] if k_prefill.dim() == 4 else -1, HEAD_DIM))
+
+
 class DecodingLoop:
     def __init__(self, layers: Sequence[Sequence[B.Proj]], head: B.Proj, embedding, forecast, n_streams: int, branch: Sequence[int],
                  budget: int, sink: int = 4, recent: int = 32, decay: float = 1.0, rope: Optional[B.Rope] = None, k_prefill=None,
@@ -31,6 +47,9 @@ class DecodingLoop:
         arguments of binding.LogitRules (counts and parent are made here).  Stream caches have room for `budget` slots."""
         L, S, m = len(layers), int(n_streams), int(forecast.shape[0])
         self.T, self.R = B.ds2d_rows(branch, m)
+        _fitting(layers, head, embedding, forecast, k_prefill, v_prefill)
+        if row_adapter is not None:
+            B._buffer(row_adapter, "decoding loop", B._AS_INT32, n=S * self.R)
         if budget < m + 1 or sink < 0 or recent < 0:     # (a step appends up to m + 1 rows)
             raise B.MloraError(B._ESHAPE, "decoding loop")
         parent, is_forecast, _ = B.ds2d_layout(branch, m)

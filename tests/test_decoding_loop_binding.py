@@ -186,3 +186,26 @@ def loop_of(**kw):
 @pytest.mark.parametrize("bad", [dict(budget=2), dict(sink=-1), dict(recent=-1)])
 def test_a_budget_below_a_step_is_refused(bad):
     refused(lambda: loop_of(**bad), ESHAPE)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(layers=[]),
+    dict(_q=(128, 320)), dict(_k=(128, 128)), dict(_v=(128, 128)), dict(_o=(256, 256)), dict(_o=(128, 128)), dict(_gate_up=(128, 1024)), dict(_down=(256, 256)),
+    dict(_q=(256, 256)), dict(head=(256, 300)), dict(head=(128, 301)),
+    dict(embedding=torch.zeros((300, 64), dtype=torch.int16)), dict(forecast=torch.zeros((2, 64), dtype=torch.int16)),
+    dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16)), dict(v_prefill=dev(2, 1, 9, 64, dtype=torch.int16)),
+    dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=dev(2, 1, 8, 64, dtype=torch.int16)),
+    dict(k_prefill=dev(1, 1, 9, 64, dtype=torch.int16), v_prefill=dev(1, 1, 9, 64, dtype=torch.int16)),
+    dict(row_adapter=dev(3)),
+])
+def test_parts_of_a_loop_that_do_not_fit_are_refused(bad):
+    refused(lambda: loop_of(**bad), ESHAPE)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(row_adapter=torch.zeros(90, dtype=torch.int32)), dict(row_adapter=dev(90, dtype=torch.float32)),
+    dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=torch.zeros((2, 1, 9, 64), dtype=torch.int16)),
+    dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=dev(2, 1, 9, 64, dtype=torch.float16)),
+])
+def test_parts_of_a_loop_in_other_memory_or_of_other_types_are_refused(bad):
+    refused(lambda: loop_of(**bad))

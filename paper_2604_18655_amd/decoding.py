@@ -38,15 +38,23 @@ def _fitting(layers, head, embedding, forecast, k_prefill, v_prefill) -> None:
         B._buffer(t, "decoding loop", B._AS_BF16, (len(layers), narrow // HEAD_DIM, k_prefill.shape[2] if k_prefill.dim() == 4 else -1, HEAD_DIM))
 
 
+def _patterns(t):
+    """A bf16 tensor as the int16 patterns of its numbers (which it may be already)."""
+    if not B._AS_BF16.takes(t.dtype):
+        raise B.MloraError(B._EINVAL, "decoding loop")
+    return t.view(torch.int16)
+
+
 class DecodingLoop:
     def __init__(self, layers: Sequence[Sequence[B.Proj]], head: B.Proj, embedding, forecast, n_streams: int, branch: Sequence[int],
                  budget: int, sink: int = 4, recent: int = 32, decay: float = 1.0, rope: Optional[B.Rope] = None, k_prefill=None,
                  v_prefill=None, row_adapter=None, rules: Optional[dict] = None, device="cuda:0"):
         """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary; embedding bf16 [V][hidden] and forecast
-        bf16 [m][hidden] as int16 patterns; k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams; rules: keyword
+        bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams; rules: keyword
         arguments of binding.LogitRules (counts and parent are made here).  Stream caches have room for `budget` slots."""
         L, S, m = len(layers), int(n_streams), int(forecast.shape[0])
         self.T, self.R = B.ds2d_rows(branch, m)
+        embedding, forecast = _patterns(embedding), _patterns(forecast)
         _fitting(layers, head, embedding, forecast, k_prefill, v_prefill)
         if row_adapter is not None:
             B._buffer(row_adapter, "decoding loop", B._AS_INT32, n=S * self.R)

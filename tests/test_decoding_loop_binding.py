@@ -203,7 +203,7 @@ def test_parts_of_a_loop_that_do_not_fit_are_refused(bad):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(row_adapter=torch.zeros(90, dtype=torch.int32)), dict(row_adapter=dev(90, dtype=torch.float32)),
+    dict(embedding=torch.zeros((300, 128), dtype=torch.float16)), dict(forecast=torch.zeros((2, 128))), dict(row_adapter=torch.zeros(90, dtype=torch.int32)), dict(row_adapter=dev(90, dtype=torch.float32)),
     dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=torch.zeros((2, 1, 9, 64), dtype=torch.int16)),
     dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=dev(2, 1, 9, 64, dtype=torch.float16)),
 ])

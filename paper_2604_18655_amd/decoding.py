@@ -56,6 +56,8 @@ class DecodingLoop:
         self.T, self.R = B.ds2d_rows(branch, m)
         embedding, forecast = _patterns(embedding), _patterns(forecast)
         _fitting(layers, head, embedding, forecast, k_prefill, v_prefill)
+        if rope is not None and (rope.struct.head_dim, rope.struct.rot, rope.struct.layout) != (HEAD_DIM, HEAD_DIM, B.ROPE_HALF):
+            raise B.MloraError(B._ESHAPE, "decoding loop")          # (what the fused projections turn)
         if row_adapter is not None:
             B._buffer(row_adapter, "decoding loop", B._AS_INT32, n=S * self.R)
         if budget < m + 1 or sink < 0 or recent < 0:     # (a step appends up to m + 1 rows)

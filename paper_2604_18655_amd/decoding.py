@@ -118,7 +118,8 @@ class DecodingLoop:
                              torch.zeros(shape, device=device), i32(shape), i32((self.S,)), i32((self.S,)))
 
     def start(self, tokens, counts=None) -> None:
-        """tokens int32 [S]: every stream's newest token, the root of its first tree (which has no drafts yet)."""
+        """tokens int32 [S]: every stream's newest token, the root of its first tree (which has no drafts yet); one outside the
+        vocabulary is embedded as the nearest."""
         self.tokens.fill_(-1)
         self.tokens[:, 0] = tokens
         self.emitted.fill_(-1)
@@ -153,7 +154,7 @@ class DecodingLoop:
     def step(self) -> None:
         """One step of all streams: emitted (int32 [S][m + 1], -1 beyond) holds the tokens given out, tokens the next tree."""
         S, T, hidden = self.S, self.T, self.h.shape[1]
-        rows = torch.index_select(self.embedding, 0, self.tokens.view(-1).clamp(min=0))
+        rows = torch.index_select(self.embedding, 0, self.tokens.view(-1).clamp(0, self.embedding.shape[0] - 1))
         self.h.view(S, self.R, hidden)[:, :T].copy_(rows.view(S, T, hidden))
         self.tables.run()
         for layer in self.layers:

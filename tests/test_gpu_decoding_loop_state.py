@@ -42,3 +42,14 @@ def test_tables_and_prefix_in_bfloat16(gpu, monkeypatch):
     torch.cuda.synchronize()
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_tokens_outside_the_vocabulary(gpu, monkeypatch):
+    """They are embedded as the nearest token; a place without a draft (-1) as the first."""
+    lib, device, torch = gpu
+    loop, _, _ = make_loop(gpu, monkeypatch, 10, 40)
+    loop.start(torch.tensor([T.V, 1 << 30, -5], dtype=torch.int32).cuda())
+    rows = loop.embedding[[T.V - 1, T.V - 1, 0]].clone()
+    loop.step()
+    torch.cuda.synchronize()
+    assert torch.equal(loop.h.view(S, 30, -1)[:, 0], rows.view(torch.int16))

@@ -750,9 +750,10 @@ class AttentionMass:
         if k_prefill is not None:
             P = int(k_prefill.shape[2]) if k_prefill.dim() == 4 else -1
             _buffer(k_prefill, "attention mass", _AS_BF16, (L, H, P, D))
-            if mass_prefill is None:
+            if P > 0 and mass_prefill is None:
                 raise MloraError(_EINVAL, "attention mass")
-            _buffer(mass_prefill, "attention mass", _AS_FP32, (L, H, P))
+            if mass_prefill is not None:
+                _buffer(mass_prefill, "attention mass", _AS_FP32, (L, H, P))
         self.keep = (cache, k_prefill, mass_prefill)
         self.streams, self.q_elements = S, L * S * int(rows_per_stream) * int(n_q_heads) * D
         self.struct = _AttentionMassStruct(cache.struct, int(n_q_heads), int(rows_per_stream), float(scale),

@@ -113,6 +113,17 @@ def test_a_rotation_of_no_rows():
     assert lib.load_library().mlora_rope_tables(r.struct, rows, None, None, None) == EINVAL
 
 
+def test_a_prefix_of_no_tokens():
+    """It needs no masses, as the header says of len 0."""
+    none = dev(1, 3, 0, 64, dtype=torch.bfloat16)
+    for kw in (dict(k_prefill=none), dict(k_prefill=none, mass_prefill=dev(1, 3, 0, dtype=torch.float32)), dict()):
+        op, calls = a_mass(**kw)
+        op.run(dev(1, 8, 6, 64, dtype=torch.bfloat16), None, dev(1 << 16, dtype=torch.uint8), stream=0)
+        assert len(calls) == 1 and op.struct.len_prefill == 0
+    refused(lambda: a_mass(k_prefill=dev(1, 3, 2, 64, dtype=torch.bfloat16)))
+    refused(lambda: a_mass(k_prefill=none, mass_prefill=dev(1, 3, 1, dtype=torch.float32)), ESHAPE)
+
+
 def test_elements_of_another_type_of_the_same_size_are_refused():
     bf16, f32, i32, f16, i16 = torch.bfloat16, torch.float32, torch.int32, torch.float16, torch.int16
     on = lambda shape, dtype: dev(*shape, dtype=dtype)   # noqa: E731

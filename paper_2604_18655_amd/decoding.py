@@ -50,7 +50,9 @@ class DecodingLoop:
                  budget: int, sink: int = 4, recent: int = 32, decay: float = 1.0, rope: Optional[B.Rope] = None, k_prefill=None,
                  v_prefill=None, row_adapter=None, rules: Optional[dict] = None, device="cuda:0"):
         """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary; embedding bf16 [V][hidden] and forecast
-        bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams; rules: keyword
+        bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams,
+        keys turned by their positions 0 .. P - 1.  A stream's own positions (next_pos and slot_pos of its cache, sink) count from its
+        first token, which is turned as the one at position P.  rules: keyword
         arguments of binding.LogitRules (counts and parent are made here).  Stream caches have room for `budget` slots."""
         L, S, m = len(layers), int(n_streams), int(forecast.shape[0])
         self.T, self.R = B.ds2d_rows(branch, m)
@@ -75,11 +77,13 @@ class DecodingLoop:
         P = 0 if k_prefill is None else int(k_prefill.shape[2])
         self.mass_prefill = torch.zeros((L, kv, P), device=device) if P else None
 
-        # rows: the tree's tokens, then their forecast embeddings; a row stands one position behind the one it continues
+        # rows: the tree's tokens, then their forecast embeddings; a row stands one position behind the one it continues, and a
+        # stream's first token behind the P of the prefix
         depth = []
         for up in parent:
             depth.append(0 if up < 0 else depth[up] + 1)
-        self.offset = torch.tensor(depth, dtype=torch.int32).to(device)
+        self.prefix = P
+        self.offset = torch.tensor([P + d for d in depth], dtype=torch.int32).to(device)
         self.parent = torch.tensor(parent * S, dtype=torch.int32).to(device)
         self.is_forecast = torch.tensor(is_forecast * S, dtype=torch.uint8).to(device)
         self.cos, self.sin = (torch.empty((M, HEAD_DIM // 2), device=device) for _ in range(2))
@@ -135,11 +139,11 @@ class DecodingLoop:
         N, device = int(k.shape[2]), k.device
         long = self._cache(N, device)
         turned = torch.empty((self.L, self.S, window) + tuple(q.shape[3:]), dtype=q.dtype, device=device)
-        at = torch.tensor([N - window], dtype=torch.int32).to(device)
+        first, at = (torch.tensor([self.prefix + n], dtype=torch.int32).to(device) for n in (0, N - window))
         for l in range(self.L):
             for s in range(self.S):
                 B.RopePlan(self.rope, [B.RopeTensor(k[l, s], long.k[l, s].transpose(0, 1)),
-                                       B.RopeTensor(v[l, s], long.v[l, s].transpose(0, 1), rotate=False)], N, B.Y_BF16).run()
+                                       B.RopeTensor(v[l, s], long.v[l, s].transpose(0, 1), rotate=False)], N, B.Y_BF16, base=first).run()
                 B.RopePlan(self.rope, [B.RopeTensor(q[l, s, N - window:], turned[l, s])], window, B.Y_BF16, base=at).run()
         long.slot_pos.copy_(torch.arange(N, dtype=torch.int32, device=device).expand(long.slot_pos.shape))
         long.len.fill_(N)

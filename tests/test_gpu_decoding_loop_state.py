@@ -27,6 +27,48 @@ def angles(positions):
     return D.rope_angles(positions, 64, "turns", 500000.0, **SCALING)
 
 
+@pytest.mark.parametrize("P", [40, 0])
+def test_rows_stand_behind_the_prefix(gpu, monkeypatch, P):
+    """The first token of a stream stands at position P: the prefix holds 0 .. P - 1."""
+    lib, device, torch = gpu
+    loop, _, _ = make_loop(gpu, monkeypatch, 4, P)
+    depth = []
+    for up in loop.parent.tolist()[:30]:
+        depth.append(0 if up < 0 else depth[up] + 1)
+    given = np.zeros(S, np.int64)
+    for _ in range(4):
+        loop.step()
+        torch.cuda.synchronize()
+        want = angles((P + given[:, None] + np.asarray(depth)[None, :]).reshape(-1))
+        assert np.abs(loop.cos.cpu().numpy() - np.cos(want)).max() <= 4 * 2.0 ** -24
+        assert np.abs(loop.sin.cpu().numpy() - np.sin(want)).max() <= 4 * 2.0 ** -24
+        given += (loop.emitted >= 0).sum(1).cpu().numpy()
+
+
+@pytest.mark.parametrize("P", [40, 0])
+def test_a_prompts_keys_stand_behind_the_prefix(gpu, monkeypatch, P):
+    """Turned by their places in one sequence of prefix and prompt; bf16's half step.  Steps go on behind them."""
+    lib, device, torch = gpu
+    loop, _, bits = make_loop(gpu, monkeypatch, 5, P)
+    N = 70
+    k = bits(L, S, N, KV, 64)
+    kept = loop.prompt(bits(L, S, N, HEADS, 64), k, bits(L, S, N, KV, 64), 16).cpu().numpy()
+    torch.cuda.synchronize()
+    place, cache_k = angles(P + np.arange(N)), wide(loop.cache.k)
+    for l in range(L):
+        for s in range(S):
+            turned = D.rope(wide(k[l, s]), place, 64, False)
+            for h in range(KV):
+                want = turned[kept[l, s, h], h]
+                assert np.all(np.abs(cache_k[l, s, h] - want) <= np.abs(want) * 2.0 ** -8 + 2.0 ** -20)
+    # the first two of the stream's own slots and its newest five are protected
+    assert np.all(kept[..., -5:] == np.arange(N - 5, N)) and np.all(kept[..., :2] == [0, 1])
+    loop.start(torch.tensor([1, 2, 3], dtype=torch.int32).cuda())
+    loop.step()
+    torch.cuda.synchronize()
+    assert np.abs(loop.cos.cpu().numpy().reshape(S, 30, 32)[:, 0] - np.cos(angles(np.full(S, P + N)))).max() <= 4 * 2.0 ** -24
+
+
 def test_tables_and_prefix_in_bfloat16(gpu, monkeypatch):
     """The same numbers handed in as bfloat16 and as their patterns."""
     lib, device, torch = gpu

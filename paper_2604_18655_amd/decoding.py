@@ -135,7 +135,7 @@ class DecodingLoop:
 
     def prompt(self, q, k, v, window: int) -> torch.Tensor:
         """Every stream's own prompt of N tokens, not yet turned: q bf16 [L][S][N][heads][64], k and v [L][S][N][kv][64].  Its last
-        `window` rows weigh the slots, the heaviest of which stay.  Returns the slots that were kept, [L][S][kv][budget]."""
+        `window` rows weigh what they see, the prefix and the slots, the heaviest of which stay.  Returns the slots that were kept, [L][S][kv][budget]."""
         N, device = int(k.shape[2]), k.device
         long = self._cache(N, device)
         turned = torch.empty((self.L, self.S, window) + tuple(q.shape[3:]), dtype=q.dtype, device=device)
@@ -148,7 +148,7 @@ class DecodingLoop:
         long.slot_pos.copy_(torch.arange(N, dtype=torch.int32, device=device).expand(long.slot_pos.shape))
         long.len.fill_(N)
         long.next_pos.fill_(N)
-        weigh = B.AttentionMass(long, self.heads, window, self.scale, decay=self.decay)
+        weigh = B.AttentionMass(long, self.heads, window, self.scale, k_prefill=self.keep[0], mass_prefill=self.mass_prefill, decay=self.decay)
         ws = torch.empty(max(256, weigh.workspace_bytes()), dtype=torch.uint8, device=device)
         weigh.run(turned.view(self.L, self.S * window, self.heads, HEAD_DIM), None, ws)
         kept = torch.empty((self.L, self.S, self.kv, self.budget), dtype=torch.int32, device=device)

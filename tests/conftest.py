@@ -17,8 +17,8 @@ def pytest_configure(config):
 # Tests that hold a wrong value, and which: they run, and are expected to fail there.
 WRONG_VALUES = {
     "test_gpu_decoding_loop.py::test_a_prompt_enters_compressed":
-        "a prompt behind a shared prefix of 40 tokens is held to positions from 0, where the prefix's own keys stand "
-        "(tests/test_gpu_decoding_loop_state.py has the prefix and the prompt as one sequence)",
+        "a prompt behind a shared prefix of 40 tokens is held to positions from 0, where the prefix's own keys stand, and to "
+        "weights that leave the prefix out (tests/test_gpu_decoding_loop_state.py has the two as one sequence)",
 }
 
 

@@ -69,6 +69,40 @@ def test_a_prompts_keys_stand_behind_the_prefix(gpu, monkeypatch, P):
     assert np.abs(loop.cos.cpu().numpy().reshape(S, 30, 32)[:, 0] - np.cos(angles(np.full(S, P + N)))).max() <= 4 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("P", [40, 0])
+def test_a_prompt_beside_the_prefix_is_one_sequence(gpu, monkeypatch, P):
+    """A row's weights run over the prefix and the prompt, taken as one sequence of P + N tokens.  Bounds: keys and queries are rounded
+    to bf16 (half a step each), a weight is off by twice a score's error."""
+    lib, device, torch = gpu
+    loop, _, bits = make_loop(gpu, monkeypatch, 5, P)
+    N, window = 70, 16
+    q, k, v = bits(L, S, N, HEADS, 64), bits(L, S, N, KV, 64), bits(L, S, N, KV, 64)
+    kept = loop.prompt(q, k, v, window).cpu().numpy()
+    torch.cuda.synchronize()
+    place, mass = angles(P + np.arange(N)), loop.cache.mass.cpu().numpy()
+    prefix = wide(loop.keep[0]) if P else np.zeros((L, KV, 0, 64))
+    shared = np.zeros((L, KV, P))
+    norm = lambda a: np.sqrt((a ** 2).sum(-1)).max() if a.size else 0.0   # noqa: E731
+    most = 0.0
+    for l in range(L):
+        for s in range(S):
+            turned, tq = D.rope(wide(k[l, s]), place, 64, False), D.rope(wide(q[l, s]), place, 64, False)
+            far = 2 * (2 * 2.0 ** -8) * loop.scale * max(norm(turned), norm(prefix)) * norm(tq)
+            most = max(most, far)
+            for h in range(KV):
+                whole, got = np.concatenate([prefix[l, h], turned[:, h]]), np.zeros(P + N)
+                for r in range(N - window, N):
+                    for g in range(HEADS // KV):
+                        x = whole[:P + r + 1] @ tq[r, h * (HEADS // KV) + g] * loop.scale
+                        e = np.exp(x - x.max())
+                        got[:P + r + 1] += e / e.sum()
+                shared[l, h] += got[:P]
+                at = P + kept[l, s, h]
+                assert np.all(np.abs(mass[l, s, h] - got[at]) <= got[at] * (np.exp(far) - 1) + 1e-6)
+    if P:
+        assert np.all(np.abs(loop.mass_prefill.cpu().numpy() - shared) <= shared * (np.exp(most) - 1) + 1e-6)
+
+
 def test_tables_and_prefix_in_bfloat16(gpu, monkeypatch):
     """The same numbers handed in as bfloat16 and as their patterns."""
     lib, device, torch = gpu

@@ -49,7 +49,8 @@ class DecodingLoop:
     def __init__(self, layers: Sequence[Sequence[B.Proj]], head: B.Proj, embedding, forecast, n_streams: int, branch: Sequence[int],
                  budget: int, sink: int = 4, recent: int = 32, decay: float = 1.0, rope: Optional[B.Rope] = None, k_prefill=None,
                  v_prefill=None, row_adapter=None, rules: Optional[dict] = None, device="cuda:0"):
-        """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary; embedding bf16 [V][hidden] and forecast
+        """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary, the last normalisation's
+        weight folded in; embedding bf16 [V][hidden] and forecast
         bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams,
         keys turned by their positions 0 .. P - 1.  A stream's own positions (next_pos and slot_pos of its cache, sink) count from its
         first token, which is turned as the one at position P.  rules: keyword
@@ -104,6 +105,9 @@ class DecodingLoop:
         self.head, self.final, self.row_adapter = head, h, row_adapter
         self.head_ws = torch.zeros(max(256, B.workspace_bytes([head], M)), dtype=torch.uint8, device=device)
         self.logits = i16(M, V)
+        # (the last normalisation: 1 / rms from the sums of squares that the last layer leaves, as between the layers)
+        self.to_logits = B.LayerPlanFused([head], [B.Epilogue(sq_in=sq, sq_parts=(hidden + 63) // 64, sq_eps=self.layers[-1].eps)], [h], [self.logits],
+                                          row_adapter, M, B.Y_BF16, self.head_ws)
 
         self.counts = i32(S, V)
         self.rules = B.LogitRules(S, self.R, self.T, V, B.Y_BF16, self.parent, counts=self.counts, **(rules or {}))
@@ -163,7 +167,7 @@ class DecodingLoop:
         self.tables.run()
         for layer in self.layers:
             layer.run()
-        B.linear(self.head, self.final, self.row_adapter, self.M, self.logits, B.Y_BF16, self.head_ws)
+        self.to_logits.run()
         self.rules.run(self.logits, self.tokens, self.logits, new_tokens=self.emitted)
         self.ds2d.run(self.logits, self.tokens, self.n_accepted, self.accepted_rows, self.emitted, self.next_tokens, self.ds2d_ws)
         self.cache.append(self.k_new, self.v_new, self.R, self.accepted_rows, self.budget, self.sink, self.recent)

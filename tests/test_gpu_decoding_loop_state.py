@@ -103,6 +103,28 @@ def test_a_prompt_beside_the_prefix_is_one_sequence(gpu, monkeypatch, P):
         assert np.all(np.abs(loop.mass_prefill.cpu().numpy() - shared) <= shared * (np.exp(most) - 1) + 1e-6)
 
 
+def test_the_head_takes_normalised_rows(gpu, monkeypatch):
+    """Logits before the rules: the head's product on the last layer's rows times 1 / rms.  Bound: bf16's half step, and both
+    products' sums in fp32 (2^-12 of the row's largest covers 128 products and their roundings)."""
+    lib, device, torch = gpu
+    loop, _, _ = make_loop(gpu, monkeypatch, 7, 40)
+    seen, run_rules = {}, loop.rules.run
+
+    def keep_logits(z, tokens, out, new_tokens=None):
+        seen["logits"] = wide(z)
+        run_rules(z, tokens, out, new_tokens=new_tokens)
+
+    loop.rules.run = keep_logits
+    for _ in range(3):
+        loop.step()
+        torch.cuda.synchronize()
+        plain = torch.empty((loop.M, T.V), device="cuda")
+        lib.linear(loop.head, loop.final, loop.row_adapter, loop.M, plain, lib.Y_FP32, loop.head_ws)
+        rows = wide(loop.final)
+        want = plain.cpu().numpy().astype(np.float64) / np.sqrt((rows ** 2).mean(1) + 1e-5)[:, None]
+        assert np.all(np.abs(seen["logits"] - want) <= np.abs(want) * 2.0 ** -8 + np.abs(want).max(1, keepdims=True) * 2.0 ** -12)
+
+
 def test_tables_and_prefix_in_bfloat16(gpu, monkeypatch):
     """The same numbers handed in as bfloat16 and as their patterns."""
     lib, device, torch = gpu

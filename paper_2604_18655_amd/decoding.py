@@ -118,6 +118,7 @@ class DecodingLoop:
         self.mass = B.AttentionMass(self.cache, heads, self.R, self.scale, k_prefill=k_prefill, mass_prefill=self.mass_prefill, decay=decay)
         self.mass_ws = torch.empty(max(256, self.mass.workspace_bytes(m + 1)), dtype=torch.uint8, device=device)
         self.keep = (k_prefill, v_prefill)
+        self.prompted = False                            # the caches hold a prompt that no generation has started on
 
     def _cache(self, cap: int, device) -> B.StreamCache:
         shape = (self.L, self.S, self.kv, cap)
@@ -125,9 +126,21 @@ class DecodingLoop:
         return B.StreamCache(*(torch.zeros(shape + (HEAD_DIM,), dtype=torch.int16, device=device) for _ in range(2)),
                              torch.zeros(shape, device=device), i32(shape), i32((self.S,)), i32((self.S,)))
 
+    def reset(self) -> None:
+        """Empties the caches and forgets the prefix's masses: the next token is a stream's first."""
+        self.cache.len.zero_()
+        self.cache.next_pos.zero_()
+        if self.mass_prefill is not None:
+            self.mass_prefill.zero_()
+        self.prompted = False
+
     def start(self, tokens, counts=None) -> None:
-        """tokens int32 [S]: every stream's newest token, the root of its first tree (which has no drafts yet); one outside the
+        """A new generation, behind the prompt if there has been one since the last start and otherwise on empty caches.
+        tokens int32 [S]: every stream's newest token, the root of its first tree (which has no drafts yet); one outside the
         vocabulary is embedded as the nearest."""
+        if not self.prompted:
+            self.reset()
+        self.prompted = False
         self.tokens.fill_(-1)
         self.tokens[:, 0] = tokens
         self.emitted.fill_(-1)
@@ -141,6 +154,7 @@ class DecodingLoop:
         """Every stream's own prompt of N tokens, not yet turned: q bf16 [L][S][N][heads][64], k and v [L][S][N][kv][64].  Its last
         `window` rows weigh what they see, the prefix and the slots, the heaviest of which stay.  Returns the slots that were kept, [L][S][kv][budget]."""
         N, device = int(k.shape[2]), k.device
+        self.reset()
         long = self._cache(N, device)
         turned = torch.empty((self.L, self.S, window) + tuple(q.shape[3:]), dtype=q.dtype, device=device)
         first, at = (torch.tensor([self.prefix + n], dtype=torch.int32).to(device) for n in (0, N - window))
@@ -157,6 +171,7 @@ class DecodingLoop:
         weigh.run(turned.view(self.L, self.S * window, self.heads, HEAD_DIM), None, ws)
         kept = torch.empty((self.L, self.S, self.kv, self.budget), dtype=torch.int32, device=device)
         long.compress(self.cache, kept, self.budget, self.sink, self.recent)
+        self.prompted = True
         return kept
 
     def step(self) -> None:

@@ -125,6 +125,34 @@ def test_the_head_takes_normalised_rows(gpu, monkeypatch):
         assert np.all(np.abs(seen["logits"] - want) <= np.abs(want) * 2.0 ** -8 + np.abs(want).max(1, keepdims=True) * 2.0 ** -12)
 
 
+@pytest.mark.parametrize("prompt", [False, True])
+def test_a_second_generation_is_as_the_first(gpu, monkeypatch, prompt):
+    """Two generations in a row on one loop, and each of them on a loop of its own: the same tokens, positions and live slots."""
+    lib, device, torch = gpu
+
+    def generation(loop, i, bits):
+        if prompt:
+            g = torch.Generator().manual_seed(i)
+            some = lambda *shape: torch.randn(shape, generator=g).to(torch.bfloat16).view(torch.int16).cuda()   # noqa: E731
+            loop.prompt(some(L, S, 31 + i, HEADS, 64), some(L, S, 31 + i, KV, 64), some(L, S, 31 + i, KV, 64), 8)
+        loop.start(torch.tensor([5 + i, 60, 7 * i], dtype=torch.int32).cuda())
+        given = T.run_steps(loop, 9)
+        torch.cuda.synchronize()
+        live = torch.arange(BUDGET, device="cuda") < loop.cache.len[:, None, None]
+        out = {n: getattr(loop.cache, n).clone() for n in ("len", "next_pos")}
+        out.update({n: torch.where(live, getattr(loop.cache, n), 0) for n in ("mass", "slot_pos")})
+        out.update({n: torch.where(live[..., None], getattr(loop.cache, n), 0) for n in ("k", "v")})
+        out.update(emitted=torch.stack(given), counts=loop.counts.clone(), mass_prefill=loop.mass_prefill.clone(), tokens=loop.tokens.clone())
+        return out
+
+    one, _, bits = make_loop(gpu, monkeypatch, 8, 40)
+    for i in range(2):
+        alone, _, _ = make_loop(gpu, monkeypatch, 8, 40)
+        got, want = generation(one, i, bits), generation(alone, i, bits)
+        for n in want:
+            assert torch.equal(got[n], want[n]), (i, n)
+
+
 def test_tables_and_prefix_in_bfloat16(gpu, monkeypatch):
     """The same numbers handed in as bfloat16 and as their patterns."""
     lib, device, torch = gpu

@@ -153,6 +153,7 @@ class DecodingLoop:
     def prompt(self, q, k, v, window: int) -> torch.Tensor:
         """Every stream's own prompt of N tokens, not yet turned: q bf16 [L][S][N][heads][64], k and v [L][S][N][kv][64].  Its last
         `window` rows weigh what they see, the prefix and the slots, the heaviest of which stay.  Returns the slots that were kept, [L][S][kv][budget]."""
+        q, k, v = _patterns(q), _patterns(k), _patterns(v)
         N, device = int(k.shape[2]), k.device
         self.reset()
         long = self._cache(N, device)

@@ -103,6 +103,19 @@ def test_a_prompt_beside_the_prefix_is_one_sequence(gpu, monkeypatch, P):
         assert np.all(np.abs(loop.mass_prefill.cpu().numpy() - shared) <= shared * (np.exp(most) - 1) + 1e-6)
 
 
+def test_a_prompt_in_bfloat16(gpu, monkeypatch):
+    lib, device, torch = gpu
+    results = []
+    for dtype in (torch.int16, torch.bfloat16):
+        loop, _, bits = make_loop(gpu, monkeypatch, 6, 40)
+        q, k, v = (t.view(dtype) for t in (bits(L, S, 50, HEADS, 64), bits(L, S, 50, KV, 64), bits(L, S, 50, KV, 64)))
+        kept = loop.prompt(q, k, v, 9)
+        torch.cuda.synchronize()
+        results.append([kept] + [getattr(loop.cache, n) for n in ("k", "v", "mass", "slot_pos", "len", "next_pos")])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_the_head_takes_normalised_rows(gpu, monkeypatch):
     """Logits before the rules: the head's product on the last layer's rows times 1 / rms.  Bound: bf16's half step, and both
     products' sums in fp32 (2^-12 of the row's largest covers 128 products and their roundings)."""

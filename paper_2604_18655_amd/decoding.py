@@ -49,11 +49,10 @@ class DecodingLoop:
     def __init__(self, layers: Sequence[Sequence[B.Proj]], head: B.Proj, embedding, forecast, n_streams: int, branch: Sequence[int],
                  budget: int, sink: int = 4, recent: int = 32, decay: float = 1.0, rope: Optional[B.Rope] = None, k_prefill=None,
                  v_prefill=None, row_adapter=None, rules: Optional[dict] = None, device="cuda:0"):
-        """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary, the last normalisation's
-        weight folded in; embedding bf16 [V][hidden] and forecast
-        bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill bf16 [L][H][P][64], shared by the streams,
-        keys turned by their positions 0 .. P - 1.  A stream's own positions (next_pos and slot_pos of its cache, sink) count from its
-        first token, which is turned as the one at position P.  rules: keyword
+        """layers: (q, k, v, o, gate_up, down) of each layer; head: hidden -> vocabulary, the last normalisation's weight folded in;
+        embedding bf16 [V][hidden] and forecast bf16 [m][hidden] (or their int16 patterns, like all bf16 here); k_prefill, v_prefill
+        bf16 [L][H][P][64], shared by the streams, keys turned by their positions 0 .. P - 1.  A stream's own positions (next_pos
+        and slot_pos of its cache, sink) count from its first token, which is turned as the one at position P.  rules: keyword
         arguments of binding.LogitRules (counts and parent are made here).  Stream caches have room for `budget` slots."""
         L, S, m = len(layers), int(n_streams), int(forecast.shape[0])
         self.T, self.R = B.ds2d_rows(branch, m)
@@ -152,11 +151,19 @@ class DecodingLoop:
 
     def prompt(self, q, k, v, window: int) -> torch.Tensor:
         """Every stream's own prompt of N tokens, not yet turned: q bf16 [L][S][N][heads][64], k and v [L][S][N][kv][64].  Its last
-        `window` rows weigh what they see, the prefix and the slots, the heaviest of which stay.  Returns the slots that were kept, [L][S][kv][budget]."""
+        `window` rows weigh what they see, the prefix and the slots, the heaviest of which stay.  Returns the slots that were
+        kept, [L][S][kv][budget]."""
         q, k, v = _patterns(q), _patterns(k), _patterns(v)
-        N, device = int(k.shape[2]), k.device
-        self.reset()
+        N, device = int(k.shape[2]) if k.dim() == 5 else 0, k.device
+        for t, heads in ((q, self.heads), (k, self.kv), (v, self.kv)):
+            if tuple(t.shape) != (self.L, self.S, N, heads, HEAD_DIM) or not 1 <= window <= N:
+                raise B.MloraError(B._ESHAPE, "decoding loop's prompt")
         long = self._cache(N, device)
+        weigh = B.AttentionMass(long, self.heads, window, self.scale, k_prefill=self.keep[0], mass_prefill=self.mass_prefill, decay=self.decay)
+        ws = torch.empty(weigh.workspace_bytes(), dtype=torch.uint8, device=device)
+        if ws.numel() == 0:                              # (more rows than a call takes)
+            raise B.MloraError(B._ESHAPE, "decoding loop's prompt")
+        self.reset()
         turned = torch.empty((self.L, self.S, window) + tuple(q.shape[3:]), dtype=q.dtype, device=device)
         first, at = (torch.tensor([self.prefix + n], dtype=torch.int32).to(device) for n in (0, N - window))
         for l in range(self.L):
@@ -167,8 +174,6 @@ class DecodingLoop:
         long.slot_pos.copy_(torch.arange(N, dtype=torch.int32, device=device).expand(long.slot_pos.shape))
         long.len.fill_(N)
         long.next_pos.fill_(N)
-        weigh = B.AttentionMass(long, self.heads, window, self.scale, k_prefill=self.keep[0], mass_prefill=self.mass_prefill, decay=self.decay)
-        ws = torch.empty(max(256, weigh.workspace_bytes()), dtype=torch.uint8, device=device)
         weigh.run(turned.view(self.L, self.S * window, self.heads, HEAD_DIM), None, ws)
         kept = torch.empty((self.L, self.S, self.kv, self.budget), dtype=torch.int32, device=device)
         long.compress(self.cache, kept, self.budget, self.sink, self.recent)

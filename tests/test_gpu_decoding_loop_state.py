@@ -116,6 +116,20 @@ def test_a_prompt_in_bfloat16(gpu, monkeypatch):
         assert torch.equal(a, b)
 
 
+def test_prompts_that_do_not_fit_are_refused(gpu, monkeypatch):
+    lib, device, torch = gpu
+    loop, _, bits = make_loop(gpu, monkeypatch, 6, 40)
+    q, k, v = bits(L, S, 20, HEADS, 64), bits(L, S, 20, KV, 64), bits(L, S, 20, KV, 64)
+    before = T.snapshot(loop)
+    for args, status in [((q, k, v, 0), -2), ((q, k, v, 21), -2), ((q[:, :2], k, v, 4), -2), ((q, k[:1], v, 4), -2), ((q, k, v[:, :, :19], 4), -2),
+                         ((q[..., :1, :], k, v, 4), -2), ((q, k, v[0], 4), -2), ((q, k.float(), v, 4), -1), ((q.half(), k, v, 4), -1)]:
+        with pytest.raises(lib.MloraError) as e:
+            loop.prompt(*args)
+        assert e.value.status == status
+    for n, t in T.snapshot(loop).items():
+        assert torch.equal(t, before[n]), n
+
+
 def test_the_head_takes_normalised_rows(gpu, monkeypatch):
     """Logits before the rules: the head's product on the last layer's rows times 1 / rms.  Bound: bf16's half step, and both
     products' sums in fp32 (2^-12 of the row's largest covers 128 products and their roundings)."""

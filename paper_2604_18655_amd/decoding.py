@@ -61,8 +61,9 @@ class DecodingLoop:
         if rope is not None and (rope.struct.head_dim, rope.struct.rot, rope.struct.layout) != (HEAD_DIM, HEAD_DIM, B.ROPE_HALF):
             raise B.MloraError(B._ESHAPE, "decoding loop")          # (what the fused projections turn)
         if row_adapter is not None:
-            B._buffer(row_adapter, "decoding loop", B._AS_INT32, n=S * self.R)
-        if budget < m + 1 or sink < 0 or recent < 0:     # (a step appends up to m + 1 rows)
+            B._buffer(row_adapter, "decoding loop", B._AS_INT32)
+        short = row_adapter is not None and row_adapter.numel() < S * self.R
+        if short or budget < m + 1 or sink < 0 or recent < 0:        # (a step appends up to m + 1 rows)
             raise B.MloraError(B._ESHAPE, "decoding loop")
         parent, is_forecast, _ = B.ds2d_layout(branch, m)
         M, V, hidden = S * self.R, head.N, head.K

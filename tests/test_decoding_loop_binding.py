@@ -208,6 +208,7 @@ def test_a_budget_below_a_step_is_refused(bad):
     dict(k_prefill=dev(2, 1, 9, 64, dtype=torch.int16), v_prefill=dev(2, 1, 8, 64, dtype=torch.int16)),
     dict(k_prefill=dev(1, 1, 9, 64, dtype=torch.int16), v_prefill=dev(1, 1, 9, 64, dtype=torch.int16)),
     dict(row_adapter=dev(3)),
+    dict(row_adapter=dev(89)),
     dict(rope=lib.Rope(64, 64, lib.ROPE_INTERLEAVED, device="cpu")), dict(rope=lib.Rope(64, 32, device="cpu")), dict(rope=lib.Rope(128, 64, device="cpu")),
 ])
 def test_parts_of_a_loop_that_do_not_fit_are_refused(bad):

@@ -246,7 +246,10 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
     const auto work = [&](const Keys &x, int c) {
         const int nk = min(KC, w.keys - c * KC);
         const bool masked = nk < KC || (!w.prefill && __any(x.pos > w.newest));
-        const float factor = masked ? 1.f : a.scale2;                // of scores (hidden ones: minus infinity, at any scale)
+        // Hidden scores are minus infinity at any scale.  Scores are scaled in the multiply-add of the exponential, as mass_add does: one
+        // that had been rounded before would not be the one that is weighed (of 10^7, by as much as 2^0.9).
+        const float factor = masked && a.scale2 == 0.f ? 1.f : a.scale2, kept = a.scale2 == 0.f ? 0.f : 1.f;
+        const float hidden = a.scale2 < 0.f ? __builtin_inff() : -__builtin_inff();
         // (all tiles side by side, whether their vectors count or not: one after the other, each waits for its products)
         f32x4 sc[QT][KC / 16];
 #pragma unroll
@@ -266,7 +269,7 @@ __device__ __forceinline__ void stats_tiles(const MassArgs &a, const Unit &w, fl
                     const int key_pos = __shfl(x.pos, key);          // (all lanes: before any condition)
 #pragma unroll
                     for (int t = 0; t < QT; ++t)
-                        sc[t][j][e] = key < nk && (w.prefill || key_pos <= pos[t]) ? sc[t][j][e] * a.scale2 : -__builtin_inff();
+                        sc[t][j][e] = key < nk && (w.prefill || key_pos <= pos[t]) ? sc[t][j][e] * kept : hidden;
                 }
         }
         // Sums relative to maxima that may lie behind: the sums themselves tell when one does too far (the first chunk, and rarely

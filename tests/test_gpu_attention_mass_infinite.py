@@ -72,3 +72,24 @@ def test_keys_of_minus_infinity_beside_rows_that_do_not_count(gpu, dim, L, S, H,
     if P:
         assert np.all(np.isfinite(got_p)) and np.array_equal(got_p[..., [0, P - 1]], np.float32(0.9) * c["mass_prefill"][..., [0, P - 1]])
     assert not np.array_equal(plain["k"], c["k"])
+
+
+@pytest.mark.parametrize("L,S,H,G,dim,cap,P,R", [
+    (1, 1, 2, 4, 64, 1100, 0, 1), (1, 2, 2, 4, 128, 150, 70, 3), (1, 3, 1, 3, 64, 331, 97, 5),       # maxima and sums by themselves
+    (1, 2, 2, 4, 64, 300, 0, 3), (1, 1, 2, 3, 64, 60, 50, 3),                                         # one pass
+    (8, 16, 2, 2, 64, 80, 70, 3),                                                                     # and a shared segment's masses behind it
+    (1, 1, 2, 4, 128, 500, 0, 190), (1, 1, 4, 8, 64, 500, 0, 190),                                    # the wide products
+])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+def test_weights_of_large_scores_sum_to_one(gpu, L, S, H, G, dim, cap, P, R, scale):
+    """Scores of some 10^7, whose step in fp32 is one: a weight's share of its row is made of the very scores that are weighed.  Bound: the
+    exponentials, sums and divisions, as beside a row's weights (n^(1/2) + 16 steps)."""
+    c = T.make(45 + cap, L, S, H, G, dim, cap, P, R, [cap] * S, ordered=True, q_std=1.0)
+    c["q"] = T.bf16((T.bf16_bits_to_f32(c["q"]).astype(np.float64) * 2.0 ** 19).astype(np.float32))
+    c["scale"], c["mass"][:] = scale, 0.0
+    if P:
+        c["mass_prefill"][:] = 0.0
+    got, got_p = T.run(gpu, c, None, 1.0)
+    total = got.astype(np.float64).sum((1, 3)) + (got_p.astype(np.float64).sum(2) if P else 0.0)      # of a layer and head
+    rows = S * R * G
+    assert np.all(np.abs(total - rows) <= rows * ((cap + P) ** 0.5 + 16) * 2.0 ** -23 + rows * (cap + P) ** 0.5 * 2.0 ** -23)

@@ -211,7 +211,7 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
 
-_torch_c = None
+_raw_stream = _device = None
 
 
 class _PublicStream:
@@ -231,18 +231,19 @@ class _PublicStream:
 def _stream() -> int:
     """torch's current stream on the current device, without the Python object around it: 2.9 us of a
     call's 8.9 us of host time, where its kernel takes 6.0 (256 x 256 at 8 rows)."""
-    global _torch_c
-    if _torch_c is None:
+    global _raw_stream, _device
+    if _raw_stream is None:
         import torch
         torch.cuda.current_stream()                      # initialises the device, or says why it cannot
         both = hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice")
-        _torch_c = torch._C if both else _PublicStream
-    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
+        calls = torch._C if both else _PublicStream
+        _device, _raw_stream = calls._cuda_getDevice, calls._cuda_getCurrentRawStream
+    return _raw_stream(_device())
 
 
 def _forget_device() -> None:
-    global _torch_c
-    _torch_c = None
+    global _raw_stream, _device
+    _raw_stream = _device = None
 
 
 os.register_at_fork(after_in_child=_forget_device)       # (torch refuses a device that the parent has initialised)
@@ -593,15 +594,6 @@ def _call_buffer(t, where: str, kind: _Kind, n: int) -> None:
         _buffer(t, where, kind, n=n)
 
 
-def _call_list(t, where: str, streams: int) -> int:
-    """Entries per stream of an int32 list [streams][n]."""
-    size = t.nbytes
-    n = size // (4 * streams)
-    if size != 4 * streams * n or t.dtype is not _AS_INT32.last or not t.is_contiguous() or not t.is_cuda:
-        _buffer(t, where, _AS_INT32, n=streams * n)
-    return n
-
-
 class Rope:
     """Rotary positions (mlora_rope): `rot` of head_dim features turn, in pairs of the half or the interleaved layout, by
     frequencies that are plain, divided by factor (linear), of a larger base (base) or stretched where they turn fewer than
@@ -702,7 +694,7 @@ class StreamCache:
         self.struct = _StreamCacheStruct(L, S, H, D, cap, _ptr(k), _ptr(v), _ptr(mass), _ptr(slot_pos), _ptr(len),
                                          _ptr(next_pos), _ptr(self.tickets))
         self.ref = C.byref(self.struct)
-        self.streams, self.heads, self.row_bytes = S, L * S * H, 2 * L * S * H * D
+        self.streams, self.heads, self.row_bytes, self.list_bytes = S, L * S * H, 2 * L * S * H * D, 4 * S
         self.append_fn = load_library().mlora_stream_cache_append
         self.compress_fn = load_library().mlora_stream_cache_compress
 
@@ -719,7 +711,11 @@ class StreamCache:
                 _call_buffer(t, where, _AS_BF16, size // 2)
         listed = 0
         if rows is not None:
-            listed = _call_list(rows, where, self.streams)
+            size = rows.nbytes
+            listed = size // self.list_bytes
+            if (size != listed * self.list_bytes or rows.dtype is not _AS_INT32.last or not rows.is_contiguous()
+                    or not rows.is_cuda):
+                _buffer(rows, where, _AS_INT32, n=self.streams * listed)
             if listed == 0:                              # (its pointer is null: all rows)
                 raise MloraError(_ESHAPE, where)
         st = self.append_fn(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
@@ -755,7 +751,7 @@ class AttentionMass:
             if mass_prefill is not None:
                 _buffer(mass_prefill, "attention mass", _AS_FP32, (L, H, P))
         self.keep = (cache, k_prefill, mass_prefill)
-        self.streams, self.q_elements = S, L * S * int(rows_per_stream) * int(n_q_heads) * D
+        self.streams, self.list_bytes, self.q_elements = S, 4 * S, L * S * int(rows_per_stream) * int(n_q_heads) * D
         self.struct = _AttentionMassStruct(cache.struct, int(n_q_heads), int(rows_per_stream), float(scale),
                                            _ptr(k_prefill), _ptr(mass_prefill), P, float(decay))
         self.ref = C.byref(self.struct)
@@ -771,7 +767,11 @@ class AttentionMass:
         _call_buffer(q, where, _AS_BF16, self.q_elements)
         listed = 0
         if rows is not None:
-            listed = _call_list(rows, where, self.streams)
+            size = rows.nbytes
+            listed = size // self.list_bytes
+            if (size != listed * self.list_bytes or rows.dtype is not _AS_INT32.last or not rows.is_contiguous()
+                    or not rows.is_cuda):
+                _buffer(rows, where, _AS_INT32, n=self.streams * listed)
             if listed == 0:                              # (its pointer is null: all rows)
                 raise MloraError(_ESHAPE, where)
         if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
@@ -808,6 +808,7 @@ class LogitRules:
             _buffer(mask_row, where, _AS_INT32, n=S * R)
         self.keep = (parent, counts, repetition, frequency, presence, bias, bias_row, masks, mask_row)
         self.streams, self.tokens, self.logits, self.kind = S, S * T, S * R * V, _AS_BF16 if logits_dtype == Y_BF16 else _AS_FP32
+        self.list_bytes, self.token_bytes, self.logit_bytes = 4 * S, 4 * self.tokens, self.kind.itemsize * self.logits
         self.struct = _LogitRulesStruct(S, R, T, V, int(logits_dtype), _ptr(parent), _ptr(counts), _ptr(repetition),
                                         _ptr(frequency), _ptr(presence), _ptr(bias), _ptr(bias_row),
                                         0 if bias is None else int(bias.shape[0]), _ptr(masks), _ptr(mask_row),
@@ -818,16 +819,22 @@ class LogitRules:
     def run(self, logits, tokens, out, new_tokens=None, stream: Optional[int] = None) -> None:
         """logits [S * R][V] -> out (may be logits itself); tokens int32 [S][T]; new_tokens int32 [S][n]: counted first."""
         where = "mlora_logit_rules_apply"
-        kind = self.kind
-        size, dtype = kind.itemsize * self.logits, kind.last
-        if (logits.nbytes != size or out.nbytes != size or tokens.nbytes != 4 * self.tokens or logits.dtype is not dtype
+        kind, size = self.kind, self.logit_bytes
+        dtype = kind.last
+        if (logits.nbytes != size or out.nbytes != size or tokens.nbytes != self.token_bytes or logits.dtype is not dtype
                 or out.dtype is not dtype or tokens.dtype is not _AS_INT32.last or not logits.is_contiguous()
                 or not out.is_contiguous() or not tokens.is_contiguous() or not logits.is_cuda or not out.is_cuda
                 or not tokens.is_cuda):
             _call_buffer(logits, where, kind, self.logits)
             _call_buffer(out, where, kind, self.logits)
             _call_buffer(tokens, where, _AS_INT32, self.tokens)
-        fresh = 0 if new_tokens is None else _call_list(new_tokens, where, self.streams)
+        fresh = 0
+        if new_tokens is not None:
+            size = new_tokens.nbytes
+            fresh = size // self.list_bytes
+            if (size != fresh * self.list_bytes or new_tokens.dtype is not _AS_INT32.last or not new_tokens.is_contiguous()
+                    or not new_tokens.is_cuda):
+                _buffer(new_tokens, where, _AS_INT32, n=self.streams * fresh)
         st = self.fn(self.ref, logits.data_ptr(), tokens.data_ptr(), new_tokens.data_ptr() if fresh else None, fresh,
                      out.data_ptr(), _stream() if stream is None else stream)
         if st != 0:

@@ -13,7 +13,7 @@
  *     z2 = z1 - (frequency[s] * c + presence[s] * (c > 0)) + bias[bias_row[s]][v]
  *     out = token v is allowed by mask mask_row[row] ? z2 : -infinity           (whatever z2 is, NaN too)
  *
- * in fp32, rounded once.  First it adds the stream's new tokens to counts[] (each entry of new_tokens[s] in [0, V) once; other
+ * in fp32, rounded once at the end; z / repetition[s] is z times the fp32 number next to 1 / repetition[s].  First it adds the stream's new tokens to counts[] (each entry of new_tokens[s] in [0, V) once; other
  * values, such as the -1 behind a short list, are skipped).
  *
  * Conventions as in mlora_w4.h.  Logits need the alignment of one element only.
@@ -37,7 +37,7 @@ typedef struct {
     int32_t logits_dtype;           /* MLORA_Y_BF16 or MLORA_Y_FP32, of logits and out */
     const int32_t *parent;          /* device int32 [S * R]: an earlier row of the stream; anything else ends the path there */
     int32_t *counts;                /* device int32 [S][V], in and out, or NULL: the rows of the step are all there is */
-    const float *repetition;        /* device fp32 [S], not 0, or NULL: 1 */
+    const float *repetition;        /* device fp32 [S], of a magnitude from 2^-126 to 2^126, or NULL: 1 */
     const float *frequency;         /* device fp32 [S], or NULL: 0 */
     const float *presence;          /* device fp32 [S], or NULL: 0 */
     const float *bias;              /* device fp32 [n_bias][V] */

@@ -71,7 +71,8 @@ mlora_status mlora_stream_cache_compress(const mlora_stream_cache *from, const m
  *     mass[t]         = decay * mass[t]         + sum over rows and query heads of softmax(scale q . k)[t]     (live slots)
  *     mass_prefill[t] = decay * mass_prefill[t] + the same, over all streams
  * (the soft-max runs over both segments; a row that sees nothing, or whose scores are all minus infinity, adds nothing; one with NaN or
- * plus infinity among its scores makes what it sees NaN, and only that). */
+ * plus infinity among its scores makes what it sees NaN, and only that; finite scores scale q . k are of a magnitude below 2^30: beyond,
+ * fp32 does not hold their differences and weights may be NaN). */
 typedef struct {
     mlora_stream_cache cache;
     int32_t n_q_heads;                 /* a multiple of n_kv_heads, at most 8 query heads per kv head */

@@ -1191,11 +1191,13 @@ Plan plan_of(const mlora_attention_mass &d, int N)
     // The wide products, which take three launches and 256 vectors a block, from half a tile of vectors on, and where scores times
     // vectors are many.  Of 64 features, 8 heads: 256 vectors on 3000 slots 21.5 us and by 16 vectors 19.2, on 12000 27.3 and 34.3; 800
     // on 1500 37.0 and 31.0, on 6000 39.3 and 52.3.  Of 128, 8 heads: 400 vectors on 400 slots 28.3 and 25.4, 256 on 3000 24.9
-    // and 26.8, 128 on 12000 28.4 and 38.9.  (A layer's query vectors are reached by 32-bit offsets.)
+    // and 26.8, 128 on 12000 28.4 and 38.9.  The product does not part all of these: at 64 features 800 on 1500 slots (0.9 of 2^33)
+    // go wide, where they lose 6 us, because 256 on 12000 (0.7 of 2^33) gain 7.  (A layer's query vectors are reached by 32-bit offsets.)
     p.wide = d.scale > 0.f && own >= WIDE_OWN / 2 && d.n_q_heads <= 1024
           && (double)lh * ((double)c.cap * own * c.n_streams + (double)d.len_prefill * all) * own >= (c.head_dim == 64 ? 0x1p32 : 0x1p29);
     // One pass where a block holds the keys: up to 16 tiles in each of eight waves (9 with 17 to 32 vectors, whose scores take twice the
-    // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner.  As
+    // registers), or 9 and 4 in sixteen, in which a block that is alone on its compute unit is through sooner (4, 9 and 16 are
+    // built, and a number between takes the next; others were not timed).  As
     // the only launch it is always taken up to 64 tiles (32 with more vectors): 1000 keys on 8 or 32 blocks 8.6 and 8.5 us, in
     // two passes 11.5 and 11.3; 300 keys 5.6 and 9.8.  Beyond, a compute unit by itself draws too little from memory, so it
     // takes blocks: one per feature (32 blocks of 2000 keys of 64 features 11.8 and 11.5 us, 64 blocks 12.2 and 14.3; 64 blocks of

@@ -1,9 +1,10 @@
 """A decoding loop on a bounded cache as a sequence of library calls: several output streams, a draft tree with forecast
 embeddings per stream (Sections 3.4 and 3.5 of the paper), and stream caches that keep to a budget.
 
-    prompt   rope (queries and keys turned, keys and values into a long segment), attention weights of its last rows,
-             compression of the segment to its heaviest slots
-    step     rope tables for the rows' positions, the decoder layers (decoder.py), the head's logits, rules on them
+    prompt   rope (queries and keys turned, keys and values into a long segment), attention weights of its last rows on the
+             shared prefix and on the segment, compression of the segment to its heaviest slots
+    step     rope tables for the rows' positions behind the prefix, the decoder layers (decoder.py), the head's logits from
+             rows normalised by the sums of squares that the last layer leaves, rules on them
              (penalties, biases, grammar masks), verification and next drafts (DS2D), the accepted rows into the caches of all
              layers, their attention weights added to the slots they saw
 

@@ -13,8 +13,9 @@
  *     z2 = z1 - (frequency[s] * c + presence[s] * (c > 0)) + bias[bias_row[s]][v]
  *     out = token v is allowed by mask mask_row[row] ? z2 : -infinity           (whatever z2 is, NaN too)
  *
- * in fp32, rounded once at the end; z / repetition[s] is z times the fp32 number next to 1 / repetition[s].  First it adds the stream's new tokens to counts[] (each entry of new_tokens[s] in [0, V) once; other
- * values, such as the -1 behind a short list, are skipped).
+ * in fp32, rounded once at the end; z / repetition[s] is z times the fp32 number next to 1 / repetition[s].  First it adds the
+ * stream's new tokens to counts[] (each entry of new_tokens[s] in [0, V) once; other values, such as the -1 behind a short list, are
+ * skipped).
  *
  * Conventions as in mlora_w4.h.  Logits need the alignment of one element only.
  */

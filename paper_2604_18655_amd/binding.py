@@ -31,6 +31,12 @@ loop_symbols = (
     "mlora_attention_mass_workspace_bytes", "mlora_attention_mass_add",
     "mlora_logit_rules_apply",
 )
+# of mlora_page_cache.h, mlora_page_attention.h and mlora_beam.h: beam search on a paged cache of 8 bits
+beam_symbols = (
+    "mlora_page_cache_own_words", "mlora_page_cache_append", "mlora_page_cache_reorder", "mlora_page_cache_copy",
+    "mlora_page_attention_workspace_bytes", "mlora_page_attention_plan", "mlora_page_attention",
+    "mlora_beam_workspace_bytes", "mlora_beam_select",
+)
 
 
 class MloraError(RuntimeError):
@@ -103,6 +109,24 @@ class _LogitRulesStruct(C.Structure):
                 ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
                 ("bias", C.c_void_p), ("bias_row", C.c_void_p), ("n_bias", C.c_int32), ("masks", C.c_void_p),
                 ("mask_row", C.c_void_p), ("n_masks", C.c_int32)]
+
+
+class _PageCacheStruct(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_streams", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p), ("v_tail", C.c_void_p),
+                ("slot", C.c_void_p), ("len", C.c_void_p), ("table", C.c_void_p), ("refs", C.c_void_p), ("own", C.c_void_p)]
+
+
+class _PageAttnStruct(C.Structure):
+    _fields_ = [("cache", _PageCacheStruct), ("layer", C.c_int32), ("n_q_heads", C.c_int32), ("rows_per_stream", C.c_int32),
+                ("scale", C.c_float), ("window", C.c_int32), ("sink", C.c_int32), ("k_new", C.c_void_p), ("v_new", C.c_void_p),
+                ("parent", C.c_void_p)]
+
+
+class _BeamStruct(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("n_beams", C.c_int32), ("vocab", C.c_int32), ("logits_dtype", C.c_int32),
+                ("eos", C.c_int32), ("pad", C.c_int32), ("length_power", C.c_float)]
 
 
 def lib_path() -> str:
@@ -190,6 +214,25 @@ def load_library():
         lib.mlora_attention_mass_add.argtypes = [mp, vp, vp, i32, vp, sz, vp]
         lib.mlora_logit_rules_apply.restype = C.c_int
         lib.mlora_logit_rules_apply.argtypes = [C.POINTER(_LogitRulesStruct), vp, vp, vp, i32, vp, vp]
+        gp, ap, bp = C.POINTER(_PageCacheStruct), C.POINTER(_PageAttnStruct), C.POINTER(_BeamStruct)
+        lib.mlora_page_cache_own_words.restype = sz
+        lib.mlora_page_cache_own_words.argtypes = [i32, i32]
+        lib.mlora_page_cache_append.restype = C.c_int
+        lib.mlora_page_cache_append.argtypes = [gp, vp, vp, i32, vp, i32, vp, vp]
+        lib.mlora_page_cache_reorder.restype = C.c_int
+        lib.mlora_page_cache_reorder.argtypes = [gp, vp, i32, i32, vp]
+        lib.mlora_page_cache_copy.restype = C.c_int
+        lib.mlora_page_cache_copy.argtypes = [gp, gp, vp, vp, vp]
+        lib.mlora_page_attention_workspace_bytes.restype = sz
+        lib.mlora_page_attention_workspace_bytes.argtypes = [ap]
+        lib.mlora_page_attention_plan.restype = C.c_int
+        lib.mlora_page_attention_plan.argtypes = [ap, C.POINTER(i32)]
+        lib.mlora_page_attention.restype = C.c_int
+        lib.mlora_page_attention.argtypes = [ap, vp, vp, i32, vp, sz, vp]
+        lib.mlora_beam_workspace_bytes.restype = sz
+        lib.mlora_beam_workspace_bytes.argtypes = [bp]
+        lib.mlora_beam_select.restype = C.c_int
+        lib.mlora_beam_select.argtypes = [bp] + [vp] * 10 + [sz, vp]
         lib.mlora_w4_workspace_status.restype = C.c_int
         lib.mlora_w4_workspace_status.argtypes = [vp, C.POINTER(i32), vp]
         lib.mlora_w4_debug_spin_limit.restype = i32
@@ -578,6 +621,7 @@ class _Kind:
 _AS_BF16 = _Kind(2, "bfloat16", "int16", "uint16")       # (or their patterns)
 _AS_FP32, _AS_FP64 = _Kind(4, "float32"), _Kind(8, "float64")
 _AS_INT32 = _Kind(4, "int32", "uint32")
+_AS_INT8 = _Kind(1, "int8")
 
 
 def _buffer(t, where: str, kind: _Kind, shape=None, n: Optional[int] = None) -> None:
@@ -837,5 +881,179 @@ class LogitRules:
                 _buffer(new_tokens, where, _AS_INT32, n=self.streams * fresh)
         st = self.fn(self.ref, logits.data_ptr(), tokens.data_ptr(), new_tokens.data_ptr() if fresh else None, fresh,
                      out.data_ptr(), _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)
+
+
+PAGE_TOKENS = 64
+
+
+class PageCache:
+    """A paged cache of 8 bits (mlora_page_cache): k int8 [L][n_pages][H][64][head_dim], v int8 [L][n_pages][H][head_dim][64], scales fp32
+    [L][n_pages][H], tails bf16 [L][S][H][64][head_dim], slot and len int32 [S], table int32 [S][max_pages], refs int32
+    [n_pages].  Made outside of a graph capture (the library's own words are uploaded here)."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail, slot, len, table, refs):
+        import torch
+        where = "page cache"
+        if k.dim() != 5 or k_tail.dim() != 5 or table.dim() != 2:
+            raise MloraError(_ESHAPE, where)
+        L, N, H, tokens, D = (int(x) for x in k.shape)
+        S, columns = int(k_tail.shape[1]), int(table.shape[1])
+        if tokens != PAGE_TOKENS:
+            raise MloraError(_ESHAPE, where)
+        _buffer(k, where, _AS_INT8, (L, N, H, tokens, D))
+        _buffer(v, where, _AS_INT8, (L, N, H, D, tokens))
+        for t in (k_scale, v_scale):
+            _buffer(t, where, _AS_FP32, (L, N, H))
+        for t in (k_tail, v_tail):
+            _buffer(t, where, _AS_BF16, (L, S, H, tokens, D))
+        for t, shape in ((slot, (S,)), (len, (S,)), (table, (S, columns)), (refs, (N,))):
+            _buffer(t, where, _AS_INT32, shape)
+        words = int(load_library().mlora_page_cache_own_words(S, N))
+        if words == 0:
+            raise MloraError(_ESHAPE, where)
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail = k, v, k_scale, v_scale, k_tail, v_tail
+        self.slot, self.len, self.table, self.refs = slot, len, table, refs
+        self.own = torch.zeros(words, dtype=torch.int32).to(k.device)       # (an upload: done when it returns)
+        self.shape = (L, S, H, D)
+        self.struct = _PageCacheStruct(L, S, H, D, N, columns, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_tail),
+                                       _ptr(v_tail), _ptr(slot), _ptr(len), _ptr(table), _ptr(refs), _ptr(self.own))
+        self.ref = C.byref(self.struct)
+        self.streams, self.row_bytes, self.list_bytes = S, 2 * L * S * H * D, 4 * S
+        lib = load_library()
+        self.append_fn, self.reorder_fn, self.copy_fn = lib.mlora_page_cache_append, lib.mlora_page_cache_reorder, lib.mlora_page_cache_copy
+
+    @classmethod
+    def empty(cls, n_layers: int, n_streams: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages: int, device="cuda:0") -> "PageCache":
+        """An empty cache, its memory made here."""
+        import torch
+        L, S, H, D, N, P = n_layers, n_streams, n_kv_heads, head_dim, n_pages, PAGE_TOKENS
+        z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)   # noqa: E731
+        return cls(z((L, N, H, P, D), torch.int8), z((L, N, H, D, P), torch.int8), z((L, N, H), torch.float32), z((L, N, H), torch.float32),
+                   z((L, S, H, P, D), torch.bfloat16), z((L, S, H, P, D), torch.bfloat16), torch.arange(S, dtype=torch.int32).to(device),
+                   z((S,), torch.int32), torch.full((S, max_pages), -1, dtype=torch.int32).to(device), z((N,), torch.int32))
+
+    def append(self, k_new, v_new, rows_per_stream: int, rows=None, appended=None, stream: Optional[int] = None) -> None:
+        """Listed rows (int32 [S][n], None: all) of k_new and v_new bf16 [L][S * rows_per_stream][H][head_dim] enter; appended
+        int32 [S]: how many did."""
+        where = "mlora_page_cache_append"
+        size = self.row_bytes * rows_per_stream
+        if (k_new.nbytes != size or v_new.nbytes != size or k_new.dtype is not _AS_BF16.last
+                or v_new.dtype is not _AS_BF16.last or not k_new.is_contiguous() or not v_new.is_contiguous()
+                or not k_new.is_cuda or not v_new.is_cuda):
+            for t in (k_new, v_new):
+                _call_buffer(t, where, _AS_BF16, size // 2)
+        listed = 0
+        if rows is not None:
+            size = rows.nbytes
+            listed = size // self.list_bytes
+            if (size != listed * self.list_bytes or rows.dtype is not _AS_INT32.last or not rows.is_contiguous()
+                    or not rows.is_cuda):
+                _buffer(rows, where, _AS_INT32, n=self.streams * listed)
+            if listed == 0:                              # (its pointer is null: all rows)
+                raise MloraError(_ESHAPE, where)
+        if appended is not None:
+            _call_buffer(appended, where, _AS_INT32, self.streams)
+        st = self.append_fn(self.ref, k_new.data_ptr(), v_new.data_ptr(), rows_per_stream,
+                            None if rows is None else rows.data_ptr(), listed, None if appended is None else appended.data_ptr(),
+                            _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)
+
+    def reorder(self, source=None, window: int = 0, sink: int = 0, stream: Optional[int] = None) -> None:
+        """Stream s becomes what source[s] was (int32 [S]; outside: empty; None: all stay); window > 0: pages that it has left
+        behind, but for those of the first `sink` tokens, are given up."""
+        where = "mlora_page_cache_reorder"
+        if source is not None:
+            _call_buffer(source, where, _AS_INT32, self.streams)
+        st = self.reorder_fn(self.ref, None if source is None else source.data_ptr(), window, sink,
+                             _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)
+
+    def copy_from(self, other: "PageCache", source, n_used=None, stream: Optional[int] = None) -> None:
+        """Stream i becomes what source[i] of another cache is (int32 [S]); all that this one held is gone.  n_used int32 [1]:
+        pages that the streams hold."""
+        where = "mlora_page_cache_copy"
+        _call_buffer(source, where, _AS_INT32, self.streams)
+        if n_used is not None:
+            _call_buffer(n_used, where, _AS_INT32, 1)
+        st = self.copy_fn(other.ref, self.ref, source.data_ptr(), None if n_used is None else n_used.data_ptr(),
+                          _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)
+
+
+class PageAttention:
+    """Descriptor of mlora_page_attention for one layer of a PageCache: k_new and v_new bf16 [S * R][H][head_dim], parent int32
+    [S * R]; takes the place of a TreeAttention in a DecoderLayerStep."""
+
+    def __init__(self, cache: PageCache, layer: int, n_q_heads: int, rows_per_stream: int, scale: float, k_new, v_new, parent,
+                 window: int = 0, sink: int = 0):
+        L, S, H, D = cache.shape
+        M, where = S * int(rows_per_stream), "page attention"
+        for t in (k_new, v_new):
+            _buffer(t, where, _AS_BF16, n=M * H * D)
+        _buffer(parent, where, _AS_INT32, n=M)
+        self.keep = (cache, None, None, None, None, None, None, k_new, v_new, parent)
+        self.shape = (M, int(n_q_heads), D)
+        self.elements = M * int(n_q_heads) * D
+        self.struct = _PageAttnStruct(cache.struct, int(layer), int(n_q_heads), int(rows_per_stream), float(scale), int(window), int(sink),
+                                      _ptr(k_new), _ptr(v_new), _ptr(parent))
+        self.ref = C.byref(self.struct)
+        self.fn = load_library().mlora_page_attention
+
+    def workspace_bytes(self) -> int:
+        return int(load_library().mlora_page_attention_workspace_bytes(self.ref))
+
+    def plan(self) -> dict:
+        """How the library would run the call (see mlora_page_attention_plan)."""
+        info = (C.c_int32 * 3)()
+        _check(load_library().mlora_page_attention_plan(self.ref, info), "mlora_page_attention_plan")
+        return {"tiles": info[0], "waves": info[1], "splits": info[2]}
+
+    def run(self, q, out, out_dtype: int, workspace, stream: Optional[int] = None) -> None:
+        """q bf16 [S * R][n_q_heads][head_dim] -> out, the same shape."""
+        where = "mlora_page_attention"
+        _call_buffer(q, where, _AS_BF16, self.elements)
+        _call_buffer(out, where, _AS_FP32 if out_dtype == Y_FP32 else _AS_BF16, self.elements)
+        if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+            raise MloraError(_EINVAL, where)
+        st = self.fn(self.ref, q.data_ptr(), out.data_ptr(), out_dtype, None if workspace is None else workspace.data_ptr(),
+                     0 if workspace is None else workspace.nbytes, _stream() if stream is None else stream)
+        if st != 0:
+            raise MloraError(st, where)
+
+
+class BeamSelect:
+    """Descriptor of mlora_beam_select: the best n_beams continuations of every group of n_beams beams."""
+
+    def __init__(self, n_groups: int, n_beams: int, vocab: int, logits_dtype: int, eos: int = -1, pad: int = 0, length_power: float = 0.0):
+        self.rows = int(n_groups) * int(n_beams)
+        self.kind = _AS_BF16 if logits_dtype == Y_BF16 else _AS_FP32
+        self.logits, self.row_bytes = self.rows * int(vocab), 4 * self.rows
+        self.struct = _BeamStruct(int(n_groups), int(n_beams), int(vocab), int(logits_dtype), int(eos), int(pad), float(length_power))
+        self.ref = C.byref(self.struct)
+        self.fn = load_library().mlora_beam_select
+
+    def workspace_bytes(self) -> int:
+        return int(load_library().mlora_beam_workspace_bytes(self.ref))
+
+    def run(self, logits, score, length, finished, source, token, score_out, length_out, finished_out, workspace,
+            stream: Optional[int] = None) -> None:
+        """logits [rows][vocab]; score fp32, length and finished int32 [rows] -> source and token int32 [rows], and the new beams'
+        score, length and finished, which may be the old ones' tensors."""
+        where = "mlora_beam_select"
+        _call_buffer(logits, where, self.kind, self.logits)
+        for t in (score, score_out):
+            _call_buffer(t, where, _AS_FP32, self.rows)
+        for t in (length, finished, source, token, length_out, finished_out):
+            _call_buffer(t, where, _AS_INT32, self.rows)
+        if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+            raise MloraError(_EINVAL, where)
+        st = self.fn(self.ref, logits.data_ptr(), score.data_ptr(), length.data_ptr(), finished.data_ptr(), source.data_ptr(), token.data_ptr(),
+                     score_out.data_ptr(), length_out.data_ptr(), finished_out.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                     0 if workspace is None else workspace.nbytes, _stream() if stream is None else stream)
         if st != 0:
             raise MloraError(st, where)

@@ -1,0 +1,548 @@
+// A paged cache of keys and values in 8 bits (see include/mlora_page_cache.h): rows that enter it, streams that become others, copies
+// into another cache.
+//
+// Every call is a block that does the bookkeeping (which pages, which slots) and leaves what the others need in the cache's own words,
+// and a launch that moves the data with blocks all over the card.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.hpp"
+
+#include "../../include/mlora_page_cache.h"
+
+namespace mlora {
+
+namespace {
+
+constexpr int P = MLORA_PAGE_TOKENS;
+constexpr int CTRL = 1024;                               // threads of a bookkeeping block; at least MLORA_PAGE_MAX_STREAMS
+static_assert(CTRL >= MLORA_PAGE_MAX_STREAMS, "a thread per stream");
+
+// the cache's own words: where the search for free pages starts (no page below is free), then what a call's two launches hand over
+constexpr int OWN_LOW = 0, OWN_COUNT = 1, OWN_PLAN = 64;
+struct Plan {
+    int first, count, slot, other;
+};
+constexpr int PLAN_WORDS = 4;
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+struct CacheArgs {
+    int8_t *k, *v;
+    float *k_scale, *v_scale;
+    uint16_t *k_tail, *v_tail;
+    int *slot, *len, *table, *refs, *own;
+    int L, S, H, D, pages, columns;
+};
+
+__device__ __forceinline__ int slot_of(const CacheArgs &c, int s) { return min(max(c.slot[s], 0), c.S - 1); }
+__device__ __forceinline__ int len_of(const CacheArgs &c, int s) { return min(max(c.len[s], 0), P * c.columns + P - 1); }
+__device__ __forceinline__ Plan *plans(const CacheArgs &c) { return reinterpret_cast<Plan *>(c.own + OWN_PLAN); }
+
+// Sums over the threads before this one, and over all of them.  One __syncthreads before `part` is used again is the caller's.
+struct Sums {
+    int before, all;
+};
+__device__ __forceinline__ Sums sums_of(int x, int (&part)[CTRL / 64])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int run = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(run, d);
+        run += lane >= d ? y : 0;
+    }
+    if (lane == 63) part[wave] = run;
+    __syncthreads();
+    int base = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < CTRL / 64; ++w) {
+        const int y = part[w];
+        base += w < wave ? y : 0;
+        all += y;
+    }
+    return Sums{base + run - x, all};
+}
+
+// The last of n ascending numbers, the first of them 0, that is at most i.
+__device__ __forceinline__ int last_from(const int *start, int n, int i)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (start[mid] <= i) lo = mid;
+        else                 hi = mid;
+    }
+    return lo;
+}
+
+// ---------------------------------------------------------------------------------------------- append
+
+struct AppendArgs {
+    CacheArgs c;
+    const uint16_t *k_new, *v_new;
+    const int *rows;
+    int *appended;
+    int R, n_rows;
+};
+
+constexpr int MAX_FILLED = MLORA_MAX_ROWS / P + MLORA_PAGE_MAX_STREAMS;   // pages that one call can fill: (S * 63 + S * R) / 64
+
+// Who enters, and which pages fill.
+__global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
+{
+    __shared__ int count[CTRL], start[CTRL], place[CTRL], part[CTRL / 64], list[MAX_FILLED], last;
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x;
+    count[tid] = a.n_rows;
+    if (tid == 0) last = 0;
+    __syncthreads();
+    if (a.rows)
+        for (int i = tid; i < c.S * a.n_rows; i += CTRL) {
+            const int r = a.rows[i], s = i / a.n_rows;
+            if (r < 0 || r >= a.R) atomicMin(&count[s], i - s * a.n_rows);
+        }
+    const int low = min(max(c.own[OWN_LOW], 0), c.pages) & ~3;
+    int len = 0, slot = 0, n = 0, wish = 0;
+    if (tid < c.S) {
+        len = len_of(c, tid);
+        slot = slot_of(c, tid);
+    }
+    __syncthreads();
+    if (tid < c.S) {
+        n = count[tid];
+        wish = (len % P + n) / P;
+        if (len / P + wish > c.columns) n = wish = 0;
+    }
+    const Sums want = sums_of(wish, part);
+    start[tid] = want.before;
+    place[tid] = len / P;
+    // the lowest free pages, as many as are wanted
+    int found = 0;
+    for (int p0 = low; found < want.all && p0 < c.pages; p0 += 4 * CTRL) {
+        int refs[4], some = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int p = p0 + 4 * tid + u;
+            refs[u] = p < c.pages ? c.refs[p] : 1;
+            some += refs[u] <= 0;
+        }
+        __syncthreads();
+        const Sums at = sums_of(some, part);
+        int number = found + at.before;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (refs[u] <= 0) {
+                if (number < want.all) list[number] = p0 + 4 * tid + u;
+                ++number;
+            }
+        found += at.all;
+    }
+    found = min(found, want.all);
+    const bool enters = wish == 0 || want.before + wish <= found;
+    if (!enters) n = 0;
+    else if (wish > 0) atomicMax(&last, want.before + wish);
+    __syncthreads();
+    const int used = last;                               // (streams that do not enter stand behind all that fill pages)
+    for (int i = tid; i < used; i += CTRL) {
+        const int s = last_from(start, c.S, i);
+        c.table[(size_t)slot_of(c, s) * c.columns + place[s] + (i - start[s])] = list[i];
+        c.refs[list[i]] = 1;
+    }
+    if (tid < c.S) {
+        c.len[tid] = len + n;
+        plans(c)[tid] = Plan{len, n, slot, 0};
+        if (a.appended) a.appended[tid] = n;
+    }
+    if (tid == 0 && used > 0) c.own[OWN_LOW] = used < found ? list[used] : list[used - 1] + 1;
+}
+
+// A page's 64 x D numbers to codes and a scale: the largest magnitude, as the bits of a bf16 number (which order like it)
+__device__ __forceinline__ unsigned top_bits(const u32x4 &x, unsigned top)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7FFFu, x[i] >> 16 & 0x7FFFu));
+    return top;
+}
+__device__ __forceinline__ u32x2 codes_of(const u32x4 &x, float top)
+{
+    u32x2 out = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float f = bf16_bits_to_float(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu);
+        out[i / 4] |= ((unsigned)(int)rintf(127.f * f / top) & 0xFFu) << 8 * (i % 4);
+    }
+    return out;
+}
+
+// Block y of a layer, stream and head fills its y-th page; the first one writes the tail as well, behind the page that takes what was there.
+template <int D>
+__global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
+{
+    constexpr int PIECES = D / 8, NP = P * PIECES / 256, PITCH = P + 16;
+    __shared__ __align__(16) unsigned char turned[D * PITCH];
+    __shared__ unsigned tops[2][4];
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, head = blockIdx.x, j = blockIdx.y;
+    const int s = head / c.H % c.S, l = head / (c.H * c.S), h = head - (l * c.S + s) * c.H;
+    const Plan plan = plans(c)[s];
+    const int t = plan.first % P, full = plan.first / P, filled = (t + plan.count) / P;
+    const size_t tail = (((size_t)l * c.S + plan.slot) * c.H + h) * P * D, stream = ((size_t)l * c.S + s) * a.R;
+    // token g of those behind the full pages (in the tail up to t), 8 of its features from f on
+    const auto from = [&](int g) {
+        const int i = min(g - t, plan.count - 1), row = a.rows ? a.rows[s * a.n_rows + i] : i;
+        return ((stream + row) * c.H + h) * D;
+    };
+    if (j < filled) {
+        u32x4 kx[NP], vx[NP];
+        unsigned kt = 0, vt = 0;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            const int piece = u * 256 + tid, g = j * P + piece / PIECES, f = piece % PIECES * 8;
+            const size_t at = g < t ? tail + (size_t)g * D + f : from(g) + f;
+            kx[u] = *reinterpret_cast<const u32x4 *>((g < t ? c.k_tail : a.k_new) + at);
+            vx[u] = *reinterpret_cast<const u32x4 *>((g < t ? c.v_tail : a.v_new) + at);
+        }
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            kt = top_bits(kx[u], kt);
+            vt = top_bits(vx[u], vt);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            kt = max(kt, (unsigned)__shfl_xor((int)kt, d));
+            vt = max(vt, (unsigned)__shfl_xor((int)vt, d));
+        }
+        if ((tid & 63) == 0) tops[0][tid >> 6] = kt, tops[1][tid >> 6] = vt;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) kt = max(kt, tops[0][w]), vt = max(vt, tops[1][w]);
+        const int page = min(max(c.table[(size_t)plan.slot * c.columns + full + j], 0), c.pages - 1);
+        const size_t unit = ((size_t)l * c.pages + page) * c.H + h;
+        const bool k_ok = kt > 0 && kt < 0x7F80u, v_ok = vt > 0 && vt < 0x7F80u;
+        const float k_top = bf16_bits_to_float(kt), v_top = bf16_bits_to_float(vt);
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            const int piece = u * 256 + tid, g = piece / PIECES, f = piece % PIECES * 8;
+            *reinterpret_cast<u32x2 *>(c.k + (unit * P + g) * D + f) = k_ok ? codes_of(kx[u], k_top) : u32x2{0, 0};
+            const u32x2 v = v_ok ? codes_of(vx[u], v_top) : u32x2{0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) turned[(f + e) * PITCH + g] = (unsigned char)(v[e / 4] >> 8 * (e % 4));
+        }
+        if (tid == 0) {
+            c.k_scale[unit] = kt < 0x7F80u ? k_top / 127.f : __builtin_nanf("");
+            c.v_scale[unit] = vt < 0x7F80u ? v_top / 127.f : __builtin_nanf("");
+        }
+        __syncthreads();
+        for (int i = tid; i < D * P / 16; i += 256)
+            *reinterpret_cast<u32x4 *>(c.v + unit * P * D + 16 * i) = *reinterpret_cast<const u32x4 *>(turned + (i / 4) * PITCH + (i % 4) * 16);
+    }
+    if (j == 0) {
+        // (everybody has read the old tail: the first barrier above)
+        const int first = filled ? filled * P : t, n = t + plan.count - first;
+        for (int piece = tid; piece < n * PIECES; piece += 256) {
+            const int g = first + piece / PIECES, f = piece % PIECES * 8;
+            const size_t at = from(g) + f, to = tail + (size_t)(g % P) * D + f;
+            *reinterpret_cast<u32x4 *>(c.k_tail + to) = *reinterpret_cast<const u32x4 *>(a.k_new + at);
+            *reinterpret_cast<u32x4 *>(c.v_tail + to) = *reinterpret_cast<const u32x4 *>(a.v_new + at);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- reorder
+
+struct ReorderArgs {
+    CacheArgs c;
+    const int *source;
+    int window, sink;
+};
+
+// Slots and lengths.  A stream's plan: its new length, whether its data moves (2: from a slot, 1: it becomes empty, 0: it stays), the slots
+// to and from; the words behind the plans hold what every slot held.
+__global__ __launch_bounds__(CTRL) void reorder_plan(const ReorderArgs a)
+{
+    __shared__ int first[CTRL], taken[CTRL], place[CTRL], part[CTRL / 64];
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, S = c.S;
+    int *const held = c.own + OWN_PLAN + PLAN_WORDS * S;
+    first[tid] = CTRL;
+    taken[tid] = 0;
+    int from = -1, len = 0, slot = 0;
+    if (tid < S) {
+        from = a.source ? a.source[tid] : tid;
+        if (from < 0 || from >= S) from = -1;
+        if (from >= 0) {
+            len = len_of(c, from);
+            slot = slot_of(c, from);
+        }
+        held[slot_of(c, tid)] = len_of(c, tid);
+    }
+    __syncthreads();
+    if (from >= 0) atomicMin(&first[from], tid);
+    __syncthreads();
+    const bool keeps = from >= 0 && first[from] == tid;
+    if (keeps) taken[slot] = 1;
+    __syncthreads();
+    const bool open = tid < S && !taken[tid];
+    const Sums slots = sums_of(open, part);
+    if (open) place[slots.before] = tid;
+    __syncthreads();
+    const Sums others = sums_of(tid < S && !keeps, part);
+    if (tid < S) {
+        const int to = keeps ? slot : place[others.before];
+        c.slot[tid] = to;
+        c.len[tid] = len;
+        plans(c)[tid] = Plan{len, keeps ? 0 : from >= 0 ? 2 : 1, to, slot};
+    }
+}
+
+// A table entry is given up: if nobody else holds its page, the page is free.
+__device__ __forceinline__ void give_up(const CacheArgs &c, int page)
+{
+    if (page >= 0 && page < c.pages && atomicSub(&c.refs[page], 1) == 1) atomicMin(&c.own[OWN_LOW], page);
+}
+
+// For every stream: `table_blocks` blocks over its table row, then one per layer and head for its tail.
+// No page is free in between: who gives one up held it, and who takes one takes it from a slot that keeps it.
+template <int D>
+__global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int table_blocks)
+{
+    const CacheArgs &c = a.c;
+    const Plan plan = plans(c)[blockIdx.y];
+    const int len = plan.first, moves = plan.count, to = plan.slot, from = plan.other;
+    if ((int)blockIdx.x < table_blocks) {
+        const int i = (int)blockIdx.x * 256 + (int)threadIdx.x, full = len / P;
+        if (i >= c.columns) return;
+        const bool gone = a.window > 0 && (i + 1) * P <= len - a.window + 1 && i * P >= a.sink;
+        int *const mine = c.table + (size_t)to * c.columns + i;
+        if (moves == 0) {
+            if (i >= full || !gone) return;
+            give_up(c, *mine);
+            *mine = -1;
+            return;
+        }
+        const int old_full = c.own[OWN_PLAN + PLAN_WORDS * c.S + to] / P;
+        const int page = moves == 2 && i < full && !gone ? c.table[(size_t)from * c.columns + i] : -1;
+        if (page >= 0 && page < c.pages) atomicAdd(&c.refs[page], 1);
+        if (i < old_full) give_up(c, *mine);
+        if (i < max(full, old_full)) *mine = page;
+        return;
+    }
+    const int n = len % P;
+    if (moves != 2 || n == 0) return;
+    const int unit = (int)blockIdx.x - table_blocks, l = unit / c.H, h = unit - l * c.H;
+    const size_t src = (((size_t)l * c.S + from) * c.H + h) * P * D, dst = (((size_t)l * c.S + to) * c.H + h) * P * D;
+    for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
+        reinterpret_cast<u32x4 *>(c.k_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.k_tail + src)[i];
+        reinterpret_cast<u32x4 *>(c.v_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.v_tail + src)[i];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- copy
+
+struct CopyArgs {
+    CacheArgs from, to;
+    const int *source;
+    int *n_used;
+};
+
+// Pages that the streams hold, how often, and which place each takes.  The marks of the pool's pages stand behind the plans of `from`, the list
+// of pages to copy behind those of `to`.
+__global__ __launch_bounds__(CTRL) void copy_plan(const CopyArgs a)
+{
+    __shared__ int part[CTRL / 64], start[CTRL], row[CTRL], too_long;
+    const CacheArgs &f = a.from, &t = a.to;
+    const int tid = threadIdx.x;
+    int *const marks = f.own + OWN_PLAN + (PLAN_WORDS + 1) * f.S, *const list = t.own + OWN_PLAN + (PLAN_WORDS + 1) * t.S;
+    if (tid == 0) too_long = 0;
+    for (int p = tid; p < f.pages; p += CTRL) __hip_atomic_store(&marks[p], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int len = 0, slot = 0, has = 0;
+    if (tid < t.S) {
+        const int s = a.source[tid];
+        has = s >= 0 && s < f.S;
+        if (has) {
+            len = len_of(f, s);
+            slot = slot_of(f, s);
+        }
+    }
+    __syncthreads();
+    if (len / P > t.columns) atomicOr(&too_long, 1);
+    const Sums entries = sums_of(len / P, part);
+    start[tid] = entries.before;
+    row[tid] = slot;
+    __syncthreads();
+    for (int i = tid; i < entries.all; i += CTRL) {
+        const int s = last_from(start, t.S, i);
+        const int page = f.table[(size_t)row[s] * f.columns + (i - start[s])];
+        if (page >= 0 && page < f.pages) __hip_atomic_fetch_add(&marks[page], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    int used = 0;
+    for (int p0 = 0; p0 < f.pages; p0 += CTRL) {
+        const int p = p0 + tid, held = p < f.pages ? __hip_atomic_load(&marks[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+        __syncthreads();
+        const Sums at = sums_of(held > 0, part);
+        const int place = used + at.before;
+        if (p < f.pages) marks[p] = held > 0 ? place : -1;
+        if (held > 0 && place < t.pages) {
+            list[place] = p;
+            t.refs[place] = held;
+        }
+        used += at.all;
+    }
+    __syncthreads();
+    const bool fits = used <= t.pages && !too_long;
+    for (int p = (fits ? used : 0) + tid; p < t.pages; p += CTRL) t.refs[p] = 0;
+    if (tid < t.S) {
+        t.slot[tid] = tid;
+        t.len[tid] = fits ? len : 0;
+        plans(t)[tid] = Plan{fits ? len : 0, has && fits, tid, slot};
+    }
+    if (tid == 0) {
+        t.own[OWN_LOW] = t.own[OWN_COUNT] = fits ? used : 0;
+        if (a.n_used) *a.n_used = used;
+    }
+}
+
+// Blocks over the pages of a layer, then over the tails of its streams and heads, then (in the first layer) over the table.
+template <int D>
+__global__ __launch_bounds__(256) void copy_move(const CopyArgs a, int page_blocks, int tail_blocks)
+{
+    const CacheArgs &f = a.from, &t = a.to;
+    const int tid = threadIdx.x, l = blockIdx.y, b = blockIdx.x;
+    if (b < page_blocks) {
+        if (b >= t.own[OWN_COUNT]) return;
+        const int page = t.own[OWN_PLAN + (PLAN_WORDS + 1) * t.S + b];
+        const size_t src = ((size_t)l * f.pages + page) * f.H, dst = ((size_t)l * t.pages + b) * t.H;
+        const u32x4 *const ks = reinterpret_cast<const u32x4 *>(f.k + src * P * D), *const vs = reinterpret_cast<const u32x4 *>(f.v + src * P * D);
+        u32x4 *const kt = reinterpret_cast<u32x4 *>(t.k + dst * P * D), *const vt = reinterpret_cast<u32x4 *>(t.v + dst * P * D);
+        for (int i = tid; i < f.H * (P * D / 16); i += 256) {
+            kt[i] = ks[i];
+            vt[i] = vs[i];
+        }
+        for (int h = tid; h < f.H; h += 256) {
+            t.k_scale[dst + h] = f.k_scale[src + h];
+            t.v_scale[dst + h] = f.v_scale[src + h];
+        }
+    } else if (b < page_blocks + tail_blocks) {
+        const int unit = b - page_blocks, s = unit / t.H, h = unit - s * t.H;
+        const Plan plan = plans(t)[s];
+        const int n = plan.count ? plan.first % P : 0;
+        const size_t src = (((size_t)l * f.S + plan.other) * f.H + h) * P * D, dst = (((size_t)l * t.S + s) * t.H + h) * P * D;
+        for (int i = tid; i < n * (D / 8); i += 256) {
+            reinterpret_cast<u32x4 *>(t.k_tail + dst)[i] = reinterpret_cast<const u32x4 *>(f.k_tail + src)[i];
+            reinterpret_cast<u32x4 *>(t.v_tail + dst)[i] = reinterpret_cast<const u32x4 *>(f.v_tail + src)[i];
+        }
+    } else if (l == 0) {
+        const int *const marks = f.own + OWN_PLAN + (PLAN_WORDS + 1) * f.S;
+        const long long i = (long long)(b - page_blocks - tail_blocks) * 256 + tid;
+        const int s = (int)(i / t.columns), column = (int)(i - (long long)s * t.columns);
+        if (s >= t.S) return;
+        const Plan plan = plans(t)[s];
+        int page = -1;
+        if (plan.count && column < plan.first / P) page = f.table[(size_t)plan.other * f.columns + column];
+        t.table[i] = page >= 0 && page < f.pages ? marks[page] : -1;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+bool misaligned(const void *p, unsigned mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; }
+
+CacheArgs args_of(const mlora_page_cache *c)
+{
+    return CacheArgs{reinterpret_cast<int8_t *>(c->k), reinterpret_cast<int8_t *>(c->v), c->k_scale, c->v_scale,
+                     reinterpret_cast<uint16_t *>(c->k_tail), reinterpret_cast<uint16_t *>(c->v_tail), c->slot, c->len, c->table, c->refs, c->own,
+                     c->n_layers, c->n_streams, c->n_kv_heads, c->head_dim, c->n_pages, c->max_pages};
+}
+
+}  // namespace
+
+mlora_status check_page_cache(const mlora_page_cache *c)
+{
+    if (!c) return MLORA_EINVAL;
+    if (c->head_dim != 64 && c->head_dim != 128) return MLORA_ESHAPE;
+    if (c->n_layers <= 0 || c->n_streams <= 0 || c->n_kv_heads <= 0 || c->n_pages <= 0 || c->max_pages <= 0) return MLORA_ESHAPE;
+    if (c->n_streams > MLORA_PAGE_MAX_STREAMS || c->n_pages > MLORA_PAGE_MAX_PAGES || c->max_pages > MLORA_PAGE_MAX_COLUMNS) return MLORA_ESHAPE;
+    if ((double)c->n_layers * c->n_streams * c->n_kv_heads > MLORA_PAGE_MAX_HEADS || c->n_layers > 65535) return MLORA_ESHAPE;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail || !c->slot || !c->len || !c->table || !c->refs || !c->own)
+        return MLORA_EINVAL;
+    for (const void *p : {(const void *)c->k, (const void *)c->v, (const void *)c->k_tail, (const void *)c->v_tail})
+        if (misaligned(p, 15u)) return MLORA_EALIGN;
+    for (const void *p : {(const void *)c->k_scale, (const void *)c->v_scale, (const void *)c->slot, (const void *)c->len, (const void *)c->table,
+                          (const void *)c->refs, (const void *)c->own})
+        if (misaligned(p, 3u)) return MLORA_EALIGN;
+    return MLORA_OK;
+}
+
+}  // namespace mlora
+
+using namespace mlora;
+
+extern "C" {
+
+size_t mlora_page_cache_own_words(int32_t n_streams, int32_t n_pages)
+{
+    if (n_streams <= 0 || n_streams > MLORA_PAGE_MAX_STREAMS || n_pages <= 0 || n_pages > MLORA_PAGE_MAX_PAGES) return 0;
+    return (size_t)OWN_PLAN + (size_t)(PLAN_WORDS + 1) * n_streams + n_pages;
+}
+
+mlora_status mlora_page_cache_append(const mlora_page_cache *c, const void *k_new, const void *v_new, int32_t rows_per_stream,
+                                     const int32_t *rows, int32_t n_rows, int32_t *appended, void *stream)
+{
+    const mlora_status st = check_page_cache(c);
+    if (st != MLORA_OK) return st;
+    if (!k_new || !v_new) return MLORA_EINVAL;
+    if (misaligned(k_new, 15u) || misaligned(v_new, 15u) || misaligned(rows, 3u) || misaligned(appended, 3u)) return MLORA_EALIGN;
+    if (rows_per_stream <= 0 || (long long)c->n_streams * rows_per_stream > MLORA_MAX_ROWS) return MLORA_ESHAPE;
+    const int n = rows ? n_rows : rows_per_stream;
+    if (n < 1 || n > rows_per_stream) return MLORA_ESHAPE;
+    const AppendArgs a{args_of(c), reinterpret_cast<const uint16_t *>(k_new), reinterpret_cast<const uint16_t *>(v_new), rows, appended, rows_per_stream, n};
+    hipStream_t s = (hipStream_t)stream;
+    append_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
+    const dim3 grid((unsigned)(c->n_layers * c->n_streams * c->n_kv_heads), (unsigned)((P - 1 + n) / P));
+    if (c->head_dim == 64) append_rows<64><<<grid, dim3(256), 0, s>>>(a);
+    else                   append_rows<128><<<grid, dim3(256), 0, s>>>(a);
+    return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
+}
+
+mlora_status mlora_page_cache_reorder(const mlora_page_cache *c, const int32_t *source, int32_t window, int32_t sink, void *stream)
+{
+    const mlora_status st = check_page_cache(c);
+    if (st != MLORA_OK) return st;
+    if (misaligned(source, 3u)) return MLORA_EALIGN;
+    if (window < 0 || sink < 0) return MLORA_ESHAPE;
+    const ReorderArgs a{args_of(c), source, window, sink};
+    hipStream_t s = (hipStream_t)stream;
+    reorder_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
+    const int table_blocks = (c->max_pages + 255) / 256;
+    const dim3 grid((unsigned)(table_blocks + c->n_layers * c->n_kv_heads), (unsigned)c->n_streams);
+    if (c->head_dim == 64) reorder_move<64><<<grid, dim3(256), 0, s>>>(a, table_blocks);
+    else                   reorder_move<128><<<grid, dim3(256), 0, s>>>(a, table_blocks);
+    return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
+}
+
+mlora_status mlora_page_cache_copy(const mlora_page_cache *from, const mlora_page_cache *to, const int32_t *source, int32_t *n_used, void *stream)
+{
+    mlora_status st = check_page_cache(from);
+    if (st == MLORA_OK) st = check_page_cache(to);
+    if (st != MLORA_OK) return st;
+    if (!source) return MLORA_EINVAL;
+    if (misaligned(source, 3u) || misaligned(n_used, 3u)) return MLORA_EALIGN;
+    if (from->n_layers != to->n_layers || from->n_kv_heads != to->n_kv_heads || from->head_dim != to->head_dim) return MLORA_ESHAPE;
+    if (from->k == to->k || from->v == to->v || from->k_scale == to->k_scale || from->v_scale == to->v_scale || from->k_tail == to->k_tail
+        || from->v_tail == to->v_tail || from->slot == to->slot || from->len == to->len || from->table == to->table || from->refs == to->refs
+        || from->own == to->own) return MLORA_EINVAL;
+    const CopyArgs a{args_of(from), args_of(to), source, n_used};
+    hipStream_t s = (hipStream_t)stream;
+    copy_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
+    const int page_blocks = std::min(from->n_pages, to->n_pages), tail_blocks = to->n_streams * to->n_kv_heads;
+    const long long entries = (long long)to->n_streams * to->max_pages;
+    const dim3 grid((unsigned)(page_blocks + tail_blocks + (entries + 255) / 256), (unsigned)to->n_layers);
+    if (to->head_dim == 64) copy_move<64><<<grid, dim3(256), 0, s>>>(a, page_blocks, tail_blocks);
+    else                    copy_move<128><<<grid, dim3(256), 0, s>>>(a, page_blocks, tail_blocks);
+    return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
+}
+
+}  // extern "C"

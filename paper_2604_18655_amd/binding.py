@@ -601,7 +601,7 @@ class Ds2dStep:
 
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS = 0, 1, 2, 3
-_EINVAL, _ESHAPE = -1, -2
+_EINVAL, _ESHAPE, _EWORKSPACE = -1, -2, -4
 
 
 class _Kind:

@@ -165,13 +165,28 @@ __device__ __forceinline__ unsigned top_bits(const u32x4 &x, unsigned top)
     for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7FFFu, x[i] >> 16 & 0x7FFFu));
     return top;
 }
-__device__ __forceinline__ u32x2 codes_of(const u32x4 &x, float top)
+// Codes of 8 numbers.  All are moved by the power of two that brings `top` into [1/2, 1), since 127 x may not be a number.  127 x / top is a quotient of
+// numbers of 15 and 8 bits: it is a half, which one correction of the product with the reciprocal gives exactly, or further from one than
+// 2^-17, and the codes are those of the exact quotient.
+struct Divide {
+    float top, inverse;
+    int shift;
+};
+__device__ __forceinline__ Divide divide_by(unsigned bits)
+{
+    const float top = bf16_bits_to_float(bits);
+    const int e = __builtin_amdgcn_frexp_expf(top);
+    const float t = __builtin_ldexpf(top, -e);
+    return Divide{t, __builtin_amdgcn_rcpf(t), -e};
+}
+__device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &by)
 {
     u32x2 out = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float f = bf16_bits_to_float(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu);
-        out[i / 4] |= ((unsigned)(int)rintf(127.f * f / top) & 0xFFu) << 8 * (i % 4);
+        const float f = 127.f * __builtin_ldexpf(bf16_bits_to_float(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu), by.shift), near = f * by.inverse;
+        const float quotient = __builtin_fmaf(__builtin_fmaf(-near, by.top, f), by.inverse, near);
+        out[i / 4] |= ((unsigned)(int)rintf(quotient) & 0xFFu) << 8 * (i % 4);
     }
     return out;
 }
@@ -221,18 +236,18 @@ __global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
         const int page = min(max(c.table[(size_t)plan.slot * c.columns + full + j], 0), c.pages - 1);
         const size_t unit = ((size_t)l * c.pages + page) * c.H + h;
         const bool k_ok = kt > 0 && kt < 0x7F80u, v_ok = vt > 0 && vt < 0x7F80u;
-        const float k_top = bf16_bits_to_float(kt), v_top = bf16_bits_to_float(vt);
+        const Divide k_by = divide_by(kt), v_by = divide_by(vt);
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
             const int piece = u * 256 + tid, g = piece / PIECES, f = piece % PIECES * 8;
-            *reinterpret_cast<u32x2 *>(c.k + (unit * P + g) * D + f) = k_ok ? codes_of(kx[u], k_top) : u32x2{0, 0};
-            const u32x2 v = v_ok ? codes_of(vx[u], v_top) : u32x2{0, 0};
+            *reinterpret_cast<u32x2 *>(c.k + (unit * P + g) * D + f) = k_ok ? codes_of(kx[u], k_by) : u32x2{0, 0};
+            const u32x2 v = v_ok ? codes_of(vx[u], v_by) : u32x2{0, 0};
 #pragma unroll
             for (int e = 0; e < 8; ++e) turned[(f + e) * PITCH + g] = (unsigned char)(v[e / 4] >> 8 * (e % 4));
         }
         if (tid == 0) {
-            c.k_scale[unit] = kt < 0x7F80u ? k_top / 127.f : __builtin_nanf("");
-            c.v_scale[unit] = vt < 0x7F80u ? v_top / 127.f : __builtin_nanf("");
+            c.k_scale[unit] = kt < 0x7F80u ? bf16_bits_to_float(kt) / 127.f : __builtin_nanf("");
+            c.v_scale[unit] = vt < 0x7F80u ? bf16_bits_to_float(vt) / 127.f : __builtin_nanf("");
         }
         __syncthreads();
         for (int i = tid; i < D * P / 16; i += 256)

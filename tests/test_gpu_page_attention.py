@@ -1,0 +1,226 @@
+"""Attention over the paged cache on the GPU against float64, to bounds counted from roundings.
+
+Scores: a query vector's numbers are cut at 2^-22 of its largest, which moves a score by at most scale * max |q| * sum |k| * 2^-22; products of bf16
+(tail, rows) and the conversions, scales and exponents around them are fp32: D + 16 roundings of 2^-24 of sum |q k| * scale.  Each moves a
+weighted mean by twice itself.  Weights: on pages cut at 2^-24 of the page's largest, 64 of them, twice; in the tail two bf16 halves
+(2^-18, with the sum's own roundings 2^-16).  Sums: a rounding of 2^-23 per item and merge."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import beams as O
+from test_gpu_page_cache import bits, make, upload
+
+pytestmark = pytest.mark.gpu
+
+
+def bound(size, q, scale, D, items, want, fp32):
+    vmax, s1, k1 = size[..., 0], size[..., 1], size[..., 2]
+    qmax = np.abs(q).max(-1)
+    far = 2 * (abs(scale) * k1 * qmax * 2.0 ** -22 + (D + 16) * 2.0 ** -24 * s1) + 2.0 ** -16 + 128 * 2.0 ** -24 + (items + 32) * 2.0 ** -23
+    return (vmax * far)[..., None] + (0 if fp32 else np.abs(want) * 2.0 ** -8)
+
+
+def run(gpu, c, layer, q, k_new, v_new, parent, R, scale, window=0, sink=0, fp32=True, stream=None):
+    lib, _, torch = gpu
+    _, cache = upload(gpu, c)
+    on = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (q, k_new, v_new, np.asarray(parent, np.int32))]
+    op = lib.PageAttention(cache, layer, q.shape[1], R, scale, on[1], on[2], on[3], window, sink)
+    out = torch.empty(q.shape, dtype=torch.float32 if fp32 else torch.bfloat16).cuda()
+    ws = torch.full((op.workspace_bytes(),), 0xFF, dtype=torch.uint8).cuda()             # (nothing in it counts)
+    op.run(on[0], out, lib.Y_FP32 if fp32 else lib.Y_BF16, ws)
+    torch.cuda.synchronize()
+    first = out.double().cpu().numpy()
+    op.run(on[0], out, lib.Y_FP32 if fp32 else lib.Y_BF16, ws)
+    torch.cuda.synchronize()
+    assert np.array_equal(first, out.double().cpu().numpy(), equal_nan=True)             # the same from call to call
+    return first, op
+
+
+def check(gpu, seed, lengths, R, H, G, D, window=0, sink=0, fp32=True, L=1, columns=None, share=None, q_scale=1.5, tree=True, scale=None):
+    rng = np.random.default_rng(seed)
+    S, need = len(lengths), sum(n // 64 for n in lengths)
+    columns = columns or max(lengths) // 64 + 1
+    c = make(seed, L, S, H, D, need + 3, columns, lengths)
+    if share:
+        c = O.reorder(c, share)
+    scale = D ** -0.5 if scale is None else scale
+    q, k, v = bits(rng, S * R, H * G, D, scale=q_scale), bits(rng, S * R, H, D), bits(rng, S * R, H, D)
+    parent = np.array([[rng.integers(-1, max(r, 1)) if r and tree else r - 1 for r in range(R)] for _ in range(S)]).reshape(-1)
+    layer = int(rng.integers(0, L))
+    got, op = run(gpu, c, layer, q, k, v, parent, R, scale, window, sink, fp32)
+    want, size = O.attention(c, layer, q, k, v, parent, R, float(np.float32(scale)), window, sink)
+    assert np.all(np.isfinite(got))
+    items = max(lengths) // 64 + 5
+    assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), scale, D, items, want, fp32))
+    return op.plan()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("length", [0, 1, 31, 32, 33, 63, 64, 65, 127, 128, 1000])
+def test_one_token(gpu, D, length):
+    check(gpu, length, [length], 1, 2, 3, D)
+
+
+@pytest.mark.parametrize("R,G", [(1, 1), (1, 8), (2, 8), (3, 5), (5, 3), (16, 1), (17, 1), (30, 4), (33, 1), (64, 8), (64, 1)])
+def test_rows_and_heads(gpu, R, G):
+    check(gpu, R * 10 + G, [100, 321, 64], R, 2, G, 64, fp32=R % 2 == 1)
+
+
+@pytest.mark.parametrize("window,sink", [(1, 0), (2, 1), (33, 0), (64, 64), (65, 5), (100, 70), (300, 200), (10000, 3), (7, 10000)])
+@pytest.mark.parametrize("R", [1, 40])
+def test_windows(gpu, window, sink, R):
+    check(gpu, window + sink + R, [700, 64, 130, 5, 0, 449], R, 2, 4, 64, window, sink)
+    check(gpu, window + sink + R + 1, [333, 200], R, 1, 2, 128, window, sink, tree=False)
+
+
+def test_layers_and_shared_pages(gpu):
+    check(gpu, 1, [400, 200, 64, 70], 3, 3, 2, 64, L=4, share=[0, 0, 0, 1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_pages(gpu, D):
+    plan = check(gpu, 2, [6000, 10], 1, 2, 4, D)
+    assert plan["splits"] > 1
+    check(gpu, 3, [9000], 20, 1, 4, D, fp32=False)
+
+
+def test_a_table_far_longer_than_the_stream(gpu):
+    plan = check(gpu, 4, [70, 3, 0], 2, 2, 4, 64, columns=3000)
+    assert plan["splits"] > 1
+
+
+@pytest.mark.parametrize("q_scale", [1e-30, 1e-3, 40.0])
+def test_sharp_and_flat(gpu, q_scale):
+    check(gpu, 5, [500, 130], 3, 2, 2, 64, q_scale=q_scale)
+
+
+def test_scales_of_either_sign(gpu):
+    check(gpu, 6, [300], 2, 1, 2, 64, scale=-0.2)
+    check(gpu, 7, [300], 2, 1, 2, 64, scale=0.0)
+
+
+def test_means_of_equal_values(gpu):
+    """All keys alike: every weight is the same, and a mean of equal numbers is that number."""
+    lib, _, torch = gpu
+    c = make(8, 1, 1, 1, 64, 5, 5, [200])
+    c["k"][:], c["v"][:], c["v_scale"][:] = 3, 64, 0.03125
+    c["k_scale"][:] = 0.5
+    c["k_tail"][:], c["v_tail"][:] = 0x3FC0, 0x4000                                      # 1.5 and 2
+    q = np.full((1, 4, 64), 0x3F80, np.int16)
+    new = [np.full((1, 1, 64), x, np.int16) for x in (0x3FC0, 0x4000)]
+    got, _ = run(gpu, c, 0, q, *new, [-1], 1, 0.125)
+    assert np.all(np.abs(got - 2.0) <= 2.0 * 4 * 2.0 ** -23)                             # page, tail, merge and quotient
+
+
+def test_what_a_row_does_not_see_does_not_touch_it(gpu):
+    """Infinities and NaN behind the window, on other branches, behind the tail's end, in pages that only others hold."""
+    rng = np.random.default_rng(9)
+    R, H, G, D = 6, 2, 2, 64
+    c = make(9, 1, 2, H, D, 12, 5, [300, 200])
+    parent = [-1, 0, 1, 0, 3, 3, -1, 0, 0, 0, 0, 0]
+    q, k, v = bits(rng, 2 * R, H * G, D), bits(rng, 2 * R, H, D), bits(rng, 2 * R, H, D)
+    # the first 2 pages and the tail's rest are poison, and so are rows 1 (seen by 2) and 5 of stream 0
+    for s in range(2):
+        for i in range(2):
+            p = c["table"][c["slot"][s], i]
+            c["k_scale"][:, p], c["v_scale"][:, p] = math.nan, math.nan
+            c["k"][:, p], c["v"][:, p] = 0, 0
+        c["k_tail"][:, c["slot"][s], :, c["len"][s] % 64:], c["v_tail"][:, c["slot"][s], :, c["len"][s] % 64:] = 0x7FC0, 0x7F80
+    k[1], v[5, 0, 3], v[1, 1, 7] = 0x7FC0, 0x7F80, 0x7FC0
+    window, sink = 60, 0
+    got, _ = run(gpu, c, 0, q, k, v, parent, R, 0.125, window, sink)
+    want, size = O.attention(c, 0, q, k, v, parent, R, 0.125, window, sink)
+    clean = np.array([r not in (1, 2, 5) for r in range(2 * R)])
+    assert np.all(np.isfinite(want[clean])) and np.all(np.isfinite(got[clean]))
+    assert np.all(np.abs(got[clean] - want[clean]) <= bound(size, O.bf16(q), 0.125, D, 9, want, True)[clean])
+    assert np.all(np.isnan(got[1])) and np.all(np.isnan(got[2]))                         # NaN among the scores
+    odd = np.zeros(D, bool)
+    odd[3] = True
+    assert np.all(got[5, :G][:, odd] == math.inf) and np.all(np.isfinite(got[5, :G][:, ~odd])) and np.all(np.isfinite(got[5, G:]))
+    # seen from a wider window all is NaN, in every feature
+    got, _ = run(gpu, c, 0, q, k, v, parent, R, 0.125, 400)
+    assert np.all(np.isnan(got))
+
+
+def test_values_of_nan_alone(gpu):
+    """A page whose keys are numbers and whose values are not: NaN for those that see one of its tokens, in every feature."""
+    rng = np.random.default_rng(10)
+    c = make(10, 1, 1, 1, 64, 6, 5, [200])
+    c["v_scale"][:, c["table"][c["slot"][0], 0]] = math.nan
+    q, k, v = bits(rng, 3, 1, 64), bits(rng, 3, 1, 64), bits(rng, 3, 1, 64)
+    for window, sink, bad in ((0, 0, [0, 1, 2]), (138, 0, [0]), (137, 0, []), (10, 1, [0, 1, 2])):
+        got, _ = run(gpu, c, 0, q, k, v, [-1, 0, 1], 3, 0.125, window, sink)             # rows at 200, 201, 202: the page is 0 .. 63
+        assert [r for r in range(3) if np.any(np.isnan(got[r]))] == bad
+        assert all(np.all(np.isnan(got[r])) for r in bad)
+
+
+@pytest.mark.parametrize("odd", [0x7FC0, 0x7F80, 0xFF80])
+def test_query_vectors_that_are_not_finite(gpu, odd):
+    rng = np.random.default_rng(11)
+    c = make(11, 1, 1, 2, 64, 6, 5, [200])
+    q, k, v = bits(rng, 4, 4, 64), bits(rng, 4, 2, 64), bits(rng, 4, 2, 64)
+    q.view(np.uint16)[1, 2, 17] = odd
+    want, size = O.attention(c, 0, q, k, v, [-1, 0, 1, 2], 4, 0.125)
+    got, _ = run(gpu, c, 0, q, k, v, [-1, 0, 1, 2], 4, 0.125)
+    assert np.all(np.isnan(got[1, 2]))
+    got[1, 2] = want[1, 2] = 0
+    q[1, 2] = 0
+    assert np.all(np.abs(got - want) <= bound(np.nan_to_num(size), O.bf16(q), 0.125, 64, 9, want, True))
+
+
+def test_pages_that_are_not_there(gpu):
+    rng = np.random.default_rng(12)
+    c = make(12, 1, 2, 2, 64, 20, 8, [450, 300])
+    c["table"][c["slot"][0], 2], c["table"][c["slot"][0], 5], c["table"][c["slot"][1], :] = -1, 20, -1
+    q, k, v = bits(rng, 4, 4, 64), bits(rng, 4, 2, 64), bits(rng, 4, 2, 64)
+    want, size = O.attention(c, 0, q, k, v, [-1, 0] * 2, 2, 0.125, 420, 3)
+    got, _ = run(gpu, c, 0, q, k, v, [-1, 0] * 2, 2, 0.125, 420, 3)
+    assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), 0.125, 64, 12, want, True))
+
+
+def test_lengths_outside_the_table(gpu):
+    """They count as the nearer end."""
+    rng = np.random.default_rng(13)
+    c = make(13, 1, 2, 1, 64, 20, 4, [4 * 64 + 63, 0])
+    q, k, v = bits(rng, 2, 1, 64), bits(rng, 2, 1, 64), bits(rng, 2, 1, 64)
+    want, _ = run(gpu, c, 0, q, k, v, [-1, -1], 1, 0.125)
+    c["len"][:] = [1 << 30, -5]
+    got, _ = run(gpu, c, 0, q, k, v, [-1, -1], 1, 0.125)
+    assert np.array_equal(got, want)
+
+
+def test_offsets_past_32_bits(gpu):
+    lib, _, torch = gpu
+    pages, H, D = 36000, 16, 64
+    rng = np.random.default_rng(14)
+    cache = lib.PageCache.empty(1, 1, H, D, pages, 4)
+    cache.refs[:-3] = 1
+    k, v = (bits(rng, 1, 200, H, D) for _ in range(2))
+    cache.append(torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), 200)
+    assert cache.table.tolist() == [[pages - 3, pages - 2, pages - 1, -1]]
+    c, _ = O.append(O.empty_cache(1, 1, H, D, 3, 4), k, v, 200)
+    q, kn, vn = bits(rng, 1, H, D), bits(rng, 1, H, D), bits(rng, 1, H, D)
+    on = [torch.from_numpy(x).cuda() for x in (q, kn, vn)]
+    op = lib.PageAttention(cache, 0, H, 1, 0.125, on[1], on[2], torch.tensor([-1], dtype=torch.int32).cuda())
+    out, ws = torch.empty((1, H, D)).cuda(), torch.empty(op.workspace_bytes(), dtype=torch.uint8).cuda()
+    op.run(on[0], out, lib.Y_FP32, ws)
+    want, size = O.attention(c, 0, q, kn, vn, [-1], 1, 0.125)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound(size, O.bf16(q), 0.125, D, 9, want, True))
+
+
+def test_what_is_appended_is_seen_alike(gpu):
+    """Rows of a step, then the same tokens in the tail: as long as no page fills, the next row sees the same numbers."""
+    lib, _, torch = gpu
+    rng = np.random.default_rng(15)
+    H, G, D, R = 2, 4, 64, 7
+    c = make(15, 1, 1, H, D, 8, 5, [130])
+    q, k, v = bits(rng, R, H * G, D), bits(rng, R, H, D), bits(rng, R, H, D)
+    tree, _ = run(gpu, c, 0, q, k, v, np.arange(-1, R - 1), R, 0.125)
+    for r in range(1, R):
+        d, _ = O.append(c, k[None], v[None], R, [list(range(r)) + [-1] * (R - r)])
+        one, _ = run(gpu, d, 0, q[r:r + 1], k[r:r + 1], v[r:r + 1], [-1], 1, 0.125)
+        # both are within their bounds of one number
+        want, size = O.attention(d, 0, q[r:r + 1], k[r:r + 1], v[r:r + 1], [-1], 1, 0.125)
+        assert np.all(np.abs(one[0] - tree[r]) <= 2 * bound(size, O.bf16(q[r:r + 1]), 0.125, D, 9, want, True)[0])

@@ -18,6 +18,7 @@ constexpr int CHUNK = 64, SLICE = 64 * CHUNK;            // tokens
 constexpr int PICK = 1024;                               // threads of beam_pick
 constexpr int W_MAX = MLORA_BEAM_MAX_BEAMS;
 constexpr int LIST = W_MAX * CHUNK;                      // candidates that are ranked at once
+constexpr int HELD = 8;                                  // loads of beam_pick at once
 constexpr float NONE = -__builtin_inff();
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -30,10 +31,10 @@ struct BeamArgs {
     int *source, *token;
     float *score_out;
     int *length_out, *finished_out;
-    float *chunk_top;                                    // [rows][chunks]
+    float *chunk_top;                                    // [rows][slices][64]: -infinity behind the vocabulary
     float *slice_top;                                    // [rows][slices]
     double *slice_sum;                                   // [rows][slices], of exp(logit - slice_top)
-    int W, V, chunks, slices, eos, pad;
+    int W, V, slices, eos, pad;
     float power;
 };
 
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256) void beam_stats(const BeamArgs a)
         most = max_with<0x4E>(most);
         most = max_with<0x141>(most);
         if constexpr (FP32) most = max_with<0x140>(most);
-        if (lane % (CHUNK / E) == 0 && v < a.V) a.chunk_top[(size_t)row * a.chunks + v / CHUNK] = most;
+        if (lane % (CHUNK / E) == 0) a.chunk_top[(size_t)row * a.slices * 64 + v / CHUNK] = most;
         top = fmaxf(top, most);
     }
 #pragma unroll
@@ -102,26 +103,13 @@ __global__ __launch_bounds__(256) void beam_stats(const BeamArgs a)
 }
 
 struct Beam {
-    double score, lse, len;                              // len: what the score of its candidates is divided by
+    double score, lse, per;                              // per: what the score of its candidates is multiplied by
     int finished, live, tokens;                          // tokens: of its candidates
 };
 // What beam b makes of a logit; -infinity: no candidate
 __device__ __forceinline__ double ranked(const Beam &b, float z)
 {
-    if (!b.live || !(z > NONE)) return (double)NONE;
-    return (b.finished ? b.score : b.score + ((double)z - b.lse)) / b.len;
-}
-struct Candidate {
-    double rank;
-    float z;
-    int beam, at;                                        // chunk, or token
-};
-__device__ __forceinline__ bool before(const Candidate &x, const Candidate &y)
-{
-    if (x.rank != y.rank) return x.rank > y.rank;
-    if (x.beam != y.beam) return x.beam < y.beam;
-    if (x.z != y.z) return x.z > y.z;
-    return x.at < y.at;
+    return b.live && z > NONE ? (b.finished ? b.score : b.score + ((double)z - b.lse)) * b.per : (double)NONE;
 }
 // numbers, -infinity among them, as integers that order like them
 __device__ __forceinline__ int in_order(float f)
@@ -129,92 +117,210 @@ __device__ __forceinline__ int in_order(float f)
     const int b = __float_as_int(f + 0.f);
     return b < 0 ? b ^ 0x7FFFFFFF : b;
 }
+__device__ __forceinline__ long long in_order(double f)
+{
+    const long long b = __double_as_longlong(f + 0.);
+    return b < 0 ? b ^ 0x7FFFFFFFFFFFFFFFll : b;
+}
+struct Candidate {
+    long long rank;
+    float z;
+    int beam, at;                                        // at: chunk, or token
+};
+__device__ __forceinline__ bool later(const Candidate &x, const Candidate &y)        // of equal rank: x behind y
+{
+    if (x.beam != y.beam) return x.beam > y.beam;
+    if (x.z != y.z) return x.z < y.z;
+    return x.at > y.at;
+}
+__device__ __forceinline__ bool before(const Candidate &x, const Candidate &y)
+{
+    return x.rank > y.rank || (x.rank == y.rank && later(y, x));
+}
 
+struct List {
+    long long rank[LIST];
+    float z[LIST];
+    int beam[LIST], at[LIST], number[LIST];
+    int found;
+    __device__ Candidate get(int i) const { return Candidate{rank[i], z[i], beam[i], at[i]}; }
+    __device__ void put(const Candidate &x)
+    {
+        const int i = atomicAdd(&found, 1);
+        if (i < LIST) rank[i] = x.rank, z[i] = x.z, beam[i] = x.beam, at[i] = x.at;
+    }
+};
+// The W best of a list of m <= LIST, each in its place.  Every wave looks at 64 of them and at a share of all.
+__device__ __forceinline__ void best_of(List &list, int m, int W, Candidate *best)
+{
+    const int tid = threadIdx.x;
+    int per = 64;
+    while (per < m && per < PICK) per *= 2;
+    for (int i = tid; i < m; i += PICK) list.number[i] = 0;
+    __syncthreads();
+    for (int i = tid & (per - 1); i < m; i += per) {
+        const Candidate mine = list.get(i);
+        int number = 0;
+#pragma unroll 4
+        for (int j = tid / per; j < m; j += PICK / per) {
+            const long long other = list.rank[j];
+            if (other > mine.rank) ++number;
+            else if (other == mine.rank && j != i) number += later(mine, list.get(j));
+        }
+        if (number) atomicAdd(&list.number[i], number);
+    }
+    __syncthreads();
+    for (int i = tid; i < m; i += PICK)
+        if (list.number[i] < W) best[list.number[i]] = list.get(i);
+    __syncthreads();
+}
+
+// A wave's shares are of one beam (two, if there are more beams than waves), so ranks are made for few of them: a bound on ranks is one on the logits of
+// a beam.  Both passes over the chunks' best logits take four per lane and load.
 template <bool FP32>
 __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
 {
+    constexpr int WAVES = PICK / 64;
     __shared__ Beam beams[W_MAX];
-    __shared__ Candidate list[LIST];
-    __shared__ Candidate best[W_MAX];
-    __shared__ int found, at_least;
-    __shared__ Candidate wave_best[PICK / 64], winners[W_MAX];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, W = a.W, row0 = (int)blockIdx.x * W;
-    for (int b = wave; b < W; b += PICK / 64) {
-        const int row = row0 + b, done = a.finished[row];
+    __shared__ List list;
+    __shared__ Candidate best[W_MAX], wave_best[WAVES];
+    __shared__ int at_least;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), W = a.W, row0 = (int)blockIdx.x * W;
+    // shares: `parts` waves per beam, its groups of four chunks dealt out in runs
+    const int parts = W < WAVES ? WAVES / W : 1, quads = a.slices * 16, run = (quads + parts - 1) / parts;
+    struct Share {
+        const f32x4 *tops;
+        int beam, first, n;                              // groups from first on
+    };
+    const auto share_of = [&](int t) {
+        const int b = t / parts, first = (t - b * parts) * run;
+        return Share{reinterpret_cast<const f32x4 *>(a.chunk_top) + (size_t)(row0 + b) * quads + first, b, first, min(run, quads - first)};
+    };
+    const auto load = [&](const Share &s, int q0, f32x4 (&z)[HELD]) {
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const int q = q0 + u * 64 + lane;
+            z[u] = f32x4{NONE, NONE, NONE, NONE};
+            if (q < s.n) z[u] = s.tops[q];
+        }
+    };
+    // (asked for before anything else; kept where a wave has no more than that)
+    f32x4 z[HELD];
+    const bool all = W * parts <= WAVES && run <= 64 * HELD;
+    load(share_of(min(wave, W * parts - 1)), 0, z);
+    const auto top_of = [&](const f32x4 &z) { return fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])); };
+
+    for (int b = wave; b < W; b += WAVES) {
+        const int row = row0 + b, done = a.finished[row], tokens = a.length[row] + (done ? 0 : 1);
+        const float score = a.score[row];
         const float *const tops = a.slice_top + (size_t)row * a.slices;
         const double *const sums = a.slice_sum + (size_t)row * a.slices;
         float top = NONE;
-        if (!done)
-            for (int i = lane; i < a.slices; i += 64) top = fmaxf(top, tops[i]);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
         double sum = 0.;
-        if (!done)
-            for (int i = lane; i < a.slices; i += 64) sum += sums[i] * exp((double)tops[i] - (double)(top == NONE ? 0.f : top));
+        for (int i0 = 0; i0 < a.slices; i0 += 64) {      // (rows of finished beams hold anything)
+            const int i = i0 + lane;
+            const float here = i < a.slices ? tops[i] : NONE;
+            const double part = i < a.slices ? sums[i] : 0.;
+            float next = fmaxf(top, here);
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) next = fmaxf(next, __shfl_xor(next, d));
+            const float from = next == NONE ? 0.f : next;
+            sum = sum * exp((double)top - (double)from) + part * exp((double)here - (double)from);
+            top = next;
+        }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        if (lane == 0) {
-            const float score = a.score[row];
-            const double lse = (double)top + log(sum);
-            const int tokens = a.length[row] + (done ? 0 : 1);
-            beams[b] = Beam{score, lse, pow(fmax(1., (double)tokens), (double)a.power), done, isfinite(score) && (done || isfinite(lse)), tokens};
-        }
+        const double logs = log(lane == 1 ? fmax(1., (double)tokens) : sum), lse = (double)top + logs;
+        const double per = a.power == 0.f ? 1. : exp(-(double)a.power * __shfl(logs, 1));
+        if (lane == 0) beams[b] = Beam{score, lse, per, done, isfinite(score) && (done || isfinite(lse)), tokens};
     }
-    if (tid == 0) found = 0, at_least = in_order(NONE);
+    if (tid == 0) list.found = 0, at_least = in_order(NONE);
     __syncthreads();
 
     // The W best chunks.  Of each wave's 64 lanes, the W-th best best chunk: that many chunks are at least as good, so nothing below the largest
     // such bound of all waves counts.
-    const int n = W * a.chunks;
-    const auto chunk_at = [&](int i) {
-        const int b = i / a.chunks, c = i - b * a.chunks;
-        Candidate x{(double)NONE, NONE, b, c};
-        if (beams[b].finished) x.z = c == 0 ? 0.f : NONE;
-        else                   x.z = a.chunk_top[(size_t)(row0 + b) * a.chunks + c];
-        x.rank = ranked(beams[b], x.z);
-        return x;
-    };
     float mine = NONE;
-    for (int i = tid; i < n; i += PICK) mine = fmaxf(mine, (float)chunk_at(i).rank);
+    for (int t = wave; t < W * parts; t += WAVES) {
+        const Share s = share_of(t);
+        const Beam &b = beams[s.beam];
+        float most = NONE;
+        if (b.finished) {
+            most = s.first == 0 && lane == 0 ? 0.f : NONE;               // (its one candidate)
+        } else {
+            for (int q0 = 0; q0 < s.n; q0 += 64 * HELD) {
+                if (t != wave || q0) load(s, q0, z);
+#pragma unroll
+                for (int u = 0; u < HELD; ++u) most = fmaxf(most, top_of(z[u]));
+            }
+        }
+        mine = fmaxf(mine, (float)ranked(b, most));
+    }
     {
-        const int key = in_order(mine);
-        int bound = in_order(NONE);
+        const unsigned key = (unsigned)in_order(mine) ^ 0x80000000u;
         unsigned lo = 0;                                 // the largest key that W lanes reach, bit by bit from above
 #pragma unroll 1
         for (int bit = 31; bit >= 0; --bit) {
             const unsigned t = lo | 1u << bit;
-            if (__popcll(__ballot(((unsigned)key ^ 0x80000000u) >= t)) >= W) lo = t;
+            if (__popcll(__ballot(key >= t)) >= W) lo = t;
         }
-        bound = max(bound, (int)(lo ^ 0x80000000u));
-        if (lane == 0) atomicMax(&at_least, bound);
+        if (lane == 0) atomicMax(&at_least, (int)(lo ^ 0x80000000u));
     }
     __syncthreads();
     const int bound = at_least;
-    for (int i = tid; i < n; i += PICK) {
-        const Candidate x = chunk_at(i);
-        if (x.rank > (double)NONE && in_order((float)x.rank) >= bound) {
-            const int at = atomicAdd(&found, 1);
-            if (at < LIST) list[at] = x;
+    const float bound_rank = __int_as_float(bound < 0 ? bound ^ 0x7FFFFFFF : bound);
+    // the bound as one on a beam's logits, a little lower (ranks decide): what is below it has no part
+    const auto lowest = [&](const Beam &b) {
+        if (!b.live) return __builtin_inff();
+        if (bound_rank == NONE) return -3.4028235e38f;
+        const double low = ((double)bound_rank - fabs((double)bound_rank) * 0x1p-22) / b.per - b.score, z = low + b.lse;
+        return (float)(z - (fabs(low) + fabs(b.lse)) * 0x1p-22);
+    };
+    for (int t = wave; t < W * parts; t += WAVES) {
+        const Share s = share_of(t);
+        const Beam &b = beams[s.beam];
+        if (b.finished) {
+            const double rank = ranked(b, 0.f);
+            if (s.first == 0 && lane == 0 && b.live && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), 0.f, s.beam, 0});
+            continue;
+        }
+        const float from = lowest(b);
+        for (int q0 = 0; q0 < s.n; q0 += 64 * HELD) {
+            if (!all) load(s, q0, z);
+            unsigned some = 0;
+#pragma unroll
+            for (int u = 0; u < HELD; ++u) some |= top_of(z[u]) >= from ? 1u << u : 0u;
+            while (some) {
+                const int q = q0 + __builtin_ctz(some) * 64 + lane;
+                some &= some - 1;
+                const f32x4 four = s.tops[q];
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e) {
+                    const float x = e & 2 ? (e & 1 ? four[3] : four[2]) : (e & 1 ? four[1] : four[0]);
+                    const double rank = ranked(b, x);
+                    if (x >= from && x > NONE && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), x, s.beam, 4 * (s.first + q) + e});
+                }
+            }
         }
     }
     __syncthreads();
-    int chunks = min(found, W);
+    const int found = list.found, chunks = min(found, W);
+    __syncthreads();
     if (found <= LIST) {
-        const int m = found;
-        for (int i = tid; i < m; i += PICK) {
-            int number = 0;
-            for (int j = 0; j < m; ++j) number += before(list[j], list[i]);
-            if (number < W) best[number] = list[i];
-        }
-        __syncthreads();
+        best_of(list, found, W, best);
     } else {
         // (more equals than the list holds: one after the other)
-        Candidate last{__builtin_inf(), 0.f, -1, -1};
-        for (int k = 0; k < chunks; ++k) {
-            Candidate top{(double)NONE, NONE, W, 0};
-            for (int i = tid; i < n; i += PICK) {
-                const Candidate x = chunk_at(i);
-                if (x.rank > (double)NONE && before(last, x) && before(x, top)) top = x;
+        Candidate last{0x7FFFFFFFFFFFFFFFll, 0.f, -1, -1};
+        for (int n = 0; n < chunks; ++n) {
+            Candidate top{in_order((double)NONE), NONE, W, 0};
+            for (int t = wave; t < W * parts; t += WAVES) {
+                const Share s = share_of(t);
+                const Beam &b = beams[s.beam];
+                const float from = lowest(b);
+                for (int c = lane; c < (b.finished ? 1 : 4 * s.n); c += 64) {
+                    const float z = b.finished ? (s.first == 0 ? 0.f : NONE) : reinterpret_cast<const float *>(s.tops)[c];
+                    const Candidate x{in_order(ranked(b, z)), z, s.beam, 4 * s.first + c};
+                    if (z > NONE && (b.finished || z >= from) && x.rank > in_order((double)NONE) && before(last, x) && before(x, top)) top = x;
+                }
             }
 #pragma unroll 1
             for (int d = 1; d < 64; d *= 2) {
@@ -225,39 +331,35 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
             __syncthreads();
             last = wave_best[0];
 #pragma unroll 1
-            for (int w = 1; w < PICK / 64; ++w)
+            for (int w = 1; w < WAVES; ++w)
                 if (before(wave_best[w], last)) last = wave_best[w];
-            if (tid == 0) best[k] = last;
+            if (tid == 0) best[n] = last;
             __syncthreads();
         }
     }
 
     // Their logits: none that is worse than the best of the W-th chunk counts.
-    if (tid == 0) found = 0;
+    if (tid == 0) list.found = 0;
     __syncthreads();
-    const Candidate worst = best[max(chunks - 1, 0)];
+    const long long worst = chunks < W ? in_order((double)NONE) : best[W - 1].rank;
     for (int i = tid; i < chunks * CHUNK; i += PICK) {
         const Candidate of = best[i / CHUNK];
         const Beam &b = beams[of.beam];
         const int v = b.finished ? i % CHUNK : of.at * CHUNK + i % CHUNK;
-        Candidate x{(double)NONE, NONE, of.beam, v};
-        if (b.finished)   x.z = v == 0 ? 0.f : NONE;
-        else if (v < a.V) x.z = logit_at<FP32>(reinterpret_cast<const char *>(a.logits) + (size_t)(row0 + of.beam) * a.V * (FP32 ? 4 : 2), v);
-        x.rank = ranked(b, x.z);
-        if (x.rank > (double)NONE && (chunks < W || x.rank >= worst.rank)) list[atomicAdd(&found, 1)] = x;
+        float z = NONE;
+        if (b.finished)   z = v == 0 ? 0.f : NONE;
+        else if (v < a.V) z = logit_at<FP32>(reinterpret_cast<const char *>(a.logits) + (size_t)(row0 + of.beam) * a.V * (FP32 ? 4 : 2), v);
+        const double rank = ranked(b, z);
+        if (rank > (double)NONE && in_order(rank) >= worst) list.put(Candidate{in_order(rank), z, of.beam, v});
     }
     __syncthreads();
-    const int m = found;
-    for (int i = tid; i < m; i += PICK) {
-        int number = 0;
-        for (int j = 0; j < m; ++j) number += before(list[j], list[i]);
-        if (number < W) winners[number] = list[i];
-    }
+    const int m = list.found;
     __syncthreads();
+    best_of(list, m, W, best);
     if (tid < W) {
         const int row = row0 + tid;
         if (tid < m) {
-            const Candidate x = winners[tid];
+            const Candidate x = best[tid];
             const Beam &b = beams[x.beam];
             const int token = b.finished ? a.pad : x.at;
             a.source[row] = row0 + x.beam;
@@ -287,14 +389,14 @@ mlora_status check(const mlora_beam *d)
     return MLORA_OK;
 }
 
-// Where the parts of the workspace begin: 8-byte numbers first.
+// Rows, and what each leaves in the workspace.
 struct Sizes {
-    size_t rows, chunks, slices;
-    size_t bytes() const { return rows * (slices * 12 + chunks * 4) + 256; }
+    size_t rows, slices;
+    size_t bytes() const { return rows * slices * (8 + 4 + 4 * (SLICE / CHUNK)) + 256; }
 };
 Sizes sizes_of(const mlora_beam *d)
 {
-    return Sizes{(size_t)d->n_groups * d->n_beams, ((size_t)d->vocab + CHUNK - 1) / CHUNK, ((size_t)d->vocab + SLICE - 1) / SLICE};
+    return Sizes{(size_t)d->n_groups * d->n_beams, ((size_t)d->vocab + SLICE - 1) / SLICE};
 }
 
 }  // namespace
@@ -333,12 +435,11 @@ mlora_status mlora_beam_select(const mlora_beam *d, const void *logits, const fl
     a.score_out = score_out;
     a.length_out = length_out;
     a.finished_out = finished_out;
-    a.slice_sum = reinterpret_cast<double *>(workspace);
+    a.chunk_top = reinterpret_cast<float *>(workspace);
+    a.slice_sum = reinterpret_cast<double *>(a.chunk_top + n.rows * n.slices * (SLICE / CHUNK));
     a.slice_top = reinterpret_cast<float *>(a.slice_sum + n.rows * n.slices);
-    a.chunk_top = a.slice_top + n.rows * n.slices;
     a.W = d->n_beams;
     a.V = d->vocab;
-    a.chunks = (int)n.chunks;
     a.slices = (int)n.slices;
     a.eos = d->eos;
     a.pad = d->pad;

@@ -13,7 +13,7 @@
  * Position encodings are applied by the caller.
  *
  * What a row may not see does not touch it, infinite or not a number as it may be.  A row that sees NaN, or whose own query vector is not
- * finite, is NaN.  Finite scores scale q . k are of a magnitude below 2^30.
+ * finite, is NaN.  Finite scores scale q . k are of a magnitude below 2^20.
  *
  * Conventions as in mlora_w4.h; results are bit-identical from call to call.
  */

@@ -46,7 +46,7 @@ typedef struct {
     int32_t max_pages;                 /* of a stream, which holds up to 64 * max_pages + 63 tokens */
     void *k;                           /* int8 [L][n_pages][H][64][D], 16-byte aligned like all of the data */
     void *v;                           /* int8 [L][n_pages][H][D][64] */
-    float *k_scale, *v_scale;          /* fp32 [L][n_pages][H] */
+    float *k_scale, *v_scale;          /* fp32 [L][n_pages][H], not negative (or NaN) */
     void *k_tail, *v_tail;             /* bf16 [L][S][H][64][D]: token t of the stream in slot i at [l][i][h][t % 64] */
     int32_t *slot;                     /* int32 [S]: where the stream's tail and table row are; every number once */
     int32_t *len;                      /* int32 [S]: tokens of the stream (outside [0, 64 * max_pages + 63]: the nearer end) */

@@ -1,19 +1,26 @@
 // Attention over a paged cache of 8 bits (see include/mlora_page_attention.h).
 //
-// A block takes up to 16 query vectors of one stream and one kv head.  What they may see is a list of items: pages of 64
-// tokens (those of the sink, then from the window's first on), chunks of 32 tokens of the tail, chunks of 32 rows of the step.  The block's waves
-// take items in turn, each by itself, and merge their results through LDS at the end; where one block is not enough for the items several
-// share them, and a second kernel merges what they leave in the workspace.
+// A block takes up to 16 query vectors of one kv head: of one stream, or of several if they have few (a bundle).  What they may see is a list of
+// items: pages of 64 tokens (those of the sink, then from the window's first on), chunks of 32 tokens of the tails, chunks of 32 rows of
+// the step.  The block's waves take items in turn, each by itself, and merge their results through LDS at the end; where one block is not enough for
+// the items several share them, and a second kernel merges what they leave in the workspace.  Streams of a bundle that hold the same page at the same
+// place, as beams do, take it together: a page that all of four streams see costs what it costs one.
 //
 // Pages go from memory to the matrix units as they are: codes are multiplied as whole numbers (16x16x64 products of int8, exact in
-// 32 bits), nothing is widened and nothing passes through LDS.  The other side is cut into digits to the base 256, each a signed byte:
-//     q = 2^(e - 21) (65536 a + 256 b + c)         e the exponent of the vector's largest magnitude: to 2^-22 of that
-//     p = (65536 a + 256 b + c) / 8355711          p = exp(score - the page's largest score) in (0, 1]: to 2^-24
-// so that a product of scores or outputs is three products of bytes, half the work each of one of bf16.  The weights are counted relative to
+// 32 bits), nothing is widened and nothing passes through LDS.  The other side is cut into N digits to the base 256, each a signed byte, of
+// whole numbers of N bytes:
+//     q = unit * whole         to 2^-22 of the vector's largest magnitude (N = 3), 2^-15 (N = 2)
+//     p = whole / P_ONE        p = exp(score - the page's largest score) in (0, 1], to 2^-24 (N = 3), 2^-16 (N = 2)
+// so that a product of scores or outputs is N products of bytes, each half the work of one of bf16.  Outputs in fp32 take three digits, which is what fp32
+// arithmetic would leave; outputs in bf16 take two, which moves them by a few 2^-15 where their own rounding is 2^-9.  The weights are counted relative to
 // the page's own maximum; a page's sum of weights is the sum of the very integers that multiply the values.  Scores are K . Q^T: a lane
 // holds 16 keys of ONE query vector, and if the keys of a page are dealt to the products in the right order (key 16 * (i / 4) + 4 * t + i % 4 is
 // row i of product t) these are the 16 that O^T += V^T . P^T wants from it.  Values are stored feature by feature for that.
 // The tail and the step's rows are bf16, with scores and weights (two bf16 halves) as in tree_attention.hip.
+//
+// What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 5.1 TB/s); else the vector work around the weights, some 300 to 400
+// instructions per page and tile.  So whole numbers become floats and back by adding 1.5 * 2^23 or 2^23 where that is free (an accumulator's start, the
+// addend of a multiplication) and not by conversions.
 #include <algorithm>
 #include <type_traits>
 
@@ -29,7 +36,12 @@ namespace {
 
 constexpr int P = MLORA_PAGE_TOKENS, KC = 32;            // tokens of a page, of a chunk
 constexpr float UNSEEN = -__builtin_inff();
-constexpr float P_ONE = 8355711.f;                       // 127 * 65536 + 127 * 256 + 127
+// The largest weight as a whole number of N digits, 127 in each place, and what turns a float of such a size into its bits: with that addend the low
+// bytes of the sum are the number, 128 added to all digits but the first (which has room for none).
+template <int N> constexpr float P_ONE = N == 3 ? 8355711.f : 32639.f;
+template <int N> constexpr float P_BITS = 8388608.f + (N == 3 ? 32896.f : 128.f);
+constexpr int NUMBER = 0x4B400000;                       // the bits of 1.5 * 2^23: a whole number below 2^22 added to them is one added to it
+constexpr float NUMBER_F = 12582912.f;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -46,7 +58,7 @@ struct AttnArgs {
     void *out;
     int Hq, Hkv, G, S, R, M;
     int pages, columns, window, sink;
-    int splits;
+    int splits, bundle;
     unsigned g_inv;                                      // ceil(2^16 / G): v / G = (v * g_inv) >> 16 for v < 512
     int out_fp32;
     float scale2;                                        // scale * log2(e)
@@ -71,17 +83,32 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c)
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// Four whole numbers of at most 127 * 65536 + 127 * 256 + 127 in magnitude -> their digits, a register of four bytes for each place.
-struct Digits {
-    unsigned a, b, c;
-};
-__device__ __forceinline__ Digits digits_of(int x0, int x1, int x2, int x3)
+// Byte n of four registers
+__device__ __forceinline__ unsigned bytes_of(int n, unsigned y0, unsigned y1, unsigned y2, unsigned y3)
 {
-    const unsigned y0 = (unsigned)(x0 + 0x808080), y1 = (unsigned)(x1 + 0x808080), y2 = (unsigned)(x2 + 0x808080), y3 = (unsigned)(x3 + 0x808080);
-    const unsigned lo01 = __builtin_amdgcn_perm(y1, y0, 0x05010400u), lo23 = __builtin_amdgcn_perm(y3, y2, 0x05010400u);   // {b0 b0 b1 b1}
-    const unsigned hi01 = __builtin_amdgcn_perm(y1, y0, 0x0C0C0602u), hi23 = __builtin_amdgcn_perm(y3, y2, 0x0C0C0602u);
-    return Digits{__builtin_amdgcn_perm(hi23, hi01, 0x05040100u) ^ 0x80808080u, __builtin_amdgcn_perm(lo23, lo01, 0x07060302u) ^ 0x80808080u,
-                  __builtin_amdgcn_perm(lo23, lo01, 0x05040100u) ^ 0x80808080u};
+    const unsigned pair = 0x0C0C0400u + 0x0101u * n;
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(y3, y2, pair), __builtin_amdgcn_perm(y1, y0, pair), 0x05040100u);
+}
+// Digits of four whole numbers, 128 added to all but the first: d[0] the first (of four numbers), d[N - 1] the last
+template <int N>
+__device__ __forceinline__ void digits_of(const unsigned (&y)[4], unsigned (&d)[N])
+{
+    const unsigned lo01 = __builtin_amdgcn_perm(y[1], y[0], 0x05010400u), lo23 = __builtin_amdgcn_perm(y[3], y[2], 0x05010400u);   // {b0 b0 b1 b1}
+    const unsigned b0 = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u), b1 = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
+    d[N - 1] = b0 ^ 0x80808080u;
+    if constexpr (N == 3) {
+        d[1] = b1 ^ 0x80808080u;
+        d[0] = bytes_of(2, y[0], y[1], y[2], y[3]);
+    } else {
+        d[0] = b1;
+    }
+}
+// The sum of N products of digits, as a number; NUMBER_F is added to it if the last accumulator started from NUMBER.
+template <int N>
+__device__ __forceinline__ float joined(const i32x4 (&x)[N], int e)
+{
+    if constexpr (N == 3) return __builtin_fmaf((float)((x[0][e] << 8) + x[1][e]), 256.f, __int_as_float(x[2][e]));
+    else                  return (float)((x[0][e] << 8) + x[1][e]);
 }
 
 // LDS of a wave: the values of a chunk on their way to the matrix units, then its share of the result.
@@ -93,124 +120,180 @@ struct WaveLds {
     static constexpr int BYTES = KC * VROW > O_BYTES + ML_BYTES ? KC * VROW : O_BYTES + ML_BYTES;
 };
 
-template <int D, int W, bool SPLIT>
-__global__ __launch_bounds__(64 * W, 2) void page_attn(const AttnArgs a)
+template <int D, int W, int N, bool SPLIT>
+__global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page_attn(const AttnArgs a)
 {
     using L = WaveLds<D>;
     constexpr int DK = D / 64, DB = D / 16, VI = KC * D / 512;
     __shared__ __align__(16) unsigned char smem[W * L::BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int hk = blockIdx.x, s = SPLIT ? (int)blockIdx.z / a.splits : (int)blockIdx.z, z = SPLIT ? (int)blockIdx.z - s * a.splits : 0;
-    const int n_qv = a.R * a.G, qv0 = (int)blockIdx.y * 16;
+    const int hk = blockIdx.x, bz = SPLIT ? (int)blockIdx.z / a.splits : (int)blockIdx.z, z = SPLIT ? (int)blockIdx.z - bz * a.splits : 0;
+    const int s0 = bz * a.bundle, streams = min(a.bundle, a.S - s0), per_stream = a.R * a.G, n_qv = streams * per_stream, qv0 = (int)blockIdx.y * 16;
 
-    // the items
+    // this lane's query vector: its stream, row and head
+    const int vec = min(qv0 + l16, n_qv - 1), sb = a.bundle == 1 ? 0 : vec / per_stream, in_stream = vec - sb * per_stream;
+    const int row = (int)((unsigned)in_stream * a.g_inv >> 16), s = s0 + sb;
+    const uint16_t *const q_at = a.q + ((size_t)(s * a.R + row) * a.Hq + hk * a.G + (in_stream - row * a.G)) * D;
+    u32x4 qx[DK][2];
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) qx[kk][i] = *reinterpret_cast<const u32x4 *>(q_at + 64 * kk + 16 * lq + 8 * i);
+
+    // the items: page numbers that some stream of the bundle sees, then chunks
     const int len = min(max(a.len[s], 0), P * a.columns + P - 1), slot = min(max(a.slot[s], 0), a.S - 1);
-    const int full = len / P, n_tail = len % P;
-    const int first = a.window > 0 ? min(max(len - a.window + 1, 0) / P, full) : 0, sinks = min((a.sink + P - 1) / P, first);
-    const int n_pages = sinks + full - first, tail_chunks = (n_tail + KC - 1) / KC, end_t = n_pages + tail_chunks;
-    const int items = end_t + (a.R + KC - 1) / KC;
+    const int full = len / P, first = a.window > 0 ? min(max(len - a.window + 1, 0) / P, full) : 0, sinks = min((a.sink + P - 1) / P, first);
+    int b_full = full, b_first = first, b_sinks = sinks;               // of the bundle
+    if (a.bundle > 1)
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) {
+            b_full = max(b_full, __shfl_xor(b_full, d));
+            b_first = min(b_first, __shfl_xor(b_first, d));
+            b_sinks = max(b_sinks, __shfl_xor(b_sinks, d));
+        }
+    b_full = __builtin_amdgcn_readfirstlane(b_full), b_first = __builtin_amdgcn_readfirstlane(b_first);
+    b_sinks = min(__builtin_amdgcn_readfirstlane(b_sinks), b_first);
+    const int n_pages = b_sinks + b_full - b_first, per_chunks = (P - 1 + a.R + KC - 1) / KC, items = n_pages + streams * per_chunks;
     const int *const table = a.table + (size_t)slot * a.columns;
-    const auto page_of = [&](int i) { return i < sinks ? i : first + i - sinks; };
+    const int stride = SPLIT ? a.splits * W : W;
+    int c = z * W + wave;
+    // the page that this lane's stream sees as item i, or -1
+    const auto number_of = [&](int i) { return i < b_sinks ? i : b_first + i - b_sinks; };
+    const auto look_up = [&](int i) {
+        const int at = number_of(i);
+        int page = -1;
+        if (i < n_pages && at < full && (at >= first || at < sinks)) page = table[at];
+        return page < a.pages ? page : -1;
+    };
+    int todo = look_up(c), ahead = look_up(c + stride);
 
-    // this lane's query vector, its row and position
-    const int vec = min(qv0 + l16, n_qv - 1), row = (int)((unsigned)vec * a.g_inv >> 16);
-    const uint16_t *const q_at = a.q + ((size_t)(s * a.R + row) * a.Hq + hk * a.G + (vec - row * a.G)) * D;
-    u32x4 qd[3][DK];
+    // its digits
+    u32x4 qd[N][DK];
     float unit;                                          // score of a product of codes, but for the page's scale
     {
-        u32x4 x[DK][2];
         unsigned top = 0;
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[kk][i] = *reinterpret_cast<const u32x4 *>(q_at + 64 * kk + 16 * lq + 8 * i);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top = max(top, max(x[kk][i][j] & 0x7FFFu, x[kk][i][j] >> 16 & 0x7FFFu));
-            }
-        top = __float_as_uint(over_quarters(__uint_as_float(top), [](float p, float r) { return __uint_as_float(max(__float_as_uint(p), __float_as_uint(r))); }));
-        const int e = (int)max(top >> 7, 1u) - 127;
+            for (int i = 0; i < 8; ++i) top = max(top, max(qx[kk][i / 4][i % 4] & 0x7FFFu, qx[kk][i / 4][i % 4] >> 16 & 0x7FFFu));
+        top = __float_as_uint(over_quarters(__uint_as_float(top), [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); }));
+        // (whole numbers below 2^22, or, with 128 added, below 2^15: 1.99 is the next exponent's)
+        const int e = (int)max(N == 3 ? top >> 7 : (top + 1) >> 7, 1u) - 127;
         const bool ok = top < 0x7F80u;
-        unit = ok ? __builtin_ldexpf(a.scale2, e - 21) : __builtin_nanf("");
+        constexpr int BITS = N == 3 ? 21 : 14;
+        unit = ok ? __builtin_ldexpf(fabsf(a.scale2), e - BITS) : __builtin_nanf("");
+        const int shift = BITS - e;
+        const float sign = a.scale2 < 0.f ? -1.f : 1.f;
 #pragma unroll
         for (int kk = 0; kk < DK; ++kk)
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                int n[4];
+                unsigned n[4], d[N];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const unsigned pair = x[kk][w / 2][2 * (w % 2) + j / 2];
-                    const float f = __builtin_ldexpf(bf16_bits_to_float(j & 1 ? pair >> 16 : pair & 0xFFFFu), 21 - e);
-                    n[j] = ok ? (int)rintf(f) : 0;
+                    const unsigned pair = qx[kk][w / 2][2 * (w % 2) + j / 2];
+                    const float f = sign * __builtin_ldexpf(bf16_bits_to_float(j & 1 ? pair >> 16 : pair & 0xFFFFu), shift);
+                    n[j] = (unsigned)((ok ? (int)rintf(f) : 0) + (N == 3 ? 0x8080 : 0x80));
                 }
-                const Digits d = digits_of(n[0], n[1], n[2], n[3]);
-                qd[0][kk][w] = d.a, qd[1][kk][w] = d.b, qd[2][kk][w] = d.c;
+                digits_of<N>(n, d);
+#pragma unroll
+                for (int g = 0; g < N; ++g) qd[g][kk][w] = d[g];
             }
     }
-    // lane r: the rows that row r may see, itself and what it continues (a parent must be an earlier row: the walk strictly
-    // descends, so it ends and stays in bounds whatever the array holds)
-    unsigned anc_lo = lane < 32 ? 1u << lane : 0u, anc_hi = lane >= 32 ? 1u << (lane - 32) : 0u;
+    // lane sb * R + r: the rows that row r of a stream may see, itself and what it continues (a parent must be an earlier row: the walk
+    // strictly descends, so it ends and stays in bounds whatever the array holds)
+    const int my_row = a.bundle == 1 ? lane : lane % a.R, row_lane = sb * a.R + row;
+    unsigned anc_lo = my_row < 32 ? 1u << my_row : 0u, anc_hi = my_row >= 32 ? 1u << (my_row - 32) : 0u;
     if (a.R > 1) {
-        const int up0 = lane < a.R ? a.parent[s * a.R + lane] : -1;
-        int r = lane < a.R && up0 < lane ? up0 : -1;
+        const int up0 = lane < streams * a.R ? a.parent[s0 * a.R + lane] : -1;
+        int r = up0 < my_row ? up0 : -1;
         while (__ballot(r >= 0)) {
             if (r >= 0) {
                 anc_lo |= r < 32 ? 1u << r : 0u;
                 anc_hi |= r >= 32 ? 1u << (r - 32) : 0u;
             }
-            const int up = __shfl(up0, max(r, 0));
+            const int up = __shfl(up0, lane - my_row + max(r, 0));
             r = r >= 0 && up < r ? up : -1;
         }
     }
-    const int depth = __popc(anc_lo) + __popc(anc_hi) - 1;             // of row `lane`
-    const unsigned sees_lo = (unsigned)__shfl((int)anc_lo, row), sees_hi = (unsigned)__shfl((int)anc_hi, row);
-    const int since = a.window > 0 ? len + __shfl(depth, row) - a.window + 1 : 0;      // positions that the row sees begin here, but for the sink
-    int latest = since;                                                                // of all rows of the tile
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) latest = max(latest, __shfl_xor(latest, d));
+    const int depth = __popc(anc_lo) + __popc(anc_hi) - 1;             // of row `my_row`
+    unsigned long long path = (unsigned long long)(unsigned)__shfl((int)anc_hi, row_lane) << 32 | (unsigned)__shfl((int)anc_lo, row_lane);
+    const int since = a.window > 0 ? len + __shfl(depth, row_lane) - a.window + 1 : 0;      // positions that the row sees begin here, but for the sink
+    if (a.window > 0 && a.window < a.R)                  // the rows of the path that the window has left behind
+        for (int j = 0; j < a.R; ++j) {
+            const int pos = len + __shfl(depth, sb * a.R + j);
+            if (pos < since && pos >= a.sink) path &= ~(1ull << j);
+        }
 
-    float m = UNSEEN, l = 0.f;                           // l: of the lane's own keys
+    float m = UNSEEN, l = 0.f, over = 0.f;               // l: of the lane's own keys; over: what NUMBER_F adds to every output
     f32x4 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int c = z * W + wave;
-    const int stride = SPLIT ? a.splits * W : W;
 
-    // pages
-    const size_t unit_bytes = (size_t)P * D;
-    for (; c < n_pages; c += stride) {
-        const int i = page_of(c), page = table[i];
-        if (page < 0 || page >= a.pages) continue;
+    // pages: the next one to look at, and who sees it
+    int page = -1;
+    bool mine = false;
+    u32x4 kf[4][DK], vf[DB];
+    float ks, vs;
+    const auto next = [&]() {
+        for (;;) {
+            const unsigned long long left = __ballot(todo >= 0);
+            if (left) {
+                page = __builtin_amdgcn_readlane(todo, __builtin_ctzll(left));
+                mine = todo == page;
+                todo = mine ? -1 : todo;
+                return true;
+            }
+            if (c + stride >= n_pages) return false;
+            c += stride;
+            todo = ahead;
+            ahead = look_up(c + stride);
+        }
+    };
+    const auto load_k = [&]() {
         const size_t at = (size_t)page * a.Hkv + hk;
-        const int8_t *const kp = a.k + at * unit_bytes + (16 * (l16 >> 2) + (l16 & 3)) * D + 16 * lq;
-        const int8_t *const vp = a.v + at * unit_bytes + l16 * P + 16 * lq;
-        u32x4 kf[4][DK], vf[DB];
+        const int8_t *const kp = a.k + at * (P * D) + (16 * (l16 >> 2) + (l16 & 3)) * D + 16 * lq;
+        ks = a.k_scale[at], vs = a.v_scale[at];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int kk = 0; kk < DK; ++kk) kf[t][kk] = *reinterpret_cast<const u32x4 *>(kp + 4 * t * D + 64 * kk);
-        const float ks = a.k_scale[at], vs = a.v_scale[at];
+    };
+    const auto load_v = [&]() {
+        const int8_t *const vp = a.v + ((size_t)page * a.Hkv + hk) * (P * D) + l16 * P + 16 * lq;
 #pragma unroll
         for (int db = 0; db < DB; ++db) vf[db] = *reinterpret_cast<const u32x4 *>(vp + 16 * db * P);
-        // scores: element e of sc[t] is key 16 * lq + 4 * t + e
+    };
+    bool more = c < n_pages && next();
+    if (more) {
+        load_k();
+        load_v();
+    }
+#pragma nounroll
+    while (more) {
+        // scores: element e of sc[t] is key 16 * lq + 4 * t + e; in units of `per`, and NUMBER_F too large
         f32x4 sc[4];
         float per = unit * ks;
-        const bool bad = !(fabsf(per) < __builtin_inff());
-        if (bad) per = 0.f;                              // (a query vector or a page that is not finite: whoever sees a token becomes NaN below)
+        const float vs_here = vs;
+        // (a query vector or a page that is not finite: whoever sees a token becomes NaN below.  Zeros are all alike, and hidden keys stay hidden.)
+        const bool bad = !(per >= 0.f && per < __builtin_inff()), seen = mine;
+        if (bad || per == 0.f) per = 1e-30f;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            i32x4 x[3];
+            i32x4 x[N];
 #pragma unroll
-            for (int g = 0; g < 3; ++g) {
-                x[g] = i32x4{0, 0, 0, 0};
+            for (int g = 0; g < N; ++g) {
+                x[g] = g == 2 ? i32x4{NUMBER, NUMBER, NUMBER, NUMBER} : i32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int kk = 0; kk < DK; ++kk) x[g] = mfma_i8(kf[t][kk], qd[g][kk], x[g]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[t][e] = ((float)((x[0][e] << 8) + x[1][e]) * 256.f + (float)x[2][e]) * per;
+            for (int e = 0; e < 4; ++e) sc[t][e] = joined<N>(x, e);
         }
-        const int t0 = i * P;
-        if (t0 < latest && t0 + P > a.sink) {
+        const int t0 = number_of(c) * P;
+        more = next();
+        if (more) load_k();
+        if (__ballot(seen && t0 < since && t0 + P > a.sink)) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -225,84 +308,100 @@ __global__ __launch_bounds__(64 * W, 2) void page_attn(const AttnArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[t][e]);
         top = over_quarters(top, most);
-        // weights relative to the page's maximum, as whole numbers
-        const float from = finite_or_0(top);
-        int sum = 0;
-        u32x4 pd[3];
+        // weights relative to the page's maximum, as whole numbers; nothing of a page that the lane's stream does not hold
+        // (its maximum a little too large, since that of a product is rounded and no weight may be above 1)
+        const float scaled = finite_or_0(top) * per, from = scaled + fabsf(scaled) * 0x1p-23f, one = seen ? P_ONE<N> : 0.f;
+        unsigned sum = 0;
+        u32x4 pd[N];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            int n[4];
+            unsigned n[4], d[N];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                n[e] = (int)rintf(__builtin_amdgcn_exp2f(sc[t][e] - from) * P_ONE);
+                n[e] = __float_as_uint(__builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e], per, -from)), one, P_BITS<N>));
                 sum += n[e];
             }
-            const Digits d = digits_of(n[0], n[1], n[2], n[3]);
-            pd[0][t] = d.a, pd[1][t] = d.b, pd[2][t] = d.c;
+            digits_of<N>(n, d);
+#pragma unroll
+            for (int g = 0; g < N; ++g) pd[g][t] = d[g];
         }
-        const float m_new = fmaxf(m, top), base = finite_or_0(m_new), keep = __builtin_amdgcn_exp2f(m - base);
-        float w = __builtin_amdgcn_exp2f(top - base) * (1.f / P_ONE);
+        sum -= 16u * __float_as_uint(P_BITS<N>);
+        top = top == UNSEEN || !seen ? UNSEEN : N == 3 ? __builtin_fmaf(-NUMBER_F, per, from) : from;
+        // The sums so far are relative to a maximum that is raised only where a page's is more than 2^40 times as heavy: fp32 has the room, and what the
+        // lane holds need not be scaled for every page that is a little heavier.
+        if (__ballot(top > m + 40.f)) {
+            const float m_new = top > m + 40.f ? top : m, keep = __builtin_amdgcn_exp2f(m - finite_or_0(m_new));
+            m = m_new;
+            l *= keep;
+            over *= keep;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] *= keep;
+        }
+        float w = __builtin_amdgcn_exp2f(top - finite_or_0(m)) * (1.f / P_ONE<N>);
         if (bad && top != UNSEEN) w = __builtin_nanf("");
-        m = m_new;
-        l = l * keep + (float)sum * w;
-        const float wv = top != UNSEEN ? w * vs : 0.f;   // (a page of NaN that the row does not see)
+        l += (float)(int)sum * w;
+        const float wv = top != UNSEEN ? w * vs_here : 0.f;              // (a page of NaN that the row does not see)
+        if constexpr (N == 3) over += NUMBER_F * wv;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            i32x4 x[3];
+            i32x4 x[N];
 #pragma unroll
-            for (int g = 0; g < 3; ++g) x[g] = mfma_i8(vf[db], pd[g], i32x4{0, 0, 0, 0});
+            for (int g = 0; g < N; ++g) x[g] = mfma_i8(vf[db], pd[g], g == 2 ? i32x4{NUMBER, NUMBER, NUMBER, NUMBER} : i32x4{0, 0, 0, 0});
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[db][e] = o[db][e] * keep + ((float)((x[0][e] << 8) + x[1][e]) * 256.f + (float)x[2][e]) * wv;
+            for (int e = 0; e < 4; ++e) o[db][e] = __builtin_fmaf(joined<N>(x, e), wv, o[db][e]);
         }
+        if (more) load_v();
     }
+    while (c < n_pages) c += stride;
+    if constexpr (N == 3)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] -= over;
 
-    // chunks of the tail and of the step's rows
-    unsigned char *const mine = smem + wave * L::BYTES;
-    unsigned char *const v_in = mine + (lane / (D / 8)) * L::VROW + (lane % (D / 8)) * 16;
+    // chunks of a tail and, behind it, the step's rows
+    unsigned char *const piece_of = smem + wave * L::BYTES;
+    unsigned char *const v_in = piece_of + (lane / (D / 8)) * L::VROW + (lane % (D / 8)) * 16;
     using Lds4 = __attribute__((address_space(3))) s16x4;
-    const unsigned char *const v_out = mine + (4 * lq + (l16 >> 2)) * L::VROW + (l16 & 3) * 8;
+    const unsigned char *const v_out = piece_of + (4 * lq + (l16 >> 2)) * L::VROW + (l16 & 3) * 8;
     for (; c < items; c += stride) {
-        const bool tail = c < end_t;
-        const int k0 = (tail ? c - n_pages : c - end_t) * KC, n = min((tail ? n_tail : a.R) - k0, KC), pitch = tail ? D : a.Hkv * D;
-        const size_t at = tail ? (((size_t)slot * a.Hkv + hk) * P + k0) * D : ((size_t)(s * a.R + k0) * a.Hkv + hk) * D;
-        const uint16_t *const kp = (tail ? a.k_tail : a.k_new) + at, *const vp = (tail ? a.v_tail : a.v_new) + at;
+        const int cs = (c - n_pages) / per_chunks, k0 = (c - n_pages - cs * per_chunks) * KC;
+        const int its_len = __builtin_amdgcn_readlane(len, cs * per_stream), its_slot = __builtin_amdgcn_readlane(slot, cs * per_stream);
+        const int n_tail = its_len % P, n = min(n_tail + a.R - k0, KC);
+        if (n <= 0) continue;
+        const size_t tail_at = ((size_t)its_slot * a.Hkv + hk) * P * D, rows_at = ((size_t)(s0 + cs) * a.R * a.Hkv + hk) * D;
+        // key number k0 + i, the last one behind the end
+        const auto from = [&](const uint16_t *tail, const uint16_t *rows, int i) {
+            const int k = k0 + min(i, n - 1);
+            return k < n_tail ? tail + tail_at + k * D : rows + rows_at + (size_t)(k - n_tail) * (a.Hkv * D);
+        };
         // scores: element e of sc[j] is key 16 * j + 4 * lq + e
         f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        u32x4 vr[VI];
+        const uint16_t *const kp[2] = {from(a.k_tail, a.k_new, l16) + 8 * lq, from(a.k_tail, a.k_new, 16 + l16) + 8 * lq};
+#pragma unroll
+        for (int u = 0; u < VI; ++u) {
+            const int piece = u * 64 + lane;
+            vr[u] = *reinterpret_cast<const u32x4 *>(from(a.v_tail, a.v_new, piece / (D / 8)) + (piece % (D / 8)) * 8);
+        }
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk) {
             const uint4 qf = *reinterpret_cast<const uint4 *>(q_at + 32 * kk + 8 * lq);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sc[j] = mfma16(*reinterpret_cast<const uint4 *>(kp + (unsigned)min(16 * j + l16, n - 1) * (unsigned)pitch + 32 * kk + 8 * lq), qf, sc[j]);
+            for (int j = 0; j < 2; ++j) sc[j] = mfma16(*reinterpret_cast<const uint4 *>(kp[j] + 32 * kk), qf, sc[j]);
         }
-        u32x4 vr[VI];
         unsigned odd = 0;                                // values that are not finite (what a row does not see is weighed with 0)
-#pragma unroll
-        for (int u = 0; u < VI; ++u) {
-            const int piece = u * 64 + lane;
-            vr[u] = *reinterpret_cast<const u32x4 *>(vp + (unsigned)min(piece / (D / 8), n - 1) * (unsigned)pitch + (piece % (D / 8)) * 8);
-        }
 #pragma unroll
         for (int u = 0; u < VI; ++u) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) odd |= (unsigned)((vr[u][j] & 0x7F80u) == 0x7F80u) | (unsigned)((vr[u][j] & 0x7F800000u) == 0x7F800000u);
             *reinterpret_cast<u32x4 *>(v_in + u * (512 / D) * L::VROW) = vr[u];
         }
-        unsigned see;
-        if (tail) {
-            see = n < KC ? (1u << n) - 1 : ~0u;
-            const int p0 = full * P + k0, skip = min(max(since - p0, 0), KC), still = min(max(a.sink - p0, 0), KC);
-            see &= (skip < KC ? ~0u << skip : 0u) | (still < KC ? (1u << still) - 1 : ~0u);
-        } else {
-            see = k0 == 0 ? sees_lo : sees_hi;
-            if (a.window > 0) {                          // the rows of the path whose positions the window has left behind
-                for (int j = 0; j < n; ++j) {
-                    const int pos = len + __shfl(depth, k0 + j);
-                    if (pos < since && pos >= a.sink) see &= ~(1u << j);
-                }
-            }
-        }
-        see >>= 4 * lq;
-        float top = m;
+        const auto first_bits = [](int n) { return n >= KC ? ~0u : n <= 0 ? 0u : (1u << n) - 1; };
+        const int p0 = its_len - n_tail + k0, behind = n_tail - k0;      // position of the first; keys of the tail from here on
+        const unsigned in_tail = first_bits(behind) & (~first_bits(since - p0) | first_bits(a.sink - p0));
+        const unsigned rows = (unsigned)(behind >= 0 ? path << min(behind, 63) : path >> min(-behind, 63));
+        unsigned see = in_tail | (rows & ~first_bits(behind) & first_bits(n));
+        see = sb == cs ? see >> 4 * lq : 0u;
+        float top = m;                                   // (which may lie below the largest score so far: see above)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -350,7 +449,7 @@ __global__ __launch_bounds__(64 * W, 2) void page_attn(const AttnArgs a)
 #pragma unroll 1
                     for (int g = 0; g < 4; ++g) {
                         const float pk = __shfl(p[j][e], 16 * g + l16), sk = __shfl(sc[j][e], 16 * g + l16);
-                        const unsigned char *const v = mine + (16 * j + 4 * g + e) * L::VROW;
+                        const unsigned char *const v = piece_of + (16 * j + 4 * g + e) * L::VROW;
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
                             const uint2 x = *reinterpret_cast<const uint2 *>(v + (16 * db + 4 * lq) * 2);
@@ -365,9 +464,9 @@ __global__ __launch_bounds__(64 * W, 2) void page_attn(const AttnArgs a)
 
     // the waves' results, merged in the order of the waves
     {
-        float *const om = reinterpret_cast<float *>(mine);
+        float *const om = reinterpret_cast<float *>(piece_of);
         const float sum = over_quarters(l, [](float x, float y) { return x + y; });
-        if (lq == 0) reinterpret_cast<float2 *>(mine + L::O_BYTES)[l16] = make_float2(m, sum);
+        if (lq == 0) reinterpret_cast<float2 *>(piece_of + L::O_BYTES)[l16] = make_float2(m, sum);
 #pragma unroll
         for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(om + l16 * L::OROW + 16 * db + 4 * lq) = o[db];
     }
@@ -389,8 +488,8 @@ __global__ __launch_bounds__(64 * W, 2) void page_attn(const AttnArgs a)
             num += weight * *reinterpret_cast<const f32x4 *>(smem + w * L::BYTES + (qv * L::OROW + f) * 4);
             den += weight * x.y;
         }
-        const int r = (int)((unsigned)v * a.g_inv >> 16);
-        const size_t vec_at = (size_t)(s * a.R + r) * a.Hq + hk * a.G + (v - r * a.G);
+        const int b = a.bundle == 1 ? 0 : v / per_stream, in = v - b * per_stream, r = (int)((unsigned)in * a.g_inv >> 16);
+        const size_t vec_at = (size_t)((s0 + b) * a.R + r) * a.Hq + hk * a.G + (in - r * a.G);
         if constexpr (SPLIT) {
             const size_t at = (size_t)z * a.M * a.Hq + vec_at;
             if (f == 0) a.part_ml[at] = make_float2(top, den);
@@ -449,24 +548,20 @@ bool misaligned(const void *p, unsigned mask) { return (reinterpret_cast<uintptr
 
 // How a call is cut.
 struct Plan {
-    int waves, splits;
+    int waves, splits, bundle;
 };
 constexpr int MOST_SPLITS = 64;
-long long most_items(const mlora_page_attn &t)
-{
-    const long long pages = t.cache.max_pages;
-    const long long seen = t.window > 0 ? std::min(pages, (long long)t.window / P + 2 + ((long long)t.sink + P - 1) / P) : pages;
-    return seen + 2 + (t.rows_per_stream + KC - 1) / KC;
-}
 Plan plan_of(const mlora_page_attn &t)
 {
     Plan p;
-    const long long items = most_items(t);
+    const long long pages = t.cache.max_pages;
+    const long long seen = t.window > 0 ? std::min(pages, (long long)t.window / P + 2 + ((long long)t.sink + P - 1) / P) : pages;
     const int qv = t.rows_per_stream * (t.n_q_heads / t.cache.n_kv_heads);
-    const long long blocks = (long long)t.cache.n_kv_heads * t.cache.n_streams * ((qv + 15) / 16);
-    p.waves = 4;
-    const long long wanted = std::max(1ll, std::min(1024 / blocks, items / (2 * p.waves)));
-    p.splits = (int)std::min((long long)MOST_SPLITS, wanted);
+    p.bundle = seen < 8 ? 1 : std::max(1, std::min(std::min(16 / qv, 8), t.cache.n_streams));
+    const long long items = p.bundle * (seen + (P - 1 + t.rows_per_stream + KC - 1) / KC);
+    const long long blocks = (long long)t.cache.n_kv_heads * ((t.cache.n_streams + p.bundle - 1) / p.bundle) * ((qv + 15) / 16);
+    p.splits = items < 32 ? 1 : (int)std::max(1ll, std::min(std::min((200 + blocks / 2) / blocks, items / 8), (long long)MOST_SPLITS));
+    p.waves = blocks * p.splits <= 256 ? 8 : 4;
     return p;
 }
 size_t workspace_floats(const mlora_page_attn &t)
@@ -555,6 +650,7 @@ mlora_status mlora_page_attention(const mlora_page_attn *t, const void *q, void 
     a.window = t->window;
     a.sink = std::min(t->sink, P * c.max_pages + 2 * P);
     a.splits = p.splits;
+    a.bundle = p.bundle;
     a.part_out = reinterpret_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float2 *>(a.part_out + (size_t)p.splits * a.M * a.Hq * c.head_dim);
     a.g_inv = (65536u + (unsigned)a.G - 1) / (unsigned)a.G;
@@ -562,18 +658,26 @@ mlora_status mlora_page_attention(const mlora_page_attn *t, const void *q, void 
     a.scale2 = t->scale * 1.44269504088896340736f;
 
     hipStream_t s = (hipStream_t)stream;
-    const dim3 grid((unsigned)a.Hkv, (unsigned)((a.R * a.G + 15) / 16), (unsigned)(a.S * p.splits));
-    const auto go = [&](auto d) {
-        constexpr int D = decltype(d)::value, W = 4;
+    const dim3 grid((unsigned)a.Hkv, (unsigned)((p.bundle * a.R * a.G + 15) / 16), (unsigned)((a.S + p.bundle - 1) / p.bundle * p.splits));
+    const auto go = [&](auto d, auto digits, auto waves) {
+        constexpr int D = decltype(d)::value, N = decltype(digits)::value, W = decltype(waves)::value;
         if (p.splits == 1) {
-            page_attn<D, W, false><<<grid, dim3(64 * W), 0, s>>>(a);
+            page_attn<D, W, N, false><<<grid, dim3(64 * W), 0, s>>>(a);
         } else {
-            page_attn<D, W, true><<<grid, dim3(64 * W), 0, s>>>(a);
+            page_attn<D, W, N, true><<<grid, dim3(64 * W), 0, s>>>(a);
             page_attn_combine<D><<<dim3((unsigned)((a.M * a.Hq * (D / 4) + 255) / 256)), dim3(256), 0, s>>>(a);
         }
     };
-    if (c.head_dim == 64) go(std::integral_constant<int, 64>{});
-    else                  go(std::integral_constant<int, 128>{});
+    const auto by_waves = [&](auto d, auto digits) {
+        if (p.waves == 8) go(d, digits, std::integral_constant<int, 8>{});
+        else              go(d, digits, std::integral_constant<int, 4>{});
+    };
+    const auto by_digits = [&](auto d) {
+        if (a.out_fp32) by_waves(d, std::integral_constant<int, 3>{});
+        else            by_waves(d, std::integral_constant<int, 2>{});
+    };
+    if (c.head_dim == 64) by_digits(std::integral_constant<int, 64>{});
+    else                  by_digits(std::integral_constant<int, 128>{});
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }
 

@@ -3,7 +3,10 @@
 Scores: a query vector's numbers are cut at 2^-22 of its largest, which moves a score by at most scale * max |q| * sum |k| * 2^-22; products of bf16
 (tail, rows) and the conversions, scales and exponents around them are fp32: D + 16 roundings of 2^-24 of sum |q k| * scale.  Each moves a
 weighted mean by twice itself.  Weights: on pages cut at 2^-24 of the page's largest, 64 of them, twice; in the tail two bf16 halves
-(2^-18, with the sum's own roundings 2^-16).  Sums: a rounding of 2^-23 per item and merge."""
+(2^-18, with the sum's own roundings 2^-16).  Sums: a rounding of 2^-23 per item and merge.
+
+Outputs in bf16 are made with two digits to the base 256 instead of three: query vectors are cut at 2^-15 of their largest number, weights at 2^-16 of
+the page's largest."""
 import math
 
 import numpy as np
@@ -18,7 +21,8 @@ pytestmark = pytest.mark.gpu
 def bound(size, q, scale, D, items, want, fp32):
     vmax, s1, k1 = size[..., 0], size[..., 1], size[..., 2]
     qmax = np.abs(q).max(-1)
-    far = 2 * (abs(scale) * k1 * qmax * 2.0 ** -22 + (D + 16) * 2.0 ** -24 * s1) + 2.0 ** -16 + 128 * 2.0 ** -24 + (items + 32) * 2.0 ** -23
+    q_cut, p_cut = (2.0 ** -22, 2.0 ** -24) if fp32 else (2.0 ** -15, 2.0 ** -16)
+    far = 2 * (abs(scale) * k1 * qmax * q_cut + (D + 16) * 2.0 ** -24 * s1) + 2.0 ** -16 + 128 * p_cut + (items + 32) * 2.0 ** -23
     return (vmax * far)[..., None] + (0 if fp32 else np.abs(want) * 2.0 ** -8)
 
 
@@ -224,3 +228,56 @@ def test_what_is_appended_is_seen_alike(gpu):
         # both are within their bounds of one number
         want, size = O.attention(d, 0, q[r:r + 1], k[r:r + 1], v[r:r + 1], [-1], 1, 0.125)
         assert np.all(np.abs(one[0] - tree[r]) <= 2 * bound(size, O.bf16(q[r:r + 1]), 0.125, D, 9, want, True)[0])
+
+
+def test_pages_of_zeros(gpu):
+    """Scale 0: all scores alike, and what the window hides stays hidden; values of zero."""
+    rng = np.random.default_rng(16)
+    c = make(16, 1, 1, 2, 64, 6, 5, [200])
+    pages = c["table"][c["slot"][0], :3]
+    for n in ("k", "v"):
+        c[n][:, pages[1]], c[n + "_scale"][:, pages[1]] = 0, 0
+    q, k, v = bits(rng, 2, 4, 64), bits(rng, 2, 2, 64), bits(rng, 2, 2, 64)
+    for window, sink in ((0, 0), (100, 0), (90, 70)):
+        want, size = O.attention(c, 0, q, k, v, [-1, 0], 2, 0.125, window, sink)
+        got, _ = run(gpu, c, 0, q, k, v, [-1, 0], 2, 0.125, window, sink)
+        assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), 0.125, 64, 9, want, True))
+
+
+@pytest.mark.parametrize("fp32", [True, False])
+@pytest.mark.parametrize("R,G", [(1, 1), (1, 2), (1, 4), (2, 4), (3, 1), (5, 3), (1, 5)])
+def test_streams_that_share_some_of_their_pages(gpu, R, G, fp32):
+    """Bundles of streams: the same pages at the same places, others, none, and other lengths; windows of several starts."""
+    rng = np.random.default_rng(17 + R * G)
+    S, H, D = 19, 2, 64
+    c = make(17, 1, S, H, D, 200, 12, [int(x) for x in rng.integers(0, 700, S)])
+    c = O.reorder(c, [0, 0, 0, 3, 3, 5, 6, 6, 6, 6, 6, 0, 12, 13, 14, 12, 12, 12, 18])
+    k, v = bits(rng, 1, S * 70, H, D), bits(rng, 1, S * 70, H, D)                       # then they go on by themselves
+    c, _ = O.append(c, k, v, 70, [(list(range(rng.integers(0, 71))) + [-1] * 70)[:70] for _ in range(S)])
+    c["table"][c["slot"][7], 1] = -1
+    q, kn, vn = bits(rng, S * R, H * G, D, scale=1.5), bits(rng, S * R, H, D), bits(rng, S * R, H, D)
+    parent = np.array([[rng.integers(-1, max(r, 1)) if r else -1 for r in range(R)] for _ in range(S)]).reshape(-1)
+    for window, sink in ((0, 0), (150, 70)):
+        want, size = O.attention(c, 0, q, kn, vn, parent, R, 0.125, window, sink)
+        got, _ = run(gpu, c, 0, q, kn, vn, parent, R, 0.125, window, sink, fp32)
+        assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), 0.125, D, 17, want, fp32))
+
+
+def test_a_page_of_nan_that_only_one_of_a_bundle_holds(gpu):
+    rng = np.random.default_rng(18)
+    S, H, D = 8, 1, 64
+    c = make(18, 1, S, H, D, 40, 5, [200] * S)
+    c = O.reorder(c, [0, 0, 0, 3, 4, 5, 6, 7])
+    bad = c["table"][c["slot"][4], 1]
+    c["k_scale"][:, bad], c["v_scale"][:, c["table"][c["slot"][6], 0]] = np.nan, np.nan
+    q, kn, vn = bits(rng, S, 2, D), bits(rng, S, 1, D), bits(rng, S, 1, D)
+    kn[1], vn[2], vn[7] = 0x7FC0, 0x7F80, 0x7FC0
+    want, size = O.attention(c, 0, q, kn, vn, [-1] * S, 1, 0.125)
+    got, _ = run(gpu, c, 0, q, kn, vn, [-1] * S, 1, 0.125)
+    for s in range(S):
+        if s in (1, 4, 6, 7):
+            assert np.all(np.isnan(got[s]))
+        elif s == 2:
+            assert np.all(got[s] == np.inf)
+        else:
+            assert np.all(np.abs(got[s] - want[s]) <= bound(size, O.bf16(q), 0.125, D, 9, want, True)[s])

@@ -1,8 +1,10 @@
 // A paged cache of keys and values in 8 bits (see include/mlora_page_cache.h): rows that enter it, streams that become others, copies
 // into another cache.
 //
-// Every call is a block that does the bookkeeping (which pages, which slots) and leaves what the others need in the cache's own words,
-// and a launch that moves the data with blocks all over the card.
+// A call of some hundred streams or fewer is one launch: every block works out what it needs of the bookkeeping (which pages, which slots) by itself,
+// moves its share of the data, and the last block to have read the cache's lists writes them anew.  Who is the last is found by counters that wrap,
+// a line of memory per stream and one above them.  Larger calls, and prompts, are two launches: a block for the bookkeeping, which leaves what the
+// others need in the cache's own words, and blocks that move the data.  (Two launches for a step's calls, too, was: 7.9 us for a reordering.)
 #include <algorithm>
 #include <type_traits>
 
@@ -16,10 +18,12 @@ namespace {
 
 constexpr int P = MLORA_PAGE_TOKENS;
 constexpr int CTRL = 1024;                               // threads of a bookkeeping block; at least MLORA_PAGE_MAX_STREAMS
+constexpr int ONE = 256;                                 // of a block of a call that is one launch; its streams at most
 static_assert(CTRL >= MLORA_PAGE_MAX_STREAMS, "a thread per stream");
 
 // the cache's own words: where the search for free pages starts (no page below is free), then what a call's two launches hand over
-constexpr int OWN_LOW = 0, OWN_COUNT = 1, OWN_PLAN = 64;
+constexpr int OWN_LOW = 0, OWN_COUNT = 1, OWN_TICKETS = 64, TICKET_WORDS = 32;
+__host__ __device__ constexpr int own_plan(int streams) { return OWN_TICKETS + TICKET_WORDS * (streams + 1); }
 struct Plan {
     int first, count, slot, other;
 };
@@ -38,13 +42,14 @@ struct CacheArgs {
 
 __device__ __forceinline__ int slot_of(const CacheArgs &c, int s) { return min(max(c.slot[s], 0), c.S - 1); }
 __device__ __forceinline__ int len_of(const CacheArgs &c, int s) { return min(max(c.len[s], 0), P * c.columns + P - 1); }
-__device__ __forceinline__ Plan *plans(const CacheArgs &c) { return reinterpret_cast<Plan *>(c.own + OWN_PLAN); }
+__device__ __forceinline__ Plan *plans(const CacheArgs &c) { return reinterpret_cast<Plan *>(c.own + own_plan(c.S)); }
 
 // Sums over the threads before this one, and over all of them.  One __syncthreads before `part` is used again is the caller's.
 struct Sums {
     int before, all;
 };
-__device__ __forceinline__ Sums sums_of(int x, int (&part)[CTRL / 64])
+template <int T>
+__device__ __forceinline__ Sums sums_of(int x, int (&part)[T / 64])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int run = x;
@@ -57,12 +62,20 @@ __device__ __forceinline__ Sums sums_of(int x, int (&part)[CTRL / 64])
     __syncthreads();
     int base = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < CTRL / 64; ++w) {
+    for (int w = 0; w < T / 64; ++w) {
         const int y = part[w];
         base += w < wave ? y : 0;
         all += y;
     }
     return Sums{base + run - x, all};
+}
+
+// Thread 0 of a block that has read the lists draws a ticket; true for the last of all (blocks_per_stream) * S blocks.  The counters are zero again then.
+__device__ __forceinline__ bool last_to_read(const CacheArgs &c, int s, unsigned blocks_per_stream)
+{
+    unsigned *const tickets = reinterpret_cast<unsigned *>(c.own + OWN_TICKETS);
+    if (atomicInc(tickets + TICKET_WORDS * (s + 1), blocks_per_stream - 1) != blocks_per_stream - 1) return false;
+    return atomicInc(tickets, (unsigned)c.S - 1) == (unsigned)c.S - 1;
 }
 
 // The last of n ascending numbers, the first of them 0, that is at most i.
@@ -87,22 +100,24 @@ struct AppendArgs {
     int R, n_rows;
 };
 
-constexpr int MAX_FILLED = MLORA_MAX_ROWS / P + MLORA_PAGE_MAX_STREAMS;   // pages that one call can fill: (S * 63 + S * R) / 64
+// pages that one call can fill: (S * 63 + S * R) / 64
+template <int T> constexpr int MOST_FILLED = MLORA_MAX_ROWS / P + T;
 
-// Who enters, and which pages fill.
-__global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
+template <int T>
+struct AppendLds {
+    int count[T], start[T], place[T], part[T / 64], list[MOST_FILLED<T>], last;
+};
+// Who enters, and which pages fill: those of stream s are list[start[s]] and on.  The result is the stream's of the thread's number; `used`: all pages.
+struct Entry {
+    int len, slot, n, used, low;
+};
+template <int T>
+__device__ __forceinline__ Entry append_plan_of(const AppendArgs &a, AppendLds<T> &lds)
 {
-    __shared__ int count[CTRL], start[CTRL], place[CTRL], part[CTRL / 64], list[MAX_FILLED], last;
     const CacheArgs &c = a.c;
     const int tid = threadIdx.x;
-    count[tid] = a.n_rows;
-    if (tid == 0) last = 0;
-    __syncthreads();
-    if (a.rows)
-        for (int i = tid; i < c.S * a.n_rows; i += CTRL) {
-            const int r = a.rows[i], s = i / a.n_rows;
-            if (r < 0 || r >= a.R) atomicMin(&count[s], i - s * a.n_rows);
-        }
+    lds.count[tid] = a.n_rows;
+    if (tid == 0) lds.last = 0;
     const int low = min(max(c.own[OWN_LOW], 0), c.pages) & ~3;
     int len = 0, slot = 0, n = 0, wish = 0;
     if (tid < c.S) {
@@ -110,17 +125,23 @@ __global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
         slot = slot_of(c, tid);
     }
     __syncthreads();
+    if (a.rows)
+        for (int i = tid; i < c.S * a.n_rows; i += T) {
+            const int r = a.rows[i], s = i / a.n_rows;
+            if (r < 0 || r >= a.R) atomicMin(&lds.count[s], i - s * a.n_rows);
+        }
+    __syncthreads();
     if (tid < c.S) {
-        n = count[tid];
+        n = lds.count[tid];
         wish = (len % P + n) / P;
         if (len / P + wish > c.columns) n = wish = 0;
     }
-    const Sums want = sums_of(wish, part);
-    start[tid] = want.before;
-    place[tid] = len / P;
+    const Sums want = sums_of<T>(wish, lds.part);
+    lds.start[tid] = want.before;
+    lds.place[tid] = len / P;
     // the lowest free pages, as many as are wanted
     int found = 0;
-    for (int p0 = low; found < want.all && p0 < c.pages; p0 += 4 * CTRL) {
+    for (int p0 = low; found < want.all && p0 < c.pages; p0 += 4 * T) {
         int refs[4], some = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -129,12 +150,12 @@ __global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
             some += refs[u] <= 0;
         }
         __syncthreads();
-        const Sums at = sums_of(some, part);
+        const Sums at = sums_of<T>(some, lds.part);
         int number = found + at.before;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (refs[u] <= 0) {
-                if (number < want.all) list[number] = p0 + 4 * tid + u;
+                if (number < want.all) lds.list[number] = p0 + 4 * tid + u;
                 ++number;
             }
         found += at.all;
@@ -142,20 +163,35 @@ __global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
     found = min(found, want.all);
     const bool enters = wish == 0 || want.before + wish <= found;
     if (!enters) n = 0;
-    else if (wish > 0) atomicMax(&last, want.before + wish);
+    else if (wish > 0) atomicMax(&lds.last, want.before + wish);
     __syncthreads();
-    const int used = last;                               // (streams that do not enter stand behind all that fill pages)
-    for (int i = tid; i < used; i += CTRL) {
-        const int s = last_from(start, c.S, i);
-        c.table[(size_t)slot_of(c, s) * c.columns + place[s] + (i - start[s])] = list[i];
-        c.refs[list[i]] = 1;
+    const int used = lds.last;                           // (streams that do not enter stand behind all that fill pages)
+    return Entry{len, slot, n, used, used == 0 ? -1 : used < found ? lds.list[used] : lds.list[used - 1] + 1};
+}
+// and what is to be written of it
+template <int T>
+__device__ __forceinline__ void append_commit(const AppendArgs &a, const AppendLds<T> &lds, const Entry &e)
+{
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x;
+    for (int i = tid; i < e.used; i += T) {
+        const int s = last_from(lds.start, c.S, i);
+        c.table[(size_t)slot_of(c, s) * c.columns + lds.place[s] + (i - lds.start[s])] = lds.list[i];
+        c.refs[lds.list[i]] = 1;
     }
     if (tid < c.S) {
-        c.len[tid] = len + n;
-        plans(c)[tid] = Plan{len, n, slot, 0};
-        if (a.appended) a.appended[tid] = n;
+        c.len[tid] = e.len + e.n;
+        if (a.appended) a.appended[tid] = e.n;
     }
-    if (tid == 0 && used > 0) c.own[OWN_LOW] = used < found ? list[used] : list[used - 1] + 1;
+    if (tid == 0 && e.low >= 0) c.own[OWN_LOW] = e.low;
+}
+
+__global__ __launch_bounds__(CTRL) void append_plan(const AppendArgs a)
+{
+    __shared__ AppendLds<CTRL> lds;
+    const Entry e = append_plan_of<CTRL>(a, lds);
+    append_commit<CTRL>(a, lds, e);
+    if ((int)threadIdx.x < a.c.S) plans(a.c)[threadIdx.x] = Plan{e.len, e.n, e.slot, 0};
 }
 
 // A page's 64 x D numbers to codes and a scale: the largest magnitude, as the bits of a bf16 number (which order like it)
@@ -191,18 +227,23 @@ __device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &by)
     return out;
 }
 
-// Block y of a layer, stream and head fills its y-th page; the first one writes the tail as well, behind the page that takes what was there.
+// The rows of a layer, stream and head: they fill its j-th page, `page` of the pool; with the first one the tail is written as well, behind the page that
+// takes what was there.
 template <int D>
-__global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
+struct PageLds {
+    static constexpr int PITCH = P + 16;
+    __align__(16) unsigned char turned[D * PITCH];
+    unsigned tops[2][4];
+};
+template <int D>
+__device__ __forceinline__ void append_head(const AppendArgs &a, PageLds<D> &lds, const Plan &plan, int page, int l, int s, int h, int j)
 {
-    constexpr int PIECES = D / 8, NP = P * PIECES / 256, PITCH = P + 16;
-    __shared__ __align__(16) unsigned char turned[D * PITCH];
-    __shared__ unsigned tops[2][4];
+    constexpr int PIECES = D / 8, NP = P * PIECES / 256, PITCH = PageLds<D>::PITCH;
+    auto &turned = lds.turned;
+    auto &tops = lds.tops;
     const CacheArgs &c = a.c;
-    const int tid = threadIdx.x, head = blockIdx.x, j = blockIdx.y;
-    const int s = head / c.H % c.S, l = head / (c.H * c.S), h = head - (l * c.S + s) * c.H;
-    const Plan plan = plans(c)[s];
-    const int t = plan.first % P, full = plan.first / P, filled = (t + plan.count) / P;
+    const int tid = threadIdx.x;
+    const int t = plan.first % P, filled = (t + plan.count) / P;
     const size_t tail = (((size_t)l * c.S + plan.slot) * c.H + h) * P * D, stream = ((size_t)l * c.S + s) * a.R;
     // token g of those behind the full pages (in the tail up to t), 8 of its features from f on
     const auto from = [&](int g) {
@@ -233,7 +274,6 @@ __global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < 4; ++w) kt = max(kt, tops[0][w]), vt = max(vt, tops[1][w]);
-        const int page = min(max(c.table[(size_t)plan.slot * c.columns + full + j], 0), c.pages - 1);
         const size_t unit = ((size_t)l * c.pages + page) * c.H + h;
         const bool k_ok = kt > 0 && kt < 0x7F80u, v_ok = vt > 0 && vt < 0x7F80u;
         const Divide k_by = divide_by(kt), v_by = divide_by(vt);
@@ -265,6 +305,60 @@ __global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
     }
 }
 
+// Block y of a layer, stream and head takes its y-th page.
+template <int D>
+__global__ __launch_bounds__(256) void append_rows(const AppendArgs a)
+{
+    __shared__ PageLds<D> lds;
+    const CacheArgs &c = a.c;
+    const int head = blockIdx.x, s = head / c.H % c.S, l = head / (c.H * c.S), h = head - (l * c.S + s) * c.H, j = blockIdx.y;
+    const Plan plan = plans(c)[s];
+    if (plan.first % P + plan.count < j * P) return;
+    const int at = plan.first / P + j, page = at < c.columns ? min(max(c.table[(size_t)plan.slot * c.columns + at], 0), c.pages - 1) : 0;
+    append_head<D>(a, lds, plan, page, l, s, h, j);
+}
+
+// A call of at most 64 rows per stream: a block per stream, layer and head, the stream fastest.
+template <int D>
+__global__ __launch_bounds__(ONE) void append_step(const AppendArgs a)
+{
+    __shared__ union Lds {
+        AppendLds<ONE> plan;
+        PageLds<D> page;
+    } lds;
+    __shared__ Plan mine;
+    __shared__ int my_page, is_last;
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, s = (int)blockIdx.x % c.S, unit = (int)blockIdx.x / c.S, l = unit / c.H, h = unit - l * c.H;
+    // its own rows; who else enters only where they fill a page
+    if (tid < 64) {
+        const int r = tid < a.n_rows ? (a.rows ? a.rows[s * a.n_rows + tid] : tid) : -1;
+        const unsigned long long bad = __ballot(r < 0 || r >= a.R);
+        const int n = bad ? __builtin_ctzll(bad) : 64;
+        if (tid == 0) mine = Plan{len_of(c, s), n, slot_of(c, s), 0};
+    }
+    __syncthreads();
+    Plan plan = mine;
+    int page = 0;
+    if (plan.first % P + plan.count >= P) {
+        const Entry e = append_plan_of<ONE>(a, lds.plan);
+        if (tid == s) {
+            mine.count = e.n;
+            my_page = e.n > 0 ? lds.plan.list[lds.plan.start[s]] : 0;
+        }
+        __syncthreads();
+        plan = mine;
+        page = my_page;
+    }
+    if (tid == 0) is_last = last_to_read(c, s, (unsigned)(c.L * c.H));
+    __syncthreads();
+    append_head<D>(a, lds.page, plan, page, l, s, h, 0);
+    if (!is_last) return;
+    __syncthreads();
+    const Entry e = append_plan_of<ONE>(a, lds.plan);
+    append_commit<ONE>(a, lds.plan, e);
+}
+
 // ---------------------------------------------------------------------------------------------- reorder
 
 struct ReorderArgs {
@@ -274,41 +368,62 @@ struct ReorderArgs {
 };
 
 // Slots and lengths.  A stream's plan: its new length, whether its data moves (2: from a slot, 1: it becomes empty, 0: it stays), the slots
-// to and from; the words behind the plans hold what every slot held.
-__global__ __launch_bounds__(CTRL) void reorder_plan(const ReorderArgs a)
+// to and from; and the tokens that its new slot held before.
+template <int T>
+struct ReorderLds {
+    int first[T], taken[T], place[T], held[T], part[T / 64];
+};
+struct Move {
+    Plan plan;
+    int held;
+};
+template <int T>
+__device__ __forceinline__ Move reorder_plan_of(const ReorderArgs &a, ReorderLds<T> &lds)
 {
-    __shared__ int first[CTRL], taken[CTRL], place[CTRL], part[CTRL / 64];
     const CacheArgs &c = a.c;
     const int tid = threadIdx.x, S = c.S;
-    int *const held = c.own + OWN_PLAN + PLAN_WORDS * S;
-    first[tid] = CTRL;
-    taken[tid] = 0;
-    int from = -1, len = 0, slot = 0;
+    lds.first[tid] = T;
+    lds.taken[tid] = 0;
+    lds.held[tid] = 0;
+    int from = -1, len = 0, slot = 0, was = 0, at = 0;
     if (tid < S) {
         from = a.source ? a.source[tid] : tid;
+        was = len_of(c, tid);
+        at = slot_of(c, tid);
         if (from < 0 || from >= S) from = -1;
         if (from >= 0) {
             len = len_of(c, from);
             slot = slot_of(c, from);
         }
-        held[slot_of(c, tid)] = len_of(c, tid);
     }
     __syncthreads();
-    if (from >= 0) atomicMin(&first[from], tid);
+    if (tid < S) lds.held[at] = was;
+    if (from >= 0) atomicMin(&lds.first[from], tid);
     __syncthreads();
-    const bool keeps = from >= 0 && first[from] == tid;
-    if (keeps) taken[slot] = 1;
+    const bool keeps = from >= 0 && lds.first[from] == tid;
+    if (keeps) lds.taken[slot] = 1;
     __syncthreads();
-    const bool open = tid < S && !taken[tid];
-    const Sums slots = sums_of(open, part);
-    if (open) place[slots.before] = tid;
+    const bool open = tid < S && !lds.taken[tid];
+    const Sums slots = sums_of<T>(open, lds.part);
+    if (open) lds.place[slots.before] = tid;
     __syncthreads();
-    const Sums others = sums_of(tid < S && !keeps, part);
-    if (tid < S) {
-        const int to = keeps ? slot : place[others.before];
-        c.slot[tid] = to;
-        c.len[tid] = len;
-        plans(c)[tid] = Plan{len, keeps ? 0 : from >= 0 ? 2 : 1, to, slot};
+    const Sums others = sums_of<T>(tid < S && !keeps, lds.part);
+    if (tid >= S) return Move{};
+    const int to = keeps ? slot : lds.place[others.before];
+    return Move{Plan{len, keeps ? 0 : from >= 0 ? 2 : 1, to, slot}, lds.held[to]};
+}
+
+__global__ __launch_bounds__(CTRL) void reorder_plan(const ReorderArgs a)
+{
+    __shared__ ReorderLds<CTRL> lds;
+    const CacheArgs &c = a.c;
+    const Move m = reorder_plan_of<CTRL>(a, lds);
+    __syncthreads();                                     // (everybody has read slot and len)
+    if ((int)threadIdx.x < c.S) {
+        c.slot[threadIdx.x] = m.plan.slot;
+        c.len[threadIdx.x] = m.plan.first;
+        plans(c)[threadIdx.x] = m.plan;
+        c.own[own_plan(c.S) + PLAN_WORDS * c.S + threadIdx.x] = m.held;
     }
 }
 
@@ -318,16 +433,15 @@ __device__ __forceinline__ void give_up(const CacheArgs &c, int page)
     if (page >= 0 && page < c.pages && atomicSub(&c.refs[page], 1) == 1) atomicMin(&c.own[OWN_LOW], page);
 }
 
-// For every stream: `table_blocks` blocks over its table row, then one per layer and head for its tail.
+// A stream's share of number x: the first `table_blocks` go over its table row, 256 entries each, the others over its tail, a layer and head each.
 // No page is free in between: who gives one up held it, and who takes one takes it from a slot that keeps it.
 template <int D>
-__global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int table_blocks)
+__device__ __forceinline__ void reorder_share(const ReorderArgs &a, const Move &m, int x, int table_blocks)
 {
     const CacheArgs &c = a.c;
-    const Plan plan = plans(c)[blockIdx.y];
-    const int len = plan.first, moves = plan.count, to = plan.slot, from = plan.other;
-    if ((int)blockIdx.x < table_blocks) {
-        const int i = (int)blockIdx.x * 256 + (int)threadIdx.x, full = len / P;
+    const int len = m.plan.first, moves = m.plan.count, to = m.plan.slot, from = m.plan.other;
+    if (x < table_blocks) {
+        const int i = x * 256 + (int)threadIdx.x, full = len / P;
         if (i >= c.columns) return;
         const bool gone = a.window > 0 && (i + 1) * P <= len - a.window + 1 && i * P >= a.sink;
         int *const mine = c.table + (size_t)to * c.columns + i;
@@ -337,7 +451,7 @@ __global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int tab
             *mine = -1;
             return;
         }
-        const int old_full = c.own[OWN_PLAN + PLAN_WORDS * c.S + to] / P;
+        const int old_full = m.held / P;
         const int page = moves == 2 && i < full && !gone ? c.table[(size_t)from * c.columns + i] : -1;
         if (page >= 0 && page < c.pages) atomicAdd(&c.refs[page], 1);
         if (i < old_full) give_up(c, *mine);
@@ -346,11 +460,40 @@ __global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int tab
     }
     const int n = len % P;
     if (moves != 2 || n == 0) return;
-    const int unit = (int)blockIdx.x - table_blocks, l = unit / c.H, h = unit - l * c.H;
+    const int unit = x - table_blocks, l = unit / c.H, h = unit - l * c.H;
     const size_t src = (((size_t)l * c.S + from) * c.H + h) * P * D, dst = (((size_t)l * c.S + to) * c.H + h) * P * D;
     for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
         reinterpret_cast<u32x4 *>(c.k_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.k_tail + src)[i];
         reinterpret_cast<u32x4 *>(c.v_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.v_tail + src)[i];
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int table_blocks)
+{
+    const int s = blockIdx.y;
+    const Move m{plans(a.c)[s], a.c.own[own_plan(a.c.S) + PLAN_WORDS * a.c.S + s]};
+    reorder_share<D>(a, m, blockIdx.x, table_blocks);
+}
+
+// One launch: block x takes shares x, x + gridDim.x, .. of stream blockIdx.y.
+template <int D>
+__global__ __launch_bounds__(ONE) void reorder_step(const ReorderArgs a, int table_blocks, int shares)
+{
+    __shared__ ReorderLds<ONE> lds;
+    __shared__ Move mine;
+    __shared__ int is_last;
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, s = blockIdx.y;
+    const Move m = reorder_plan_of<ONE>(a, lds);
+    if (tid == s) mine = m;
+    __syncthreads();                                     // (the block has read slot and len)
+    if (tid == 0) is_last = last_to_read(c, s, gridDim.x);
+    for (int x = blockIdx.x; x < shares; x += gridDim.x) reorder_share<D>(a, mine, x, table_blocks);
+    __syncthreads();
+    if (is_last && tid < c.S) {
+        c.slot[tid] = m.plan.slot;
+        c.len[tid] = m.plan.first;
     }
 }
 
@@ -369,7 +512,7 @@ __global__ __launch_bounds__(CTRL) void copy_plan(const CopyArgs a)
     __shared__ int part[CTRL / 64], start[CTRL], row[CTRL], too_long;
     const CacheArgs &f = a.from, &t = a.to;
     const int tid = threadIdx.x;
-    int *const marks = f.own + OWN_PLAN + (PLAN_WORDS + 1) * f.S, *const list = t.own + OWN_PLAN + (PLAN_WORDS + 1) * t.S;
+    int *const marks = f.own + own_plan(f.S) + (PLAN_WORDS + 1) * f.S, *const list = t.own + own_plan(t.S) + (PLAN_WORDS + 1) * t.S;
     if (tid == 0) too_long = 0;
     for (int p = tid; p < f.pages; p += CTRL) __hip_atomic_store(&marks[p], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     int len = 0, slot = 0, has = 0;
@@ -383,7 +526,7 @@ __global__ __launch_bounds__(CTRL) void copy_plan(const CopyArgs a)
     }
     __syncthreads();
     if (len / P > t.columns) atomicOr(&too_long, 1);
-    const Sums entries = sums_of(len / P, part);
+    const Sums entries = sums_of<CTRL>(len / P, part);
     start[tid] = entries.before;
     row[tid] = slot;
     __syncthreads();
@@ -397,7 +540,7 @@ __global__ __launch_bounds__(CTRL) void copy_plan(const CopyArgs a)
     for (int p0 = 0; p0 < f.pages; p0 += CTRL) {
         const int p = p0 + tid, held = p < f.pages ? __hip_atomic_load(&marks[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
         __syncthreads();
-        const Sums at = sums_of(held > 0, part);
+        const Sums at = sums_of<CTRL>(held > 0, part);
         const int place = used + at.before;
         if (p < f.pages) marks[p] = held > 0 ? place : -1;
         if (held > 0 && place < t.pages) {
@@ -428,7 +571,7 @@ __global__ __launch_bounds__(256) void copy_move(const CopyArgs a, int page_bloc
     const int tid = threadIdx.x, l = blockIdx.y, b = blockIdx.x;
     if (b < page_blocks) {
         if (b >= t.own[OWN_COUNT]) return;
-        const int page = t.own[OWN_PLAN + (PLAN_WORDS + 1) * t.S + b];
+        const int page = t.own[own_plan(t.S) + (PLAN_WORDS + 1) * t.S + b];
         const size_t src = ((size_t)l * f.pages + page) * f.H, dst = ((size_t)l * t.pages + b) * t.H;
         const u32x4 *const ks = reinterpret_cast<const u32x4 *>(f.k + src * P * D), *const vs = reinterpret_cast<const u32x4 *>(f.v + src * P * D);
         u32x4 *const kt = reinterpret_cast<u32x4 *>(t.k + dst * P * D), *const vt = reinterpret_cast<u32x4 *>(t.v + dst * P * D);
@@ -450,7 +593,7 @@ __global__ __launch_bounds__(256) void copy_move(const CopyArgs a, int page_bloc
             reinterpret_cast<u32x4 *>(t.v_tail + dst)[i] = reinterpret_cast<const u32x4 *>(f.v_tail + src)[i];
         }
     } else if (l == 0) {
-        const int *const marks = f.own + OWN_PLAN + (PLAN_WORDS + 1) * f.S;
+        const int *const marks = f.own + own_plan(f.S) + (PLAN_WORDS + 1) * f.S;
         const long long i = (long long)(b - page_blocks - tail_blocks) * 256 + tid;
         const int s = (int)(i / t.columns), column = (int)(i - (long long)s * t.columns);
         if (s >= t.S) return;
@@ -500,7 +643,7 @@ extern "C" {
 size_t mlora_page_cache_own_words(int32_t n_streams, int32_t n_pages)
 {
     if (n_streams <= 0 || n_streams > MLORA_PAGE_MAX_STREAMS || n_pages <= 0 || n_pages > MLORA_PAGE_MAX_PAGES) return 0;
-    return (size_t)OWN_PLAN + (size_t)(PLAN_WORDS + 1) * n_streams + n_pages;
+    return (size_t)own_plan(n_streams) + (size_t)(PLAN_WORDS + 1) * n_streams + n_pages;
 }
 
 mlora_status mlora_page_cache_append(const mlora_page_cache *c, const void *k_new, const void *v_new, int32_t rows_per_stream,
@@ -515,8 +658,14 @@ mlora_status mlora_page_cache_append(const mlora_page_cache *c, const void *k_ne
     if (n < 1 || n > rows_per_stream) return MLORA_ESHAPE;
     const AppendArgs a{args_of(c), reinterpret_cast<const uint16_t *>(k_new), reinterpret_cast<const uint16_t *>(v_new), rows, appended, rows_per_stream, n};
     hipStream_t s = (hipStream_t)stream;
+    const unsigned heads = (unsigned)(c->n_layers * c->n_streams * c->n_kv_heads);
+    if (n <= P && c->n_streams <= ONE) {
+        if (c->head_dim == 64) append_step<64><<<dim3(heads), dim3(ONE), 0, s>>>(a);
+        else                   append_step<128><<<dim3(heads), dim3(ONE), 0, s>>>(a);
+        return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
+    }
     append_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
-    const dim3 grid((unsigned)(c->n_layers * c->n_streams * c->n_kv_heads), (unsigned)((P - 1 + n) / P));
+    const dim3 grid(heads, (unsigned)((P - 1 + n) / P));
     if (c->head_dim == 64) append_rows<64><<<grid, dim3(256), 0, s>>>(a);
     else                   append_rows<128><<<grid, dim3(256), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
@@ -530,9 +679,15 @@ mlora_status mlora_page_cache_reorder(const mlora_page_cache *c, const int32_t *
     if (window < 0 || sink < 0) return MLORA_ESHAPE;
     const ReorderArgs a{args_of(c), source, window, sink};
     hipStream_t s = (hipStream_t)stream;
+    const int table_blocks = (c->max_pages + 255) / 256, shares = table_blocks + c->n_layers * c->n_kv_heads;
+    if (c->n_streams <= ONE) {
+        const dim3 grid((unsigned)std::min(shares, std::max(1, 1024 / c->n_streams)), (unsigned)c->n_streams);
+        if (c->head_dim == 64) reorder_step<64><<<grid, dim3(ONE), 0, s>>>(a, table_blocks, shares);
+        else                   reorder_step<128><<<grid, dim3(ONE), 0, s>>>(a, table_blocks, shares);
+        return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
+    }
     reorder_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
-    const int table_blocks = (c->max_pages + 255) / 256;
-    const dim3 grid((unsigned)(table_blocks + c->n_layers * c->n_kv_heads), (unsigned)c->n_streams);
+    const dim3 grid((unsigned)shares, (unsigned)c->n_streams);
     if (c->head_dim == 64) reorder_move<64><<<grid, dim3(256), 0, s>>>(a, table_blocks);
     else                   reorder_move<128><<<grid, dim3(256), 0, s>>>(a, table_blocks);
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;

@@ -106,6 +106,18 @@ def test_many_streams(gpu):
     check_append(gpu, make(10, 1, 1000, 1, 64, 9000, 5, [0] * 1000), 4, None, calls=1)
 
 
+@pytest.mark.parametrize("S", [64, 65, 255, 256, 257])
+@pytest.mark.parametrize("n", [1, 63, 64, 65])
+def test_calls_of_one_launch_and_of_two(gpu, S, n):
+    """Streams and rows at the borders, streams that fill a page beside others that do not, and a pool that ends among them."""
+    if S * n > 4096:
+        n = 4096 // S
+    rng = np.random.default_rng(S + n)
+    lengths = [int(x) for x in rng.integers(0, 130, S)]
+    check_append(gpu, make(S, 1, S, 2, 64, 3 * S // 2 + 40, 4, lengths), n, None, calls=3)
+    check_reorder(gpu, make(S, 1, S, 2, 64, 2 * S, 3, lengths), rng.integers(-1, S, S).tolist(), 20, 3, calls=3)
+
+
 def test_pages_are_taken_from_the_lowest_on(gpu):
     """A pool of several looks, with holes; and one that has none."""
     used = [p for p in range(9001) if p % 4099 != 7 and p != 9000]

@@ -203,27 +203,31 @@ __device__ __forceinline__ unsigned top_bits(const u32x4 &x, unsigned top)
 }
 // Codes of 8 numbers.  All are moved by the power of two that brings `top` into [1/2, 1), since 127 x may not be a number.  127 x / top is a quotient of
 // numbers of 15 and 8 bits: it is a half, which one correction of the product with the reciprocal gives exactly, or further from one than
-// 2^-17, and the codes are those of the exact quotient.
+// 2^-17, and the codes are those of the exact quotient.  1.5 * 2^23 added rounds to whole numbers; the low byte of the sum's bits is the code.
 struct Divide {
-    float top, inverse;
-    int shift;
+    float top, inverse, by, more;                        // x is multiplied by `by`, and by `more` where that is not 1 (top below 2^-100)
 };
 __device__ __forceinline__ Divide divide_by(unsigned bits)
 {
     const float top = bf16_bits_to_float(bits);
     const int e = __builtin_amdgcn_frexp_expf(top);
     const float t = __builtin_ldexpf(top, -e);
-    return Divide{t, __builtin_amdgcn_rcpf(t), -e};
+    return Divide{t, __builtin_amdgcn_rcpf(t), __builtin_ldexpf(127.f, min(-e, 100)), __builtin_ldexpf(1.f, max(-e - 100, 0))};
 }
-__device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &by)
+__device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &d)
 {
-    u32x2 out = {0, 0};
+    unsigned n[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float f = 127.f * __builtin_ldexpf(bf16_bits_to_float(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu), by.shift), near = f * by.inverse;
-        const float quotient = __builtin_fmaf(__builtin_fmaf(-near, by.top, f), by.inverse, near);
-        out[i / 4] |= ((unsigned)(int)rintf(quotient) & 0xFFu) << 8 * (i % 4);
+        float f = (i & 1 ? __uint_as_float(x[i / 2] & 0xFFFF0000u) : bf16_bits_to_float(x[i / 2])) * d.by;
+        if (d.more != 1.f) f *= d.more;
+        const float near = f * d.inverse, quotient = __builtin_fmaf(__builtin_fmaf(-near, d.top, f), d.inverse, near);
+        n[i] = __float_as_uint(quotient + 12582912.f);
     }
+    u32x2 out;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        out[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(n[4 * i + 3], n[4 * i + 2], 0x0C0C0400u), __builtin_amdgcn_perm(n[4 * i + 1], n[4 * i], 0x0C0C0400u), 0x05040100u);
     return out;
 }
 
@@ -231,14 +235,13 @@ __device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &by)
 // takes what was there.
 template <int D>
 struct PageLds {
-    static constexpr int PITCH = P + 16;
-    __align__(16) unsigned char turned[D * PITCH];
+    __align__(16) unsigned char turned[D * P];           // [feature][token], groups of 16 tokens in another order in each run of 8 features
     unsigned tops[2][4];
 };
 template <int D>
 __device__ __forceinline__ void append_head(const AppendArgs &a, PageLds<D> &lds, const Plan &plan, int page, int l, int s, int h, int j)
 {
-    constexpr int PIECES = D / 8, NP = P * PIECES / 256, PITCH = PageLds<D>::PITCH;
+    constexpr int PIECES = D / 8, NP = P * PIECES / 256;         // a thread has 8 features of NP tokens in a row
     auto &turned = lds.turned;
     auto &tops = lds.tops;
     const CacheArgs &c = a.c;
@@ -251,11 +254,12 @@ __device__ __forceinline__ void append_head(const AppendArgs &a, PageLds<D> &lds
         return ((stream + row) * c.H + h) * D;
     };
     if (j < filled) {
+        const int f = tid % PIECES * 8, t0 = tid / PIECES * NP;
         u32x4 kx[NP], vx[NP];
         unsigned kt = 0, vt = 0;
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
-            const int piece = u * 256 + tid, g = j * P + piece / PIECES, f = piece % PIECES * 8;
+            const int g = j * P + t0 + u;
             const size_t at = g < t ? tail + (size_t)g * D + f : from(g) + f;
             kx[u] = *reinterpret_cast<const u32x4 *>((g < t ? c.k_tail : a.k_new) + at);
             vx[u] = *reinterpret_cast<const u32x4 *>((g < t ? c.v_tail : a.v_new) + at);
@@ -276,22 +280,33 @@ __device__ __forceinline__ void append_head(const AppendArgs &a, PageLds<D> &lds
         for (int w = 0; w < 4; ++w) kt = max(kt, tops[0][w]), vt = max(vt, tops[1][w]);
         const size_t unit = ((size_t)l * c.pages + page) * c.H + h;
         const bool k_ok = kt > 0 && kt < 0x7F80u, v_ok = vt > 0 && vt < 0x7F80u;
-        const Divide k_by = divide_by(kt), v_by = divide_by(vt);
+        const Divide k_by = divide_by(k_ok ? kt : 0x3F80u), v_by = divide_by(v_ok ? vt : 0x3F80u);
+        u32x2 v[NP];
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
-            const int piece = u * 256 + tid, g = piece / PIECES, f = piece % PIECES * 8;
-            *reinterpret_cast<u32x2 *>(c.k + (unit * P + g) * D + f) = k_ok ? codes_of(kx[u], k_by) : u32x2{0, 0};
-            const u32x2 v = v_ok ? codes_of(vx[u], v_by) : u32x2{0, 0};
+            *reinterpret_cast<u32x2 *>(c.k + (unit * P + t0 + u) * D + f) = k_ok ? codes_of(kx[u], k_by) : u32x2{0, 0};
+            v[u] = v_ok ? codes_of(vx[u], v_by) : u32x2{0, 0};
+        }
+        // values feature by feature: the thread's tokens of a feature are NP bytes in a row
 #pragma unroll
-            for (int e = 0; e < 8; ++e) turned[(f + e) * PITCH + g] = (unsigned char)(v[e / 4] >> 8 * (e % 4));
+        for (int e = 0; e < 8; ++e) {
+            unsigned word = 0;
+#pragma unroll
+            for (int u = 0; u < NP; ++u) word |= (v[u][e / 4] >> 8 * (e % 4) & 0xFFu) << 8 * u;
+            unsigned char *const to = turned + (f + e) * P + (t0 ^ (f / 8 & 3) * 16);
+            if constexpr (NP == 4) *reinterpret_cast<unsigned *>(to) = word;
+            else                   *reinterpret_cast<unsigned short *>(to) = (unsigned short)word;
         }
         if (tid == 0) {
             c.k_scale[unit] = kt < 0x7F80u ? bf16_bits_to_float(kt) / 127.f : __builtin_nanf("");
             c.v_scale[unit] = vt < 0x7F80u ? bf16_bits_to_float(vt) / 127.f : __builtin_nanf("");
         }
         __syncthreads();
-        for (int i = tid; i < D * P / 16; i += 256)
-            *reinterpret_cast<u32x4 *>(c.v + unit * P * D + 16 * i) = *reinterpret_cast<const u32x4 *>(turned + (i / 4) * PITCH + (i % 4) * 16);
+#pragma unroll
+        for (int u = 0; u < D * P / 16 / 256; ++u) {
+            const int i = u * 256 + tid, feature = i / 4, group = i % 4 ^ (feature / 8 & 3);
+            *reinterpret_cast<u32x4 *>(c.v + unit * P * D + 16 * i) = *reinterpret_cast<const u32x4 *>(turned + feature * P + group * 16);
+        }
     }
     if (j == 0) {
         // (everybody has read the old tail: the first barrier above)
@@ -575,9 +590,15 @@ __global__ __launch_bounds__(256) void copy_move(const CopyArgs a, int page_bloc
         const size_t src = ((size_t)l * f.pages + page) * f.H, dst = ((size_t)l * t.pages + b) * t.H;
         const u32x4 *const ks = reinterpret_cast<const u32x4 *>(f.k + src * P * D), *const vs = reinterpret_cast<const u32x4 *>(f.v + src * P * D);
         u32x4 *const kt = reinterpret_cast<u32x4 *>(t.k + dst * P * D), *const vt = reinterpret_cast<u32x4 *>(t.v + dst * P * D);
-        for (int i = tid; i < f.H * (P * D / 16); i += 256) {
-            kt[i] = ks[i];
-            vt[i] = vs[i];
+        constexpr int AT_ONCE = 4;
+        for (int i = tid; i < f.H * (P * D / 16); i += 256 * AT_ONCE) {
+            u32x4 k[AT_ONCE], v[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i + u * 256 < f.H * (P * D / 16)) k[u] = ks[i + u * 256], v[u] = vs[i + u * 256];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i + u * 256 < f.H * (P * D / 16)) kt[i + u * 256] = k[u], vt[i + u * 256] = v[u];
         }
         for (int h = tid; h < f.H; h += 256) {
             t.k_scale[dst + h] = f.k_scale[src + h];

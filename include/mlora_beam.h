@@ -12,8 +12,8 @@
  * or +infinity.  Places that no candidate takes have score -infinity, their own row as source, token `pad`, length 0, and are not finished: beams
  * without candidates.  A search starts from one beam with score 0 and W - 1 with -infinity.
  *
- * Scores are compared in 64 bits, from sums of exponentials in fp32 of at most 64 numbers that are added in 64 bits (a sum is off by a few
- * 2^-29 of itself), and rounded once, to the fp32 number that is given out.  Conventions as in mlora_w4.h.
+ * Scores are compared in 64 bits, from exponentials in fp32 that are added 64 by 64 in fp32 and beyond that in 64 bits (a logarithm of a sum is
+ * off by 10^-8 as a rule, by 2^-17 at most), and rounded once, to the fp32 number that is given out.  Conventions as in mlora_w4.h.
  */
 #ifndef MLORA_BEAM_H
 #define MLORA_BEAM_H
@@ -40,7 +40,7 @@ typedef struct {
 size_t mlora_beam_workspace_bytes(const mlora_beam *d);
 
 /* All of the arrays but the logits have an entry for every row.
- *   logits          [G * W][vocab], alignment of one element (rows of finished beams are not read)
+ *   logits          [G * W][vocab], alignment of one element (what rows of finished beams hold does not count)
  *   score           fp32;  length, finished  int32 (finished: not 0)
  *   source          out int32: the row that the new beam continues (what mlora_page_cache_reorder takes)
  *   token           out int32

@@ -51,48 +51,76 @@ __device__ __forceinline__ float max_with(float x)
     return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)));
 }
 
+// The largest of the lanes that hold a chunk together: neighbours, pairs, halves of 8 lanes, of 16
+template <bool FP32>
+__device__ __forceinline__ float chunk_max(float x)
+{
+    x = max_with<0xB1>(x);
+    x = max_with<0x4E>(x);
+    x = max_with<0x141>(x);
+    if constexpr (FP32) x = max_with<0x140>(x);
+    return x;
+}
+
+// e^d.  The fp32 number next to 1 / log 2 alone would make all exponentials of a row too large or too small together, by 10^-8 for each unit of d.
+__device__ __forceinline__ float exp_of(float d)
+{
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(d, 1.44269502162933349609f, d * 1.92596303350001e-8f));
+}
+
 // A wave per slice and row: 16 bytes per lane and load, side by side, so that a chunk is 8 (bf16) or 16 (fp32) neighbouring lanes.
 template <bool FP32>
 __global__ __launch_bounds__(256) void beam_stats(const BeamArgs a)
 {
-    constexpr int E = FP32 ? 4 : 8, LOADS = SLICE / (64 * E);
+    constexpr int E = FP32 ? 4 : 8, LOADS = SLICE / (64 * E), SIZE = FP32 ? 4 : 2;
     const int lane = threadIdx.x & 63, slice = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), row = blockIdx.y;
-    if (slice >= a.slices || a.finished[row] != 0) return;
-    const char *const z = reinterpret_cast<const char *>(a.logits) + (size_t)row * a.V * (FP32 ? 4 : 2);
-    const int first = slice * SLICE;
-    float x[LOADS][E];
+    if (slice >= a.slices) return;
+    const char *const z = reinterpret_cast<const char *>(a.logits) + ((size_t)row * a.V + (size_t)slice * SLICE) * SIZE;
+    float *const tops = a.chunk_top + ((size_t)row * a.slices + slice) * (SLICE / CHUNK);
+    const int n = a.V - slice * SLICE;                   // tokens from here on
+    const bool head = lane % (CHUNK / E) == 0;
     u32x4 raw[LOADS];
+    if (n >= SLICE) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int v = first + (i * 64 + lane) * E;
-        if (v + E <= a.V) raw[i] = *reinterpret_cast<const u32x4_any *>(z + (size_t)v * (FP32 ? 4 : 2));
-    }
-    float top = NONE;
+        for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const u32x4_any *>(z + (i * 64 + lane) * 16);
+    } else {
+        // the vocabulary's last slice: whole pieces, one that is not, and -infinity behind it
+        constexpr unsigned NOTHING = FP32 ? 0xFF800000u : 0xFF80FF80u;
+        u32x4 rest = {NOTHING, NOTHING, NOTHING, NOTHING};
+        const int whole = n / E;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int v = first + (i * 64 + lane) * E;
-        float most = NONE;
+        for (int e = 0; e < E; ++e)
+            if (whole * E + e < n) {
+                if constexpr (FP32) rest[e] = reinterpret_cast<const unsigned *>(z)[whole * E + e];
+                else                rest[e / 2] = e & 1 ? (rest[e / 2] & 0xFFFFu) | (unsigned)reinterpret_cast<const uint16_t *>(z)[whole * E + e] << 16
+                                                        : (rest[e / 2] & 0xFFFF0000u) | reinterpret_cast<const uint16_t *>(z)[whole * E + e];
+            }
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (v + E <= a.V) x[i][e] = FP32 ? __uint_as_float(raw[i][e % 4]) : bf16_bits_to_float(e & 1 ? raw[i][e / 2] >> 16 : raw[i][e / 2] & 0xFFFFu);
-            else              x[i][e] = v + e < a.V ? logit_at<FP32>(z, v + e) : NONE;
-            most = fmaxf(most, x[i][e]);
+        for (int i = 0; i < LOADS; ++i) {
+            raw[i] = u32x4{NOTHING, NOTHING, NOTHING, NOTHING};
+            if (i * 64 + lane < whole) raw[i] = *reinterpret_cast<const u32x4_any *>(z + (i * 64 + lane) * 16);
+            if (i * 64 + lane == whole) raw[i] = rest;
         }
-        most = max_with<0xB1>(most);                     // neighbours, pairs, halves of 8, of 16
-        most = max_with<0x4E>(most);
-        most = max_with<0x141>(most);
-        if constexpr (FP32) most = max_with<0x140>(most);
-        if (lane % (CHUNK / E) == 0) a.chunk_top[(size_t)row * a.slices * 64 + v / CHUNK] = most;
+    }
+    if (a.finished[row] != 0) return;
+    const auto at = [&](int i, int e) { return FP32 ? __uint_as_float(raw[i][e % 4]) : e & 1 ? __uint_as_float(raw[i][e / 2 % 4] & 0xFFFF0000u) : bf16_bits_to_float(raw[i][e / 2 % 4]); };
+    float top = NONE, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        float most = at(i, 0);
+#pragma unroll
+        for (int e = 1; e < E; ++e) most = fmaxf(most, at(i, e));
+        most = chunk_max<FP32>(fmaxf(most, NONE));
+        if (head) tops[(i * 64 + lane) * E / CHUNK] = most;
         top = fmaxf(top, most);
     }
 #pragma unroll
     for (int d = 8; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     const float from = top == NONE ? 0.f : top;
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((x[i][e] - from) * 1.44269504088896340736f);
+        for (int e = 0; e < E; ++e) sum += exp_of(at(i, e) - from);
     double all = sum;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);

@@ -18,6 +18,7 @@ constexpr int CHUNK = 64, SLICE = 64 * CHUNK;            // tokens
 constexpr int PICK = 1024;                               // threads of beam_pick
 constexpr int W_MAX = MLORA_BEAM_MAX_BEAMS;
 constexpr int LIST = W_MAX * CHUNK;                      // candidates that are ranked at once
+constexpr int QUADS = 1024;                              // groups of four chunks that are looked at one by one
 constexpr int HELD = 8;                                  // loads of beam_pick at once
 constexpr float NONE = -__builtin_inff();
 
@@ -166,6 +167,10 @@ __device__ __forceinline__ bool before(const Candidate &x, const Candidate &y)
     return x.rank > y.rank || (x.rank == y.rank && later(y, x));
 }
 
+struct Quads {                                           // groups of four chunks with one that may count
+    f32x4 z[QUADS];
+    int task[QUADS], at[QUADS], found;
+};
 struct List {
     long long rank[LIST];
     float z[LIST];
@@ -211,6 +216,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
     constexpr int WAVES = PICK / 64;
     __shared__ Beam beams[W_MAX];
     __shared__ List list;
+    __shared__ Quads quads_of;
     __shared__ Candidate best[W_MAX], wave_best[WAVES];
     __shared__ int at_least;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), W = a.W, row0 = (int)blockIdx.x * W;
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) next = fmaxf(next, __shfl_xor(next, d));
             const float from = next == NONE ? 0.f : next;
-            sum = sum * exp((double)top - (double)from) + part * exp((double)here - (double)from);
+            sum = sum * (double)exp_of(top - from) + part * (double)exp_of(here - from);
             top = next;
         }
 #pragma unroll
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
         const double per = a.power == 0.f ? 1. : exp(-(double)a.power * __shfl(logs, 1));
         if (lane == 0) beams[b] = Beam{score, lse, per, done, isfinite(score) && (done || isfinite(lse)), tokens};
     }
-    if (tid == 0) list.found = 0, at_least = in_order(NONE);
+    if (tid == 0) list.found = quads_of.found = 0, at_least = in_order(NONE);
     __syncthreads();
 
     // The W best chunks.  Of each wave's 64 lanes, the W-th best best chunk: that many chunks are at least as good, so nothing below the largest
@@ -285,13 +291,14 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
     }
     {
         const unsigned key = (unsigned)in_order(mine) ^ 0x80000000u;
-        unsigned lo = 0;                                 // the largest key that W lanes reach, bit by bit from above
+        unsigned lo = 0;                                 // the largest key that W lanes reach, two bits at a time from above, to 20 bits
 #pragma unroll 1
-        for (int bit = 31; bit >= 0; --bit) {
-            const unsigned t = lo | 1u << bit;
-            if (__popcll(__ballot(key >= t)) >= W) lo = t;
+        for (int bit = 30; bit >= 12; bit -= 2) {
+            const unsigned t1 = lo | 1u << bit, t2 = lo | 2u << bit, t3 = lo | 3u << bit;
+            const bool one = __popcll(__ballot(key >= t1)) >= W, two = __popcll(__ballot(key >= t2)) >= W, three = __popcll(__ballot(key >= t3)) >= W;
+            lo = three ? t3 : two ? t2 : one ? t1 : lo;
         }
-        if (lane == 0) atomicMax(&at_least, (int)(lo ^ 0x80000000u));
+        if (lane == 0) atomicMax(&at_least, max((int)(lo ^ 0x80000000u), in_order(NONE)));
     }
     __syncthreads();
     const int bound = at_least;
@@ -314,26 +321,26 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
         const float from = lowest(b);
         for (int q0 = 0; q0 < s.n; q0 += 64 * HELD) {
             if (!all) load(s, q0, z);
-            unsigned some = 0;
 #pragma unroll
-            for (int u = 0; u < HELD; ++u) some |= top_of(z[u]) >= from ? 1u << u : 0u;
-            while (some) {
-                const int q = q0 + __builtin_ctz(some) * 64 + lane;
-                some &= some - 1;
-                const f32x4 four = s.tops[q];
-#pragma unroll 1
-                for (int e = 0; e < 4; ++e) {
-                    const float x = e & 2 ? (e & 1 ? four[3] : four[2]) : (e & 1 ? four[1] : four[0]);
-                    const double rank = ranked(b, x);
-                    if (x >= from && x > NONE && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), x, s.beam, 4 * (s.first + q) + e});
+            for (int u = 0; u < HELD; ++u)
+                if (top_of(z[u]) >= from) {
+                    const int i = atomicAdd(&quads_of.found, 1);
+                    if (i < QUADS) quads_of.z[i] = z[u], quads_of.task[i] = t, quads_of.at[i] = q0 + u * 64 + lane;
                 }
-            }
         }
     }
     __syncthreads();
-    const int found = list.found, chunks = min(found, W);
+    const int some = quads_of.found;
+    for (int i = tid; i < 4 * min(some, QUADS); i += PICK) {
+        const Share s = share_of(quads_of.task[i / 4]);
+        const float x = quads_of.z[i / 4][i % 4];
+        const double rank = ranked(beams[s.beam], x);
+        if (rank > (double)NONE && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), x, s.beam, 4 * (s.first + quads_of.at[i / 4]) + i % 4});
+    }
     __syncthreads();
-    if (found <= LIST) {
+    const int found = list.found, chunks = min(some > QUADS ? W : found, W);
+    __syncthreads();
+    if (found <= LIST && some <= QUADS) {
         best_of(list, found, W, best);
     } else {
         // (more equals than the list holds: one after the other)

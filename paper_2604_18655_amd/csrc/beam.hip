@@ -307,8 +307,8 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
     const auto lowest = [&](const Beam &b) {
         if (!b.live) return __builtin_inff();
         if (bound_rank == NONE) return -3.4028235e38f;
-        const double low = ((double)bound_rank - fabs((double)bound_rank) * 0x1p-22) / b.per - b.score, z = low + b.lse;
-        return (float)(z - (fabs(low) + fabs(b.lse)) * 0x1p-22);
+        const double low = ((double)bound_rank - fabs((double)bound_rank) * 0x1p-22 - 0x1p-148) / b.per - b.score, z = low + b.lse;
+        return fmaxf((float)(z - (fabs(low) + fabs(b.lse)) * 0x1p-22), -3.4028235e38f);        // (a number, also where `per` is next to nothing)
     };
     for (int t = wave; t < W * parts; t += WAVES) {
         const Share s = share_of(t);

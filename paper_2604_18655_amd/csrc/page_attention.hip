@@ -327,10 +327,10 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
         }
         sum -= 16u * __float_as_uint(P_BITS<N>);
         top = top == UNSEEN || !seen ? UNSEEN : N == 3 ? __builtin_fmaf(-NUMBER_F, per, from) : from;
-        // The sums so far are relative to a maximum that is raised only where a page's is more than 2^40 times as heavy: fp32 has the room, and what the
+        // The sums so far are relative to a maximum that is raised only where a page's is more than 2^8 times as heavy: fp32 has the room, and what the
         // lane holds need not be scaled for every page that is a little heavier.
-        if (__ballot(top > m + 40.f)) {
-            const float m_new = top > m + 40.f ? top : m, keep = __builtin_amdgcn_exp2f(m - finite_or_0(m_new));
+        if (__ballot(top > m + 8.f)) {
+            const float m_new = top > m + 8.f ? top : m, keep = __builtin_amdgcn_exp2f(m - finite_or_0(m_new));
             m = m_new;
             l *= keep;
             over *= keep;

@@ -81,6 +81,23 @@ def test_a_large_vocabulary(gpu):
     check(gpu, *inputs(5, 2, 8, 128256, "bf16", done=0.2, power=1.0), dtype="bf16", power=1.0, eos=5)
 
 
+def test_a_vocabulary_of_a_million(gpu):
+    check(gpu, *inputs(16, 1, 3, 1000003, "bf16"), dtype="bf16")
+
+
+@pytest.mark.parametrize("power", [50.0, 300.0, 1e30])
+def test_scores_that_the_length_makes_nothing_of(gpu, power):
+    """20^-50 leaves little of a score, 20^-300 and less nothing at all: then all candidates are equal, and the lower beam's best come first."""
+    z, score, length, done, W = inputs(17, 2, 4, 3000, "fp32")
+    done[2] = 1
+    if power == 50.0:
+        want, _ = O.beam_select(z, score, length, done, W, power=power)
+    else:
+        want = {"source": np.repeat([0, 4], 4), "token": np.concatenate([np.argsort(-z[0], kind="stable")[:4], np.argsort(-z[4], kind="stable")[:4]])}
+    got = run(gpu, z, score, length, done, W, "fp32", power=power)
+    assert np.array_equal(got["source"].cpu().numpy(), want["source"]) and np.array_equal(got["token"].cpu().numpy(), want["token"])
+
+
 def test_more_groups_than_the_card_has_units(gpu):
     check(gpu, *inputs(6, 400, 2, 300, "fp32"))
 

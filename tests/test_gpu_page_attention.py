@@ -281,3 +281,24 @@ def test_a_page_of_nan_that_only_one_of_a_bundle_holds(gpu):
             assert np.all(got[s] == np.inf)
         else:
             assert np.all(np.abs(got[s] - want[s]) <= bound(size, O.bf16(q), 0.125, D, 9, want, True)[s])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_values_and_rising_maxima(gpu, D):
+    """Every page heavier than the one before, by up to 2^20, and values of 1e33: sums relative to an older maximum must not pass the largest
+    number."""
+    rng = np.random.default_rng(19)
+    c = make(19, 1, 1, 1, D, 30, 25, [24 * 64 + 9])
+    c["k"][:] = 0
+    for i in range(24):
+        c["k"][:, c["table"][c["slot"][0], i], :, :, 0] = 4 * i + rng.integers(0, 4, (1, 1, 64))
+    c["k_scale"][:], c["v_scale"][:] = 1.0, 1e33 / 127
+    c["k_tail"][:] = 0
+    q, kn = np.zeros((3, 2, D), np.int16), np.zeros((3, 1, D), np.int16)
+    vn = bits(rng, 3, 1, D)
+    for scale in (0.02, 0.2, 1.0, 3.5):
+        q[..., 0] = 0x3F80                                                                # 1
+        want, size = O.attention(c, 0, q, kn, vn, [-1, 0, 1], 3, float(np.float32(scale)))
+        for fp32 in (True, False):
+            got, _ = run(gpu, c, 0, q, kn, vn, [-1, 0, 1], 3, scale, fp32=fp32)
+            assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), scale, D, 30, want, fp32))

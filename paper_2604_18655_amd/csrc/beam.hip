@@ -3,7 +3,12 @@
 // A candidate's rank inside its beam is its logit's, so the W best of a group lie in the W chunks of 64 tokens whose best candidates are the
 // best W (an order without equals: ranked score, beam, logit, token).  beam_stats goes over the logits once and leaves the largest logit
 // of every chunk, and of every slice of 64 chunks the maximum and the sum of exponentials.  beam_pick, a block per group, makes
-// the beams' log-sums, finds the W chunks among all, and looks at the 64 logits of each once more.
+// the beams' log-sums, finds the best chunks by a bound that W of them reach, and looks at their logits once more.
+//
+// A large call is bound by the logits (8 groups of 16 beams over 128256 bf16 tokens: 9 to 11 us for 29.5 MB), and then by beam_pick's chain: what
+// the slices left, the bound, the chunks above it, their logits, their order, 1 to 3 us each (12 to 14 us there; one group of 4 beams over
+// 32003 fp32 tokens 3.5 to 5.3 us and 8).  Ranks for all chunks in 64 bits, candidates ranked by one thread each and a bound found bit by bit were:
+// 84 us for that block.
 #include <type_traits>
 
 #include "common.hpp"
@@ -18,6 +23,7 @@ constexpr int CHUNK = 64, SLICE = 64 * CHUNK;            // tokens
 constexpr int PICK = 1024;                               // threads of beam_pick
 constexpr int W_MAX = MLORA_BEAM_MAX_BEAMS;
 constexpr int LIST = W_MAX * CHUNK;                      // candidates that are ranked at once
+constexpr int FEW = 64, AT_ONCE = 4;                     // chunks that are looked at before they are ranked (256: 8 groups of 16 beams 13.2 -> 15.9 us); logits per thread at once
 constexpr int QUADS = 1024;                              // groups of four chunks that are looked at one by one
 constexpr int HELD = 8;                                  // loads of beam_pick at once
 constexpr float NONE = -__builtin_inff();
@@ -171,6 +177,9 @@ struct Quads {                                           // groups of four chunk
     f32x4 z[QUADS];
     int task[QUADS], at[QUADS], found;
 };
+struct Place {
+    int beam, at;
+};
 struct List {
     long long rank[LIST];
     float z[LIST];
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
 {
     constexpr int WAVES = PICK / 64;
     __shared__ Beam beams[W_MAX];
-    __shared__ List list;
+    __shared__ List list, picked;
     __shared__ Quads quads_of;
     __shared__ Candidate best[W_MAX], wave_best[WAVES];
     __shared__ int at_least;
@@ -268,7 +277,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
         const double per = a.power == 0.f ? 1. : exp(-(double)a.power * __shfl(logs, 1));
         if (lane == 0) beams[b] = Beam{score, lse, per, done, isfinite(score) && (done || isfinite(lse)), tokens};
     }
-    if (tid == 0) list.found = quads_of.found = 0, at_least = in_order(NONE);
+    if (tid == 0) list.found = picked.found = quads_of.found = 0, at_least = in_order(NONE);
     __syncthreads();
 
     // The W best chunks.  Of each wave's 64 lanes, the W-th best best chunk: that many chunks are at least as good, so nothing below the largest
@@ -338,59 +347,81 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
         if (rank > (double)NONE && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), x, s.beam, 4 * (s.first + quads_of.at[i / 4]) + i % 4});
     }
     __syncthreads();
-    const int found = list.found, chunks = min(some > QUADS ? W : found, W);
-    __syncthreads();
-    if (found <= LIST && some <= QUADS) {
-        best_of(list, found, W, best);
-    } else {
-        // (more equals than the list holds: one after the other)
-        Candidate last{0x7FFFFFFFFFFFFFFFll, 0.f, -1, -1};
-        for (int n = 0; n < chunks; ++n) {
-            Candidate top{in_order((double)NONE), NONE, W, 0};
-            for (int t = wave; t < W * parts; t += WAVES) {
-                const Share s = share_of(t);
-                const Beam &b = beams[s.beam];
-                const float from = lowest(b);
-                for (int c = lane; c < (b.finished ? 1 : 4 * s.n); c += 64) {
-                    const float z = b.finished ? (s.first == 0 ? 0.f : NONE) : reinterpret_cast<const float *>(s.tops)[c];
-                    const Candidate x{in_order(ranked(b, z)), z, s.beam, 4 * s.first + c};
-                    if (z > NONE && (b.finished || z >= from) && x.rank > in_order((double)NONE) && before(last, x) && before(x, top)) top = x;
+    const int found = list.found;
+
+    // The logits of n chunks that reach the bound, and rank `least`
+    const auto look_at = [&](int n, const auto &chunk, long long least) {
+        for (int i0 = tid; i0 < n * CHUNK; i0 += PICK * AT_ONCE) {
+            float z[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = i0 + u * PICK;
+                z[u] = NONE;
+                if (i < n * CHUNK) {
+                    const Place of = chunk(i / CHUNK);
+                    const int v = of.at * CHUNK + i % CHUNK;
+                    if (beams[of.beam].finished) z[u] = i % CHUNK == 0 ? 0.f : NONE;
+                    else if (v < a.V)            z[u] = logit_at<FP32>(reinterpret_cast<const char *>(a.logits) + (size_t)(row0 + of.beam) * a.V * (FP32 ? 4 : 2), v);
                 }
             }
-#pragma unroll 1
-            for (int d = 1; d < 64; d *= 2) {
-                const Candidate x{__shfl_xor(top.rank, d), __shfl_xor(top.z, d), __shfl_xor(top.beam, d), __shfl_xor(top.at, d)};
-                if (before(x, top)) top = x;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = i0 + u * PICK;
+                if (!(z[u] > NONE)) continue;
+                const Place of = chunk(i / CHUNK);
+                const double rank = ranked(beams[of.beam], z[u]);
+                if (rank > (double)NONE && in_order((float)rank) >= bound && in_order(rank) >= least)
+                    picked.put(Candidate{in_order(rank), z[u], of.beam, of.at * CHUNK + i % CHUNK});
             }
-            if (lane == 0) wave_best[wave] = top;
-            __syncthreads();
-            last = wave_best[0];
-#pragma unroll 1
-            for (int w = 1; w < WAVES; ++w)
-                if (before(wave_best[w], last)) last = wave_best[w];
-            if (tid == 0) best[n] = last;
-            __syncthreads();
         }
+        __syncthreads();
+    };
+    // As a rule few chunks reach the bound, and few of their logits.
+    int m = LIST + 1;
+    if (found <= FEW && some <= QUADS) {
+        look_at(found, [&](int i) { return Place{list.beam[i], list.at[i]}; }, in_order((double)NONE));
+        m = picked.found;
     }
-
-    // Their logits: none that is worse than the best of the W-th chunk counts.
-    if (tid == 0) list.found = 0;
-    __syncthreads();
-    const long long worst = chunks < W ? in_order((double)NONE) : best[W - 1].rank;
-    for (int i = tid; i < chunks * CHUNK; i += PICK) {
-        const Candidate of = best[i / CHUNK];
-        const Beam &b = beams[of.beam];
-        const int v = b.finished ? i % CHUNK : of.at * CHUNK + i % CHUNK;
-        float z = NONE;
-        if (b.finished)   z = v == 0 ? 0.f : NONE;
-        else if (v < a.V) z = logit_at<FP32>(reinterpret_cast<const char *>(a.logits) + (size_t)(row0 + of.beam) * a.V * (FP32 ? 4 : 2), v);
-        const double rank = ranked(b, z);
-        if (rank > (double)NONE && in_order(rank) >= worst) list.put(Candidate{in_order(rank), z, of.beam, v});
+    if (m > LIST) {
+        // Else those of the W best chunks, of which there are W, that are no worse than the best of the W-th.
+        __syncthreads();
+        if (tid == 0) picked.found = 0;
+        if (found <= LIST && some <= QUADS) {
+            best_of(list, found, W, best);
+        } else {
+            // (more equals than the list holds: one after the other)
+            Candidate last{0x7FFFFFFFFFFFFFFFll, 0.f, -1, -1};
+            for (int n = 0; n < W; ++n) {
+                Candidate top{in_order((double)NONE), NONE, W, 0};
+                for (int t = wave; t < W * parts; t += WAVES) {
+                    const Share s = share_of(t);
+                    const Beam &b = beams[s.beam];
+                    const float from = lowest(b);
+                    for (int c = lane; c < (b.finished ? 1 : 4 * s.n); c += 64) {
+                        const float z = b.finished ? (s.first == 0 ? 0.f : NONE) : reinterpret_cast<const float *>(s.tops)[c];
+                        const Candidate x{in_order(ranked(b, z)), z, s.beam, 4 * s.first + c};
+                        if (z > NONE && (b.finished || z >= from) && x.rank > in_order((double)NONE) && before(last, x) && before(x, top)) top = x;
+                    }
+                }
+#pragma unroll 1
+                for (int d = 1; d < 64; d *= 2) {
+                    const Candidate x{__shfl_xor(top.rank, d), __shfl_xor(top.z, d), __shfl_xor(top.beam, d), __shfl_xor(top.at, d)};
+                    if (before(x, top)) top = x;
+                }
+                if (lane == 0) wave_best[wave] = top;
+                __syncthreads();
+                last = wave_best[0];
+#pragma unroll 1
+                for (int w = 1; w < WAVES; ++w)
+                    if (before(wave_best[w], last)) last = wave_best[w];
+                if (tid == 0) best[n] = last;
+                __syncthreads();
+            }
+        }
+        look_at(W, [&](int i) { return Place{best[i].beam, best[i].at}; }, best[W - 1].rank);
+        m = picked.found;
     }
-    __syncthreads();
-    const int m = list.found;
-    __syncthreads();
-    best_of(list, m, W, best);
+    best_of(picked, m, W, best);
     if (tid < W) {
         const int row = row0 + tid;
         if (tid < m) {

@@ -18,9 +18,12 @@
 // row i of product t) these are the 16 that O^T += V^T . P^T wants from it.  Values are stored feature by feature for that.
 // The tail and the step's rows are bf16, with scores and weights (two bf16 halves) as in tree_attention.hip.
 //
-// What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 5.1 TB/s); else the vector work around the weights, some 300 to 400
-// instructions per page and tile.  So whole numbers become floats and back by adding 1.5 * 2^23 or 2^23 where that is free (an accumulator's start, the
-// addend of a multiplication) and not by conversions.
+// What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 77 us, 5.3 TB/s), or, in short ones, the launch and the trips
+// length, table, page (333 tokens 4.7 us); else the vector work around the weights, some 250 to 290 instructions per page and tile (8 trees of 30
+// rows, 2048 tokens of window, 8 heads of 64: 20 us, of which 11 are vector instructions).  So whole numbers become floats and back by adding
+// 1.5 * 2^23 or 2^23 where that is free (an accumulator's start, the addend of a multiplication) and not by conversions, and sums are rescaled
+// only where a maximum rises by much.  The next page's keys are asked for behind the scores: without that 22 -> 39 us, with the values, too, on their way
+// earlier no difference.
 #include <algorithm>
 #include <type_traits>
 
@@ -546,7 +549,7 @@ __global__ __launch_bounds__(256) void page_attn_combine(const AttnArgs a)
 
 bool misaligned(const void *p, unsigned mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; }
 
-// How a call is cut.
+// How a call is cut.  Lines drawn from 28 calls with 4, 8 and 16 waves and 1 to 64 splits, us in a graph.
 struct Plan {
     int waves, splits, bundle;
 };
@@ -557,9 +560,14 @@ Plan plan_of(const mlora_page_attn &t)
     const long long pages = t.cache.max_pages;
     const long long seen = t.window > 0 ? std::min(pages, (long long)t.window / P + 2 + ((long long)t.sink + P - 1) / P) : pages;
     const int qv = t.rows_per_stream * (t.n_q_heads / t.cache.n_kv_heads);
+    // Streams of a bundle may share pages, but each has a tail of its own to be gone through: 21 streams of one query vector and one page 4.5 us, in
+    // bundles of 16 19.  Four beams on 4096 shared tokens take a quarter of the pages (22 -> 13 us without the merge).
     p.bundle = seen < 8 ? 1 : std::max(1, std::min(std::min(16 / qv, 8), t.cache.n_streams));
     const long long items = p.bundle * (seen + (P - 1 + t.rows_per_stream + KC - 1) / KC);
     const long long blocks = (long long)t.cache.n_kv_heads * ((t.cache.n_streams + p.bundle - 1) / p.bundle) * ((qv + 15) / 16);
+    // Shared items cost a second launch (2.4 us at least) and pay from about four per wave on (11 items: 8.3 -> 6.9 with one block; 127: 25 -> 8.2 with 16),
+    // up to some 200 blocks of eight waves (64 blocks, 3 / 4 splits: 15.0 / 15.3; 8 blocks of 3125 items, 24 / 32: 77.0 / 78.1).  Calls that fill the
+    // card without have blocks of four waves (512 blocks of 37 items: 21.3, of eight waves 23.0).  16 waves are best nowhere.
     p.splits = items < 32 ? 1 : (int)std::max(1ll, std::min(std::min((200 + blocks / 2) / blocks, items / 8), (long long)MOST_SPLITS));
     p.waves = blocks * p.splits <= 256 ? 8 : 4;
     return p;

@@ -4,7 +4,8 @@
 // A call of some hundred streams or fewer is one launch: every block works out what it needs of the bookkeeping (which pages, which slots) by itself,
 // moves its share of the data, and the last block to have read the cache's lists writes them anew.  Who is the last is found by counters that wrap,
 // a line of memory per stream and one above them.  Larger calls, and prompts, are two launches: a block for the bookkeeping, which leaves what the
-// others need in the cache's own words, and blocks that move the data.  (Two launches for a step's calls, too, was: 7.9 us for a reordering.)
+// others need in the cache's own words, and blocks that move the data.  (Two launches for a step's calls, too, was: 8 beams of 16 layers reordered
+// in 7.9 us instead of 5.7, 64 streams with a window in 8.0 instead of 5.4.)
 #include <algorithm>
 #include <type_traits>
 
@@ -231,6 +232,9 @@ __device__ __forceinline__ u32x2 codes_of(const u32x4 &x, const Divide &d)
     return out;
 }
 
+// A prompt of 4096 rows of 8 heads of 128 features, 25 MB read and written: 7.2 to 8.9 us, a launch and three dependent trips among it (values turned
+// byte by byte and divided by the hardware's steps: 10.9).
+//
 // The rows of a layer, stream and head: they fill its j-th page, `page` of the pool; with the first one the tail is written as well, behind the page that
 // takes what was there.
 template <int D>
@@ -578,6 +582,7 @@ __global__ __launch_bounds__(CTRL) void copy_plan(const CopyArgs a)
     }
 }
 
+// 384 pages of 2 layers of 8 heads of 64 features, 100 MB: 24 to 28 us (3.6 to 4.2 TB/s), and 6 for copy_plan.
 // Blocks over the pages of a layer, then over the tails of its streams and heads, then (in the first layer) over the table.
 template <int D>
 __global__ __launch_bounds__(256) void copy_move(const CopyArgs a, int page_blocks, int tail_blocks)

@@ -203,20 +203,19 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
                 for (int g = 0; g < N; ++g) qd[g][kk][w] = d[g];
             }
     }
-    // lane sb * R + r: the rows that row r of a stream may see, itself and what it continues (a parent must be an earlier row: the walk
-    // strictly descends, so it ends and stays in bounds whatever the array holds)
+    // lane b * R + r: the rows that row r of stream b may see, itself and what it continues.  A parent must be an earlier row, so a path has at most
+    // 64; each step doubles what is known of all of them.
     const int my_row = a.bundle == 1 ? lane : lane % a.R, row_lane = sb * a.R + row;
     unsigned anc_lo = my_row < 32 ? 1u << my_row : 0u, anc_hi = my_row >= 32 ? 1u << (my_row - 32) : 0u;
     if (a.R > 1) {
-        const int up0 = lane < streams * a.R ? a.parent[s0 * a.R + lane] : -1;
-        int r = up0 < my_row ? up0 : -1;
-        while (__ballot(r >= 0)) {
-            if (r >= 0) {
-                anc_lo |= r < 32 ? 1u << r : 0u;
-                anc_hi |= r >= 32 ? 1u << (r - 32) : 0u;
-            }
-            const int up = __shfl(up0, lane - my_row + max(r, 0));
-            r = r >= 0 && up < r ? up : -1;
+        int up = lane < streams * a.R ? a.parent[s0 * a.R + lane] : -1;
+        up = up < my_row ? up : -1;
+        while (__ballot(up >= 0)) {
+            const int of = lane - my_row + max(up, 0), further = __shfl(up, of);
+            const unsigned lo = (unsigned)__shfl((int)anc_lo, of), hi = (unsigned)__shfl((int)anc_hi, of);
+            anc_lo |= up >= 0 ? lo : 0u;
+            anc_hi |= up >= 0 ? hi : 0u;
+            up = up >= 0 ? further : -1;
         }
     }
     const int depth = __popc(anc_lo) + __popc(anc_hi) - 1;             // of row `my_row`

@@ -5,7 +5,7 @@
 // moves its share of the data, and the last block to have read the cache's lists writes them anew.  Who is the last is found by counters that wrap,
 // a line of memory per stream and one above them.  Larger calls, and prompts, are two launches: a block for the bookkeeping, which leaves what the
 // others need in the cache's own words, and blocks that move the data.  (Two launches for a step's calls, too, was: 8 beams of 16 layers reordered
-// in 7.9 us instead of 5.7, 64 streams with a window in 8.0 instead of 5.4.)
+// in 7.9 us, now 5.0, 64 streams with a window in 8.0, now 5.2.)
 #include <algorithm>
 #include <type_traits>
 
@@ -390,7 +390,7 @@ struct ReorderArgs {
 // to and from; and the tokens that its new slot held before.
 template <int T>
 struct ReorderLds {
-    int first[T], taken[T], place[T], held[T], part[T / 64];
+    int first[T], taken[T], place[T], slot[T], len[T], held[T], part[T / 64];
 };
 struct Move {
     Plan plan;
@@ -404,31 +404,30 @@ __device__ __forceinline__ Move reorder_plan_of(const ReorderArgs &a, ReorderLds
     lds.first[tid] = T;
     lds.taken[tid] = 0;
     lds.held[tid] = 0;
-    int from = -1, len = 0, slot = 0, was = 0, at = 0;
+    int from = -1, was = 0, at = 0;
     if (tid < S) {
         from = a.source ? a.source[tid] : tid;
         was = len_of(c, tid);
         at = slot_of(c, tid);
         if (from < 0 || from >= S) from = -1;
-        if (from >= 0) {
-            len = len_of(c, from);
-            slot = slot_of(c, from);
-        }
+        lds.slot[tid] = at;
+        lds.len[tid] = was;
     }
     __syncthreads();
     if (tid < S) lds.held[at] = was;
     if (from >= 0) atomicMin(&lds.first[from], tid);
     __syncthreads();
+    const int slot = from >= 0 ? lds.slot[from] : 0, len = from >= 0 ? lds.len[from] : 0;
     const bool keeps = from >= 0 && lds.first[from] == tid;
     if (keeps) lds.taken[slot] = 1;
     __syncthreads();
-    const bool open = tid < S && !lds.taken[tid];
-    const Sums slots = sums_of<T>(open, lds.part);
-    if (open) lds.place[slots.before] = tid;
+    // free slots and streams that look for one, both counted at once
+    const bool open = tid < S && !lds.taken[tid], looks = tid < S && !keeps;
+    const int before = sums_of<T>((int)open + ((int)looks << 16), lds.part).before;
+    if (open) lds.place[before & 0xFFFF] = tid;
     __syncthreads();
-    const Sums others = sums_of<T>(tid < S && !keeps, lds.part);
     if (tid >= S) return Move{};
-    const int to = keeps ? slot : lds.place[others.before];
+    const int to = keeps ? slot : lds.place[before >> 16];
     return Move{Plan{len, keeps ? 0 : from >= 0 ? 2 : 1, to, slot}, lds.held[to]};
 }
 
@@ -452,52 +451,55 @@ __device__ __forceinline__ void give_up(const CacheArgs &c, int page)
     if (page >= 0 && page < c.pages && atomicSub(&c.refs[page], 1) == 1) atomicMin(&c.own[OWN_LOW], page);
 }
 
-// A stream's share of number x: the first `table_blocks` go over its table row, 256 entries each, the others over its tail, a layer and head each.
-// No page is free in between: who gives one up held it, and who takes one takes it from a slot that keeps it.
+// Block x of n that a stream has: its share of the table row, 256 entries at a time, and of the tails, a layer and head at a time.  No page is free in between: who gives one up held it, and who takes one takes it from a slot that keeps it.
 template <int D>
-__device__ __forceinline__ void reorder_share(const ReorderArgs &a, const Move &m, int x, int table_blocks)
+__device__ __forceinline__ void reorder_share(const ReorderArgs &a, const Move &m, int x, int n)
 {
     const CacheArgs &c = a.c;
-    const int len = m.plan.first, moves = m.plan.count, to = m.plan.slot, from = m.plan.other;
-    if (x < table_blocks) {
-        const int i = x * 256 + (int)threadIdx.x, full = len / P;
-        if (i >= c.columns) return;
+    const int len = m.plan.first, moves = m.plan.count, to = m.plan.slot, from = m.plan.other, full = len / P, old_full = m.held / P;
+    for (int i = x * 256 + (int)threadIdx.x; i < max(full, moves ? old_full : 0); i += n * 256) {
         const bool gone = a.window > 0 && (i + 1) * P <= len - a.window + 1 && i * P >= a.sink;
         int *const mine = c.table + (size_t)to * c.columns + i;
         if (moves == 0) {
-            if (i >= full || !gone) return;
+            if (!gone) continue;
             give_up(c, *mine);
             *mine = -1;
-            return;
+            continue;
         }
-        const int old_full = m.held / P;
         const int page = moves == 2 && i < full && !gone ? c.table[(size_t)from * c.columns + i] : -1;
         if (page >= 0 && page < c.pages) atomicAdd(&c.refs[page], 1);
         if (i < old_full) give_up(c, *mine);
-        if (i < max(full, old_full)) *mine = page;
-        return;
+        *mine = page;
     }
-    const int n = len % P;
-    if (moves != 2 || n == 0) return;
-    const int unit = x - table_blocks, l = unit / c.H, h = unit - l * c.H;
-    const size_t src = (((size_t)l * c.S + from) * c.H + h) * P * D, dst = (((size_t)l * c.S + to) * c.H + h) * P * D;
-    for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
-        reinterpret_cast<u32x4 *>(c.k_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.k_tail + src)[i];
-        reinterpret_cast<u32x4 *>(c.v_tail + dst)[i] = reinterpret_cast<const u32x4 *>(c.v_tail + src)[i];
+    if (moves != 2) return;
+    constexpr int HEAD = P * D / 8, PER = HEAD / 256;    // pieces of a head's tail, of them a thread's
+    const int pieces = len % P * (D / 8), units = c.L * c.H;
+    if (pieces == 0) return;
+    u32x4 *const ks = reinterpret_cast<u32x4 *>(c.k_tail), *const vs = reinterpret_cast<u32x4 *>(c.v_tail);
+    for (int unit = x; unit < units; unit += n) {
+        const int l = unit / c.H;
+        const size_t head = (size_t)l * (c.S - 1) * c.H + unit;        // [l][slot][h] is l * S * H + slot * H + h
+        const size_t src = (head + (size_t)from * c.H) * HEAD + threadIdx.x, dst = (head + (size_t)to * c.H) * HEAD + threadIdx.x;
+        u32x4 k[PER], v[PER];
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+            if ((int)threadIdx.x + u * 256 < pieces) k[u] = ks[src + u * 256], v[u] = vs[src + u * 256];
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+            if ((int)threadIdx.x + u * 256 < pieces) ks[dst + u * 256] = k[u], vs[dst + u * 256] = v[u];
     }
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a, int table_blocks)
+__global__ __launch_bounds__(256) void reorder_move(const ReorderArgs a)
 {
     const int s = blockIdx.y;
     const Move m{plans(a.c)[s], a.c.own[own_plan(a.c.S) + PLAN_WORDS * a.c.S + s]};
-    reorder_share<D>(a, m, blockIdx.x, table_blocks);
+    reorder_share<D>(a, m, blockIdx.x, gridDim.x);
 }
 
-// One launch: block x takes shares x, x + gridDim.x, .. of stream blockIdx.y.
 template <int D>
-__global__ __launch_bounds__(ONE) void reorder_step(const ReorderArgs a, int table_blocks, int shares)
+__global__ __launch_bounds__(ONE) void reorder_step(const ReorderArgs a)
 {
     __shared__ ReorderLds<ONE> lds;
     __shared__ Move mine;
@@ -508,7 +510,7 @@ __global__ __launch_bounds__(ONE) void reorder_step(const ReorderArgs a, int tab
     if (tid == s) mine = m;
     __syncthreads();                                     // (the block has read slot and len)
     if (tid == 0) is_last = last_to_read(c, s, gridDim.x);
-    for (int x = blockIdx.x; x < shares; x += gridDim.x) reorder_share<D>(a, mine, x, table_blocks);
+    reorder_share<D>(a, mine, blockIdx.x, gridDim.x);
     __syncthreads();
     if (is_last && tid < c.S) {
         c.slot[tid] = m.plan.slot;
@@ -705,17 +707,18 @@ mlora_status mlora_page_cache_reorder(const mlora_page_cache *c, const int32_t *
     if (window < 0 || sink < 0) return MLORA_ESHAPE;
     const ReorderArgs a{args_of(c), source, window, sink};
     hipStream_t s = (hipStream_t)stream;
-    const int table_blocks = (c->max_pages + 255) / 256, shares = table_blocks + c->n_layers * c->n_kv_heads;
+    // Blocks of a stream: one per layer and head, up to some 512 in all (each draws a ticket, and tickets of a stream are drawn one after the other: 129 of
+    // each of 8 streams 5.4 us, 64 4.8).
+    const int blocks = std::max(1, std::min(std::max(c->n_layers * c->n_kv_heads, (c->max_pages + 255) / 256), 512 / c->n_streams));
+    const dim3 grid((unsigned)blocks, (unsigned)c->n_streams);
     if (c->n_streams <= ONE) {
-        const dim3 grid((unsigned)std::min(shares, std::max(1, 1024 / c->n_streams)), (unsigned)c->n_streams);
-        if (c->head_dim == 64) reorder_step<64><<<grid, dim3(ONE), 0, s>>>(a, table_blocks, shares);
-        else                   reorder_step<128><<<grid, dim3(ONE), 0, s>>>(a, table_blocks, shares);
+        if (c->head_dim == 64) reorder_step<64><<<grid, dim3(ONE), 0, s>>>(a);
+        else                   reorder_step<128><<<grid, dim3(ONE), 0, s>>>(a);
         return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
     }
     reorder_plan<<<dim3(1), dim3(CTRL), 0, s>>>(a);
-    const dim3 grid((unsigned)shares, (unsigned)c->n_streams);
-    if (c->head_dim == 64) reorder_move<64><<<grid, dim3(256), 0, s>>>(a, table_blocks);
-    else                   reorder_move<128><<<grid, dim3(256), 0, s>>>(a, table_blocks);
+    if (c->head_dim == 64) reorder_move<64><<<grid, dim3(256), 0, s>>>(a);
+    else                   reorder_move<128><<<grid, dim3(256), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }
 

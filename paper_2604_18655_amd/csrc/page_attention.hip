@@ -16,7 +16,8 @@
 // the page's own maximum; a page's sum of weights is the sum of the very integers that multiply the values.  Scores are K . Q^T: a lane
 // holds 16 keys of ONE query vector, and if the keys of a page are dealt to the products in the right order (key 16 * (i / 4) + 4 * t + i % 4 is
 // row i of product t) these are the 16 that O^T += V^T . P^T wants from it.  Values are stored feature by feature for that.
-// The tail and the step's rows are bf16, with scores and weights (two bf16 halves) as in tree_attention.hip.
+// The tail and the step's rows are bf16, with scores and weights as in tree_attention.hip, the weights as N bf16 numbers each (two leave outputs off by
+// 10^-6, which shows in fp32 where nearly all that a row sees is tail).
 //
 // What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 77 us, 5.3 TB/s), or, in short ones, the launch and the trips
 // length, table, page (333 tokens 4.7 us); else the vector work around the weights, some 250 to 290 instructions per page and tile (8 trees of 30
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
         const float base = finite_or_0(top), keep = __builtin_amdgcn_exp2f(m - base);
         m = top;
         float sum = 0.f, p[2][4];
-        uint32_t hi[4], lo[4];
+        uint32_t part[N][4];                             // the weights as N bf16 numbers each
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -425,22 +426,26 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                hi[2 * j + i] = pack_bf16(p[j][2 * i], p[j][2 * i + 1]);
-                lo[2 * j + i] = pack_bf16(p[j][2 * i] - bf16_bits_to_float(hi[2 * j + i] & 0xFFFFu), p[j][2 * i + 1] - __uint_as_float(hi[2 * j + i] & 0xFFFF0000u));
+                float x = p[j][2 * i], y = p[j][2 * i + 1];
+#pragma unroll
+                for (int g = 0; g < N; ++g) {
+                    part[g][2 * j + i] = pack_bf16(x, y);
+                    x -= bf16_bits_to_float(part[g][2 * j + i] & 0xFFFFu);
+                    y -= __uint_as_float(part[g][2 * j + i] & 0xFFFF0000u);
+                }
             }
         }
         l = l * keep + sum;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] *= keep;
         if (!__ballot(odd)) {
-            const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
                 const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4 *)(v_out + db * 32)));
                 const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4 *)(v_out + 16 * L::VROW + db * 32)));
                 const uint4 vf = make_uint4(x.x, x.y, y.x, y.y);
-                o[db] = mfma16(vf, ph, o[db]);
-                o[db] = mfma16(vf, pl, o[db]);
+#pragma unroll
+                for (int g = 0; g < N; ++g) o[db] = mfma16(vf, make_uint4(part[g][0], part[g][1], part[g][2], part[g][3]), o[db]);
             }
         } else {
             // zeros times infinity would be NaN: key by key, those that the row sees

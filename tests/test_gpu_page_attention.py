@@ -2,11 +2,11 @@
 
 Scores: a query vector's numbers are cut at 2^-22 of its largest, which moves a score by at most scale * max |q| * sum |k| * 2^-22; products of bf16
 (tail, rows) and the conversions, scales and exponents around them are fp32: D + 16 roundings of 2^-24 of sum |q k| * scale.  Each moves a
-weighted mean by twice itself.  Weights: on pages cut at 2^-24 of the page's largest, 64 of them, twice; in the tail two bf16 halves
-(2^-18, with the sum's own roundings 2^-16).  Sums: a rounding of 2^-23 per item and merge.
+weighted mean by twice itself.  Weights: on pages cut at 2^-24 of the page's largest, 64 of them, twice; in the tail three bf16 numbers
+(2^-27, with the sum's own roundings 2^-21).  Sums: a rounding of 2^-23 per item and merge.
 
 Outputs in bf16 are made with two digits to the base 256 instead of three: query vectors are cut at 2^-15 of their largest number, weights at 2^-16 of
-the page's largest."""
+the page's largest, and in the tail two bf16 numbers make a weight (2^-18, with the sum's own roundings 2^-16)."""
 import math
 
 import numpy as np
@@ -21,8 +21,8 @@ pytestmark = pytest.mark.gpu
 def bound(size, q, scale, D, items, want, fp32):
     vmax, s1, k1 = size[..., 0], size[..., 1], size[..., 2]
     qmax = np.abs(q).max(-1)
-    q_cut, p_cut = (2.0 ** -22, 2.0 ** -24) if fp32 else (2.0 ** -15, 2.0 ** -16)
-    far = 2 * (abs(scale) * k1 * qmax * q_cut + (D + 16) * 2.0 ** -24 * s1) + 2.0 ** -16 + 128 * p_cut + (items + 32) * 2.0 ** -23
+    q_cut, p_cut, tail = (2.0 ** -22, 2.0 ** -24, 2.0 ** -21) if fp32 else (2.0 ** -15, 2.0 ** -16, 2.0 ** -16)
+    far = 2 * (abs(scale) * k1 * qmax * q_cut + (D + 16) * 2.0 ** -24 * s1) + tail + 128 * p_cut + (items + 32) * 2.0 ** -23
     return (vmax * far)[..., None] + (0 if fp32 else np.abs(want) * 2.0 ** -8)
 
 

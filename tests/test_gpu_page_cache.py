@@ -188,6 +188,14 @@ def test_copies(gpu, D, source):
     check_copy(gpu, c, make(51, 2, len(source), 3, D, 30, 11, [70] * len(source)), source)
 
 
+@pytest.mark.parametrize("pages,table", [(41, 9), (60, 9), (500, 40)])
+def test_copies_into_larger_pools(gpu, pages, table):
+    c = O.reorder(make(56, 2, 5, 3, 64, 40, 9, [300, 64, 63, 512, 0]), [0, 0, 2, 3, 0])
+    for source in ([0, 1, 2, 3, 4], [3, 3], [-1, 2]):
+        to = check_copy(gpu, c, make(57, 2, len(source), 3, 64, pages, table, [70] * len(source)), source)
+        assert to["len"].tolist() == [max(0, c["len"][i]) if i >= 0 else 0 for i in source]
+
+
 def test_copies_that_find_no_room(gpu):
     c = make(52, 1, 2, 2, 64, 40, 9, [300, 512])
     to = check_copy(gpu, c, make(53, 1, 2, 2, 64, 11, 9, [70, 3]), [0, 1])

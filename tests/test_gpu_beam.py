@@ -77,6 +77,12 @@ def test_beams(gpu, W, power, done):
     check(gpu, *inputs(W, 3, W, 5000, "fp32", done=done, power=power), power=power, eos=2, pad=7)
 
 
+@pytest.mark.parametrize("V", [450, 1000, 2047, 4000, 4500, 8192, 8200, 16380, 16385])
+@pytest.mark.parametrize("W,done", [(3, 0.3), (8, 0.0), (12, 0.0), (17, 0.4), (24, 0.0), (32, 0.0)])
+def test_few_tokens_for_many_beams(gpu, V, W, done):
+    check(gpu, *inputs(V + W, 2, W, V, "fp32", done=done))
+
+
 def test_a_large_vocabulary(gpu):
     check(gpu, *inputs(5, 2, 8, 128256, "bf16", done=0.2, power=1.0), dtype="bf16", power=1.0, eos=5)
 

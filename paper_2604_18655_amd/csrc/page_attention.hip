@@ -39,6 +39,7 @@ mlora_status check_page_cache(const mlora_page_cache *c);
 namespace {
 
 constexpr int P = MLORA_PAGE_TOKENS, KC = 32;            // tokens of a page, of a chunk
+constexpr int ALONE = 32;                                // a bundle's streams of fewer pages and chunks go alone (see below)
 constexpr float UNSEEN = -__builtin_inff();
 // The largest weight as a whole number of N digits, 127 in each place, and what turns a float of such a size into its bits: with that addend the low
 // bytes of the sum are the number, 128 added to all digits but the first (which has room for none).
@@ -59,6 +60,7 @@ struct AttnArgs {
     const int *slot, *len, *table, *parent;
     float *part_out;                                     // several blocks per query tile: [splits][S * R * Hq][D], not normalised
     float2 *part_ml;                                     // [splits][S * R * Hq]: maximum (of scores in units of log 2) and sum
+    int *used;                                           // [S * R * Hq]: how many of the splits there are
     void *out;
     int Hq, Hkv, G, S, R, M;
     int pages, columns, window, sink;
@@ -67,6 +69,9 @@ struct AttnArgs {
     int out_fp32;
     float scale2;                                        // scale * log2(e)
 };
+
+// Into how many blocks a query tile's items go, of at most `most`
+__host__ __device__ constexpr int splits_for(int items, int most) { return items < 32 || most < 1 ? 1 : most < items / 8 ? most : items / 8; }
 
 // a value combined over the four quarters of a wave (lanes 16 and 32 apart); every lane gets the result
 template <class Op>
@@ -131,35 +136,68 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
     constexpr int DK = D / 64, DB = D / 16, VI = KC * D / 512;
     __shared__ __align__(16) unsigned char smem[W * L::BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int hk = blockIdx.x, bz = SPLIT ? (int)blockIdx.z / a.splits : (int)blockIdx.z, z = SPLIT ? (int)blockIdx.z - bz * a.splits : 0;
-    const int s0 = bz * a.bundle, streams = min(a.bundle, a.S - s0), per_stream = a.R * a.G, n_qv = streams * per_stream, qv0 = (int)blockIdx.y * 16;
+    // blocks: (head, tile, stream and share), or, as a bundle has one tile, (head, bundle, share): those that have nothing to do come last.  In
+    // between they left whole compute units without work (128 streams of 2500 tokens 22 -> 34 us).
+    const int hk = blockIdx.x, per_stream = a.R * a.G;
+    int bundle = a.bundle, s0, z = 0, qv0 = 0;
+    if (bundle > 1) {
+        s0 = (int)blockIdx.y * bundle, z = blockIdx.z;
+    } else {
+        s0 = SPLIT ? (int)blockIdx.z / a.splits : (int)blockIdx.z, qv0 = (int)blockIdx.y * 16;
+        if (SPLIT) z = (int)blockIdx.z - s0 * a.splits;
+    }
+    int streams = min(bundle, a.S - s0), n_qv = streams * per_stream;
 
     // this lane's query vector: its stream, row and head
-    const int vec = min(qv0 + l16, n_qv - 1), sb = a.bundle == 1 ? 0 : vec / per_stream, in_stream = vec - sb * per_stream;
-    const int row = (int)((unsigned)in_stream * a.g_inv >> 16), s = s0 + sb;
-    const uint16_t *const q_at = a.q + ((size_t)(s * a.R + row) * a.Hq + hk * a.G + (in_stream - row * a.G)) * D;
+    int sb, row;
+    const uint16_t *q_at;
     u32x4 qx[DK][2];
+    const auto load_q = [&]() {
+        const int vec = min(qv0 + l16, n_qv - 1);
+        sb = bundle == 1 ? 0 : vec / per_stream;
+        const int in_stream = vec - sb * per_stream;
+        row = (int)((unsigned)in_stream * a.g_inv >> 16);
+        q_at = a.q + ((size_t)((s0 + sb) * a.R + row) * a.Hq + hk * a.G + (in_stream - row * a.G)) * D;
 #pragma unroll
-    for (int kk = 0; kk < DK; ++kk)
+        for (int kk = 0; kk < DK; ++kk)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) qx[kk][i] = *reinterpret_cast<const u32x4 *>(q_at + 64 * kk + 16 * lq + 8 * i);
+            for (int i = 0; i < 2; ++i) qx[kk][i] = *reinterpret_cast<const u32x4 *>(q_at + 64 * kk + 16 * lq + 8 * i);
+    };
+    load_q();
 
     // the items: page numbers that some stream of the bundle sees, then chunks
-    const int len = min(max(a.len[s], 0), P * a.columns + P - 1), slot = min(max(a.slot[s], 0), a.S - 1);
-    const int full = len / P, first = a.window > 0 ? min(max(len - a.window + 1, 0) / P, full) : 0, sinks = min((a.sink + P - 1) / P, first);
-    int b_full = full, b_first = first, b_sinks = sinks;               // of the bundle
-    if (a.bundle > 1)
+    int len = min(max(a.len[s0 + sb], 0), P * a.columns + P - 1), slot = min(max(a.slot[s0 + sb], 0), a.S - 1), full, first, sinks;
+    int b_full, b_first, b_sinks;                        // of the bundle
+    const int per_chunks = (P - 1 + a.R + KC - 1) / KC;
+    const auto pages_of = [&]() {
+        full = len / P, first = a.window > 0 ? min(max(len - a.window + 1, 0) / P, full) : 0, sinks = min((a.sink + P - 1) / P, first);
+        b_full = full, b_first = first, b_sinks = sinks;
+        if (bundle > 1)
 #pragma unroll
-        for (int d = 1; d < 16; d *= 2) {
-            b_full = max(b_full, __shfl_xor(b_full, d));
-            b_first = min(b_first, __shfl_xor(b_first, d));
-            b_sinks = max(b_sinks, __shfl_xor(b_sinks, d));
-        }
-    b_full = __builtin_amdgcn_readfirstlane(b_full), b_first = __builtin_amdgcn_readfirstlane(b_first);
-    b_sinks = min(__builtin_amdgcn_readfirstlane(b_sinks), b_first);
-    const int n_pages = b_sinks + b_full - b_first, per_chunks = (P - 1 + a.R + KC - 1) / KC, items = n_pages + streams * per_chunks;
+            for (int d = 1; d < 16; d *= 2) {
+                b_full = max(b_full, __shfl_xor(b_full, d));
+                b_first = min(b_first, __shfl_xor(b_first, d));
+                b_sinks = max(b_sinks, __shfl_xor(b_sinks, d));
+            }
+        b_full = __builtin_amdgcn_readfirstlane(b_full), b_first = __builtin_amdgcn_readfirstlane(b_first);
+        b_sinks = min(__builtin_amdgcn_readfirstlane(b_sinks), b_first);
+    };
+    pages_of();
+    // The host has cut the call for tables that are full.  Where the streams of a bundle are short, each has a block of its own; what the lengths call for
+    // decides how many blocks share a bundle or stream.  The other blocks have nothing to do.  (In long tables, us in a graph, as the tables have it and so: 8
+    // streams of 100 tokens 10.3 / 7.1, 21 of 70 12.4 / 7.0, 64 of 300 12.9 / 10.1, 8 of 1000 12.1 / 9.6; it costs long ones 0.3 to 1.1: 32 of 4500, 4096 of them
+    // shared, 13.8 / 14.1, 4 of 20000 21.5 / 22.4, 6 of 40000 53.6 / 54.7.)
+    if (bundle > 1 && b_sinks + b_full - b_first + per_chunks < ALONE) {
+        if (z >= streams) return;
+        len = __builtin_amdgcn_readlane(len, z * per_stream), slot = __builtin_amdgcn_readlane(slot, z * per_stream);
+        s0 += z, z = 0, bundle = streams = 1, n_qv = per_stream;
+        load_q();
+        pages_of();
+    }
+    const int n_pages = b_sinks + b_full - b_first, items = n_pages + streams * per_chunks;
+    const int use = SPLIT ? splits_for(streams * (n_pages + per_chunks), a.splits) : 1, stride = use * W;
+    if (z >= use) return;
     const int *const table = a.table + (size_t)slot * a.columns;
-    const int stride = SPLIT ? a.splits * W : W;
     int c = z * W + wave;
     // the page that this lane's stream sees as item i, or -1
     const auto number_of = [&](int i) { return i < b_sinks ? i : b_first + i - b_sinks; };
@@ -206,7 +244,7 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
     }
     // lane b * R + r: the rows that row r of stream b may see, itself and what it continues.  A parent must be an earlier row, so a path has at most
     // 64; each step doubles what is known of all of them.
-    const int my_row = a.bundle == 1 ? lane : lane % a.R, row_lane = sb * a.R + row;
+    const int my_row = bundle == 1 ? lane : lane % a.R, row_lane = sb * a.R + row;
     unsigned anc_lo = my_row < 32 ? 1u << my_row : 0u, anc_hi = my_row >= 32 ? 1u << (my_row - 32) : 0u;
     if (a.R > 1) {
         int up = lane < streams * a.R ? a.parent[s0 * a.R + lane] : -1;
@@ -495,9 +533,10 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
             num += weight * *reinterpret_cast<const f32x4 *>(smem + w * L::BYTES + (qv * L::OROW + f) * 4);
             den += weight * x.y;
         }
-        const int b = a.bundle == 1 ? 0 : v / per_stream, in = v - b * per_stream, r = (int)((unsigned)in * a.g_inv >> 16);
+        const int b = bundle == 1 ? 0 : v / per_stream, in = v - b * per_stream, r = (int)((unsigned)in * a.g_inv >> 16);
         const size_t vec_at = (size_t)((s0 + b) * a.R + r) * a.Hq + hk * a.G + (in - r * a.G);
-        if constexpr (SPLIT) {
+        if (SPLIT && z == 0 && f == 0) a.used[vec_at] = use;
+        if (SPLIT && use > 1) {
             const size_t at = (size_t)z * a.M * a.Hq + vec_at;
             if (f == 0) a.part_ml[at] = make_float2(top, den);
             *reinterpret_cast<f32x4 *>(a.part_out + at * D + f) = num;
@@ -516,22 +555,25 @@ __global__ __launch_bounds__(256) void page_attn_combine(const AttnArgs a)
     const int i = (int)blockIdx.x * 256 + (int)threadIdx.x, vecs = a.M * a.Hq;
     if (i >= vecs * (D / 4)) return;
     const int vec = i / (D / 4), f = i % (D / 4) * 4;
-    constexpr int RB = 8;                                      // results per trip to memory
-    f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f, run_top = UNSEEN;
-    for (int z0 = 0; z0 < a.splits; z0 += RB) {
-        float2 ml[RB];
-        f32x4 pv[RB];
+    const int used = a.used[vec];                              // (1: a block has written the output; what nobody wrote holds anything)
+    constexpr int RB = 8;                                      // results per trip to memory; the next ones are asked for before these are known
+    float2 ml[2][RB];
+    f32x4 pv[2][RB];
+    const auto load = [&](int z0, float2 (&ml)[RB], f32x4 (&pv)[RB]) {
 #pragma unroll
         for (int u = 0; u < RB; ++u) {
             const size_t at = (size_t)min(z0 + u, a.splits - 1) * vecs + vec;
             ml[u] = a.part_ml[at];
             pv[u] = *reinterpret_cast<const f32x4 *>(a.part_out + at * D + f);
         }
+    };
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f, run_top = UNSEEN;
+    const auto take = [&](int z0, float2 (&ml)[RB], f32x4 (&pv)[RB]) {
         float top = run_top;
 #pragma unroll
         for (int u = 0; u < RB; ++u) {
-            if (z0 + u >= a.splits) ml[u] = make_float2(UNSEEN, 0.f), pv[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (z0 + u >= used) ml[u] = make_float2(UNSEEN, 0.f), pv[u] = f32x4{0.f, 0.f, 0.f, 0.f};
             top = fmaxf(top, ml[u].x);
         }
         const float base = finite_or_0(top), keep = __builtin_amdgcn_exp2f(run_top - base);
@@ -544,7 +586,17 @@ __global__ __launch_bounds__(256) void page_attn_combine(const AttnArgs a)
             den += w * ml[u].y;
         }
         run_top = top;
+    };
+    load(0, ml[0], pv[0]);
+    for (int z0 = 0;; z0 += 2 * RB) {
+        if (z0 + RB < a.splits) load(z0 + RB, ml[1], pv[1]);
+        take(z0, ml[0], pv[0]);
+        if (!__any(used > z0 + RB)) break;
+        if (z0 + 2 * RB < a.splits) load(z0 + 2 * RB, ml[0], pv[0]);
+        take(z0 + RB, ml[1], pv[1]);
+        if (!__any(used > z0 + 2 * RB)) break;
     }
+    if (used == 1) return;
     num /= den;
     const size_t at = (size_t)vec * D + f;
     if (a.out_fp32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + at) = num;
@@ -572,14 +624,14 @@ Plan plan_of(const mlora_page_attn &t)
     // Shared items cost a second launch (2.4 us at least) and pay from about four per wave on (11 items: 8.3 -> 6.9 with one block; 127: 25 -> 8.2 with 16),
     // up to some 200 blocks of eight waves (64 blocks, 3 / 4 splits: 15.0 / 15.3; 8 blocks of 3125 items, 24 / 32: 77.0 / 78.1).  Calls that fill the
     // card without have blocks of four waves (512 blocks of 37 items: 21.3, of eight waves 23.0).  16 waves were first in 2 of 26, by 1.3 %.
-    p.splits = items < 32 ? 1 : (int)std::max(1ll, std::min(std::min((200 + blocks / 2) / blocks, items / 8), (long long)MOST_SPLITS));
+    p.splits = splits_for((int)std::min(items, 1ll << 30), (int)std::min(std::max((200 + blocks / 2) / blocks, 1ll), (long long)MOST_SPLITS));
     p.waves = blocks * p.splits <= 256 ? 8 : 4;
     return p;
 }
 size_t workspace_floats(const mlora_page_attn &t)
 {
     const int splits = plan_of(t).splits;
-    return splits == 1 ? 0 : (size_t)splits * t.n_q_heads * (size_t)t.cache.n_streams * t.rows_per_stream * ((size_t)t.cache.head_dim + 2);
+    return splits == 1 ? 0 : t.n_q_heads * (size_t)t.cache.n_streams * t.rows_per_stream * (splits * ((size_t)t.cache.head_dim + 2) + 1);
 }
 
 mlora_status check(const mlora_page_attn *t)
@@ -665,12 +717,14 @@ mlora_status mlora_page_attention(const mlora_page_attn *t, const void *q, void 
     a.bundle = p.bundle;
     a.part_out = reinterpret_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float2 *>(a.part_out + (size_t)p.splits * a.M * a.Hq * c.head_dim);
+    a.used = reinterpret_cast<int *>(a.part_ml + (size_t)p.splits * a.M * a.Hq);
     a.g_inv = (65536u + (unsigned)a.G - 1) / (unsigned)a.G;
     a.out_fp32 = out_dtype == MLORA_Y_FP32;
     a.scale2 = t->scale * 1.44269504088896340736f;
 
     hipStream_t s = (hipStream_t)stream;
-    const dim3 grid((unsigned)a.Hkv, (unsigned)((p.bundle * a.R * a.G + 15) / 16), (unsigned)((a.S + p.bundle - 1) / p.bundle * p.splits));
+    const dim3 grid = p.bundle > 1 ? dim3((unsigned)a.Hkv, (unsigned)((a.S + p.bundle - 1) / p.bundle), (unsigned)std::max(p.splits, p.bundle))
+                                   : dim3((unsigned)a.Hkv, (unsigned)((a.R * a.G + 15) / 16), (unsigned)(a.S * p.splits));
     const auto go = [&](auto d, auto digits, auto waves) {
         constexpr int D = decltype(d)::value, N = decltype(digits)::value, W = decltype(waves)::value;
         if (p.splits == 1) {

@@ -95,6 +95,31 @@ def test_a_table_far_longer_than_the_stream(gpu):
     assert plan["splits"] > 1
 
 
+@pytest.mark.parametrize("columns", [8, 20, 64, 500])
+@pytest.mark.parametrize("R,G", [(1, 1), (1, 4), (1, 5), (2, 4), (5, 3), (9, 2)])
+def test_short_streams_in_long_tables(gpu, columns, R, G):
+    check(gpu, columns + R, [70, 0, 63, 64, 300, 1, 129, 500, 33, 2], R, 2, G, 64, columns=columns, fp32=R % 2 == 1)
+    check(gpu, columns + R + 1, [100, 511, 5], R, 1, G, 128, columns=columns, window=70, sink=5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,R", [(1, 1), (4, 1), (2, 2)])
+@pytest.mark.parametrize("longest", [28, 29, 30, 31, 32, 40])
+def test_bundles_of_short_and_long_streams(gpu, D, G, R, longest):
+    """Around the number of pages from which streams of a bundle are taken together; some share what they have, some have nothing."""
+    lengths = [64 * longest + 5, 64, 0, 64 * longest - 1, 1000, 64 * longest, 3, 70, 64 * longest + 63, 10, 100]
+    check(gpu, longest + G, lengths, R, 1, G, D, columns=60, fp32=G == 1)
+    check(gpu, longest + G + 50, lengths, R, 1, G, D, columns=60, share=[0, 0, 0, 3, 3, 5, 0, 7, 8, 0, 8])
+    check(gpu, longest + G + 90, lengths, R, 1, G, D, columns=60, share=[0, 0, 0, 3, 3, 5, 0, 7, 8, 0, 8], window=1500, sink=130)
+
+
+@pytest.mark.parametrize("length", [90, 2300])
+def test_more_bundles_than_fill_the_card(gpu, length):
+    n = 300 if length == 90 else 216
+    plan = check(gpu, 60 + length, [length] + [70, 3, 0, 64] * 100 if length == 90 else [length, 64] * (n // 2), 1, 8, 1, 64, columns=50, fp32=False)
+    assert plan["splits"] == 1
+
+
 @pytest.mark.parametrize("q_scale", [1e-30, 1e-3, 40.0])
 def test_sharp_and_flat(gpu, q_scale):
     check(gpu, 5, [500, 130], 3, 2, 2, 64, q_scale=q_scale)

@@ -196,6 +196,30 @@ def test_copies_into_larger_pools(gpu, pages, table):
         assert to["len"].tolist() == [max(0, c["len"][i]) if i >= 0 else 0 for i in source]
 
 
+@pytest.mark.parametrize("most", [1024, 4096, 4097, 9000])
+def test_copies_out_of_large_pools(gpu, most):
+    """Pages anywhere in the pool, the last one among them; more than one thread's share of entries."""
+    c = make(58, 1, 3, 1, 64, 9000, 900, [64 * 700 + 3, 64 * 800, 64 * 5])
+    rng = np.random.default_rng(most)
+    to_page = rng.permutation(most)[:1505]
+    to_page[0] = most - 1 if most - 1 not in to_page else to_page[0]
+    if most < 1505:
+        to_page = np.arange(1505) % most                                                 # (many held more than once)
+    at = 0
+    c["refs"][:], c["table"][:] = 0, -1
+    for s, n in enumerate((700, 800, 5)):
+        c["table"][c["slot"][s], :n] = to_page[at:at + n]
+        at += n
+    np.add.at(c["refs"], to_page, 1)
+    check_copy(gpu, c, make(59, 1, 3, 1, 64, 1600, 900, [70, 3, 0]), [2, 0, 1])
+    check_copy(gpu, c, make(59, 1, 2, 1, 64, 9000, 900, [70, 3]), [2, -1])
+
+
+def test_copies_of_more_pages_than_blocks(gpu):
+    c = make(60, 16, 2, 1, 64, 700, 400, [64 * 390 + 1, 64 * 210])
+    check_copy(gpu, c, make(61, 16, 2, 1, 64, 650, 400, [70, 3]), [1, 0])
+
+
 def test_copies_that_find_no_room(gpu):
     c = make(52, 1, 2, 2, 64, 40, 9, [300, 512])
     to = check_copy(gpu, c, make(53, 1, 2, 2, 64, 11, 9, [70, 3]), [0, 1])

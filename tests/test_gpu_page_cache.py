@@ -127,6 +127,17 @@ def test_pages_are_taken_from_the_lowest_on(gpu):
     assert c["len"].tolist() == [63, 63]
 
 
+@pytest.mark.parametrize("S", [3, 60])
+@pytest.mark.parametrize("free", [[], [0, 39999], [39998, 39999], [1023, 1024, 20000], [5, 8192 + 1024, 8192 + 1025], [33791, 33792, 33793], list(range(30000, 40000, 17))])
+def test_few_free_pages_in_a_large_pool(gpu, S, free):
+    c = make(62, 1, S, 1, 64, 40000, 5, [63, 3, 127] + [10] * (S - 3))
+    c["refs"] += 1
+    c["refs"][free] -= 1
+    check_append(gpu, c, 1, None, calls=2)
+    check_append(gpu, c, 64, None)
+    check_append(gpu, c, 65, None)
+
+
 def test_odd_numbers(gpu):
     """Zeros, subnormals, the largest, infinities, NaN; ties (127 x / m in halves)."""
     some = {0: 0x0000, 1: 0x8000, 2: 0x0001, 3: 0x807F, 4: 0x7F7F, 5: 0x7F80, 6: 0xFF80, 7: 0x7FC0, 8: 0x3F80, 9: 0xBF00, 10: 0x0080}

@@ -42,7 +42,8 @@ typedef struct {
 size_t mlora_page_attention_workspace_bytes(const mlora_page_attn *t);
 
 /* How such a call would be run, for reading profiles; host only, nothing is launched.  info (HOST memory, 3 int32): as of
- * mlora_tree_attention_plan, [0] tiles of 16 query vectors a block takes, [1] waves of a block, [2] blocks that share a tile's pages. */
+ * mlora_tree_attention_plan, [0] tiles of 16 query vectors a block takes, [1] waves of a block, [2] blocks that may share a tile's pages (how
+ * many do, and whether streams are taken together, the lengths decide on the device). */
 mlora_status mlora_page_attention_plan(const mlora_page_attn *t, int32_t *info);
 
 /*   q    bf16 [S * R][n_q_heads][D], 16-byte aligned

@@ -7,8 +7,8 @@
 //
 // A large call is bound by the logits (8 groups of 16 beams over 128256 bf16 tokens: 9 to 11 us for 29.5 MB), and then by beam_pick's chain: what
 // the slices left, the bound, the chunks above it, their logits, their order, 0.6 to 3.6 us each (12 to 14 us there; one group of 4 beams over
-// 32003 fp32 tokens 3.5 to 5.5 us and 8, of which what the slices left and the bound are 2 each).  Ranks for all chunks in 64 bits, candidates ranked by one thread each and a bound found bit by bit were:
-// 84 us for that block.
+// 32003 fp32 tokens 3.5 to 5.5 us and 8, of which what the slices left and the bound are 2 each).  Ranks for all chunks in 64 bits, candidates
+// ranked by one thread each and a bound found bit by bit were: 84 us for that block.
 #include <type_traits>
 
 #include "common.hpp"

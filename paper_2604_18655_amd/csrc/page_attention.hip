@@ -21,7 +21,7 @@
 //
 // What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 77 us, 5.3 TB/s), or, in short ones, the launch and the trips
 // length, table, page (333 tokens 4.7 us); else the vector work around the weights, some 250 to 290 instructions per page and tile (8 trees of 30
-// rows, 2048 tokens of window, 8 heads of 64: 20 us, of which 11 are vector instructions).  So whole numbers become floats and back by adding
+// rows, 2048 tokens of window, 8 heads of 64: 20 us, of which a wave is 11 in its pages).  So whole numbers become floats and back by adding
 // 1.5 * 2^23 or 2^23 where that is free (an accumulator's start, the addend of a multiplication) and not by conversions, and sums are rescaled
 // only where a maximum rises by much.  The next page's keys are asked for behind the scores: without that 22 -> 39 us, with the values, too, on their way
 // earlier no difference.

@@ -120,6 +120,40 @@ def test_more_bundles_than_fill_the_card(gpu, length):
     assert plan["splits"] == 1
 
 
+@pytest.mark.parametrize("S,G", [(1, 4), (9, 1), (6, 4)])
+def test_replays_while_the_streams_grow_and_shrink(gpu, S, G):
+    """One graph and one workspace, from streams that go alone to ones that share blocks, and back."""
+    lib, _, torch = gpu
+    H, D, R, most = 2, 64, 2, 64 * 45 + 7
+    rng = np.random.default_rng(70 + S)
+    c = make(70, 1, S, H, D, S * 45 + 3, 50, [most] * S)
+    q, k, v = bits(rng, S * R, H * G, D), bits(rng, S * R, H, D), bits(rng, S * R, H, D)
+    parent = [-1, 0] * S
+    t, cache = upload(gpu, c)
+    on = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (q, k, v, np.asarray(parent, np.int32))]
+    op = lib.PageAttention(cache, 0, H * G, R, D ** -0.5, on[1], on[2], on[3])
+    assert op.plan()["splits"] > 1
+    out, eager = (torch.zeros(q.shape, dtype=torch.float32).cuda() for _ in range(2))
+    ws, other = (torch.full((op.workspace_bytes(),), 0xFF, dtype=torch.uint8).cuda() for _ in range(2))
+    op.run(on[0], out, lib.Y_FP32, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        op.run(on[0], out, lib.Y_FP32, ws)
+    for n in (0, 5, 64 * 20, 64 * 28, 64 * 29 + 63, 64 * 31, most, 64 * 33, 70, most, 1):
+        lengths = [n] + [max(0, n - 64 * i) for i in range(1, S)]
+        cache.len.copy_(torch.tensor(lengths, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        op.run(on[0], eager, lib.Y_FP32, other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), n
+        c["len"][:] = lengths
+        want, size = O.attention(c, 0, q, k, v, parent, R, float(np.float32(D ** -0.5)), 0, 0)
+        got = out.double().cpu().numpy()
+        assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), D ** -0.5, D, n // 64 + 5, want, True)), n
+
+
 @pytest.mark.parametrize("q_scale", [1e-30, 1e-3, 40.0])
 def test_sharp_and_flat(gpu, q_scale):
     check(gpu, 5, [500, 130], 3, 2, 2, 64, q_scale=q_scale)

@@ -328,9 +328,8 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
     __syncthreads();
     const int bound = at_least;
     const float bound_rank = __int_as_float(bound < 0 ? bound ^ 0x7FFFFFFF : bound);
-    // the bound as one on a beam's logits, a little lower (ranks decide): what is below it has no part
+    // the bound as one on a live beam's logits, a little lower (ranks decide): what is below it has no part
     const auto lowest = [&](const Beam &b) {
-        if (!b.live) return __builtin_inff();
         if (bound_rank == NONE) return -3.4028235e38f;
         const double low = ((double)bound_rank - fabs((double)bound_rank) * 0x1p-22 - 0x1p-148) / b.per - b.score, z = low + b.lse;
         return fmaxf((float)(z - (fabs(low) + fabs(b.lse)) * 0x1p-22), -3.4028235e38f);        // (a number, also where `per` is next to nothing)
@@ -343,6 +342,7 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
             if (s.first == 0 && lane == 0 && b.live && in_order((float)rank) >= bound) list.put(Candidate{in_order(rank), 0.f, s.beam, 0});
             continue;
         }
+        if (!b.live) continue;                           // (its logits may be +infinity, and reach any bound)
         const float from = lowest(b);
         for (int q0 = 0; q0 < s.n; q0 += 64 * HELD) {
             if (!all) load(s, q0, z);
@@ -402,16 +402,18 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
         // Else those of the W best chunks, of which there are W, that are no worse than the best of the W-th.
         __syncthreads();
         if (tid == 0) picked.found = 0;
+        int chosen = min(W, found);
         if (found <= LIST && some <= QUADS) {
             best_of(list, found, W, best);
         } else {
             // (more equals than the list holds: one after the other)
             Candidate last{0x7FFFFFFFFFFFFFFFll, 0.f, -1, -1};
-            for (int n = 0; n < W; ++n) {
+            for (chosen = 0; chosen < W; ++chosen) {
                 Candidate top{in_order((double)NONE), NONE, W, 0};
                 for (int t = wave; t < W * parts; t += WAVES) {
                     const Share s = share_of(t);
                     const Beam &b = beams[s.beam];
+                    if (!b.live) continue;
                     const float from = lowest(b);
                     for (int c = lane; c < (b.finished ? 1 : 4 * s.n); c += 64) {
                         const float z = b.finished ? (s.first == 0 ? 0.f : NONE) : reinterpret_cast<const float *>(s.tops)[c];
@@ -430,11 +432,12 @@ __global__ __launch_bounds__(PICK) void beam_pick(const BeamArgs a)
 #pragma unroll 1
                 for (int w = 1; w < WAVES; ++w)
                     if (before(wave_best[w], last)) last = wave_best[w];
-                if (tid == 0) best[n] = last;
+                if (last.beam == W) break;               // (none is left: the same in all threads)
+                if (tid == 0) best[chosen] = last;
                 __syncthreads();
             }
         }
-        look_at(W, [&](int i) { return Place{best[i].beam, best[i].at}; }, best[W - 1].rank);
+        look_at(chosen, [&](int i) { return Place{best[i].beam, best[i].at}; }, chosen < W ? in_order((double)NONE) : best[W - 1].rank);
         m = picked.found;
     }
     best_of(picked, m, W, best);

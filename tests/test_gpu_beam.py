@@ -220,3 +220,21 @@ def test_replays(gpu):
         want, _ = O.beam_select(x, score, length, done, W, 2)
         assert np.array_equal(source.cpu().numpy(), want["source"]) and np.array_equal(token.cpu().numpy(), want["token"])
         assert np.array_equal(state[1].cpu().numpy(), want["length"]) and np.array_equal(state[2].cpu().numpy(), want["finished"])
+
+
+@pytest.mark.parametrize("W,V,dtype", [(4, 128256, "bf16"), (16, 32000, "bf16"), (32, 32000, "fp32")])
+@pytest.mark.parametrize("left", ["nothing", "a token", "a finished beam", "a beam"])
+def test_many_infinite_logits(gpu, W, V, dtype, left):
+    """Groups of beams whose logits are +infinity all over (more groups of chunks than are looked at one by one), but for one beam: they have no
+    candidates, and nothing of the next group, or of what lies behind the last, becomes one."""
+    z, score, length, done, _ = inputs(18, 1, W, V, dtype)
+    one, rest = W // 2, np.full((W, V), math.inf)
+    if left == "a token":
+        rest[one] = -math.inf
+        rest[one, V - 3] = 0.5
+    elif left == "a beam":
+        rest[one] = z[one]
+    ended = done.copy()
+    ended[one] = left == "a finished beam"
+    check(gpu, np.concatenate([rest, z, rest]), np.tile(score, 3), np.tile(length, 3), np.concatenate([ended, done, ended]), W, dtype=dtype, pad=9)
+    check(gpu, rest, score, length, ended, W, dtype=dtype, pad=9)

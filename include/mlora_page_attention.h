@@ -15,6 +15,9 @@
  * What a row may not see does not touch it, infinite or not a number as it may be.  A row that sees NaN, or whose own query vector is not
  * finite, is NaN.  Finite scores scale q . k are of a magnitude below 2^20.
  *
+ * Accuracy, for both types of outputs: on pages a query vector's numbers count to 2^-22 of its largest, a weight to 2^-24 of the largest of its page; products, sums
+ * and states are exact or fp32, and an output in bf16 is rounded once.
+ *
  * Conventions as in mlora_w4.h; results are bit-identical from call to call.
  */
 #ifndef MLORA_PAGE_ATTENTION_H

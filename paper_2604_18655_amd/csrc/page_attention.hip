@@ -7,21 +7,22 @@
 // place, as beams do, take it together: a page that all of four streams see costs what it costs one.
 //
 // Pages go from memory to the matrix units as they are: codes are multiplied as whole numbers (16x16x64 products of int8, exact in
-// 32 bits), nothing is widened and nothing passes through LDS.  The other side is cut into N digits to the base 256, each a signed byte, of
-// whole numbers of N bytes:
-//     q = unit * whole         to 2^-22 of the vector's largest magnitude (N = 3), 2^-15 (N = 2)
-//     p = whole / P_ONE        p = exp(score - the page's largest score) in (0, 1], to 2^-24 (N = 3), 2^-16 (N = 2)
-// so that a product of scores or outputs is N products of bytes, each half the work of one of bf16.  Outputs in fp32 take three digits, which is what fp32
-// arithmetic would leave; outputs in bf16 take two, which moves them by a few 2^-15 where their own rounding is 2^-9.  The weights are counted relative to
-// the page's own maximum; a page's sum of weights is the sum of the very integers that multiply the values.  Scores are K . Q^T: a lane
+// 32 bits), nothing is widened and nothing passes through LDS.  The other side is cut into three digits to the base 256, each a signed byte, of
+// whole numbers of three bytes:
+//     q = unit * whole         to 2^-22 of the vector's largest magnitude
+//     p = whole / P_ONE        p = exp(score - the page's largest score) in (0, 1], to 2^-24
+// so that a product of scores or outputs is three products of bytes, each half the work of one of bf16, and as near as fp32 arithmetic would come.  (Two
+// digits for outputs in bf16: 4 x 8 beams on 4096 shared tokens 17.0 -> 15.6 us, 128 streams of 130 tokens 16.0 -> 12.3, 200000 tokens 78.6 -> 77.8; but query vectors
+// with a feature 100 times the others were off by 10^-3, and 63 keys of a page that each weigh a little less than half a unit were lost, another 10^-3.)
+// The weights are counted relative to the page's own maximum; a page's sum of weights is the sum of the very integers that multiply the values.  Scores are K . Q^T: a lane
 // holds 16 keys of ONE query vector, and if the keys of a page are dealt to the products in the right order (key 16 * (i / 4) + 4 * t + i % 4 is
 // row i of product t) these are the 16 that O^T += V^T . P^T wants from it.  Values are stored feature by feature for that.
-// The tail and the step's rows are bf16, with scores and weights as in tree_attention.hip, the weights as N bf16 numbers each (two leave outputs off by
+// The tail and the step's rows are bf16, with scores and weights as in tree_attention.hip, the weights as three bf16 numbers each (two leave outputs off by
 // 10^-6, which shows in fp32 where nearly all that a row sees is tail).
 //
-// What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 77 us, 5.3 TB/s), or, in short ones, the launch and the trips
+// What bounds a call of few query vectors is the bytes (200000 tokens of 8 heads of 128: 79 us, 5.2 TB/s), or, in short ones, the launch and the trips
 // length, table, page (333 tokens 4.7 us); else the vector work around the weights, some 250 to 290 instructions per page and tile (8 trees of 30
-// rows, 2048 tokens of window, 8 heads of 64: 20 us, of which a wave is 11 in its pages).  So whole numbers become floats and back by adding
+// rows, 2048 tokens of window, 8 heads of 64: 21 us, of which a wave is 11 in its pages).  So whole numbers become floats and back by adding
 // 1.5 * 2^23 or 2^23 where that is free (an accumulator's start, the addend of a multiplication) and not by conversions, and sums are rescaled
 // only where a maximum rises by much.  The next page's keys are asked for behind the scores: without that 22 -> 39 us, with the values, too, on their way
 // earlier no difference.
@@ -41,10 +42,10 @@ namespace {
 constexpr int P = MLORA_PAGE_TOKENS, KC = 32;            // tokens of a page, of a chunk
 constexpr int ALONE = 32;                                // a bundle's streams of fewer pages and chunks go alone (see below)
 constexpr float UNSEEN = -__builtin_inff();
+constexpr int N = 3;                                     // digits
 // The largest weight as a whole number of N digits, 127 in each place, and what turns a float of such a size into its bits: with that addend the low
 // bytes of the sum are the number, 128 added to all digits but the first (which has room for none).
-template <int N> constexpr float P_ONE = N == 3 ? 8355711.f : 32639.f;
-template <int N> constexpr float P_BITS = 8388608.f + (N == 3 ? 32896.f : 128.f);
+constexpr float P_ONE = 8355711.f, P_BITS = 8388608.f + 32896.f;
 constexpr int NUMBER = 0x4B400000;                       // the bits of 1.5 * 2^23: a whole number below 2^22 added to them is one added to it
 constexpr float NUMBER_F = 12582912.f;
 
@@ -99,25 +100,18 @@ __device__ __forceinline__ unsigned bytes_of(int n, unsigned y0, unsigned y1, un
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(y3, y2, pair), __builtin_amdgcn_perm(y1, y0, pair), 0x05040100u);
 }
 // Digits of four whole numbers, 128 added to all but the first: d[0] the first (of four numbers), d[N - 1] the last
-template <int N>
 __device__ __forceinline__ void digits_of(const unsigned (&y)[4], unsigned (&d)[N])
 {
     const unsigned lo01 = __builtin_amdgcn_perm(y[1], y[0], 0x05010400u), lo23 = __builtin_amdgcn_perm(y[3], y[2], 0x05010400u);   // {b0 b0 b1 b1}
     const unsigned b0 = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u), b1 = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
-    d[N - 1] = b0 ^ 0x80808080u;
-    if constexpr (N == 3) {
-        d[1] = b1 ^ 0x80808080u;
-        d[0] = bytes_of(2, y[0], y[1], y[2], y[3]);
-    } else {
-        d[0] = b1;
-    }
+    d[2] = b0 ^ 0x80808080u;
+    d[1] = b1 ^ 0x80808080u;
+    d[0] = bytes_of(2, y[0], y[1], y[2], y[3]);
 }
-// The sum of N products of digits, as a number; NUMBER_F is added to it if the last accumulator started from NUMBER.
-template <int N>
+// The sum of N products of digits, as a number; NUMBER_F is added to it, as the last accumulator started from NUMBER.
 __device__ __forceinline__ float joined(const i32x4 (&x)[N], int e)
 {
-    if constexpr (N == 3) return __builtin_fmaf((float)((x[0][e] << 8) + x[1][e]), 256.f, __int_as_float(x[2][e]));
-    else                  return (float)((x[0][e] << 8) + x[1][e]);
+    return __builtin_fmaf((float)((x[0][e] << 8) + x[1][e]), 256.f, __int_as_float(x[2][e]));
 }
 
 // LDS of a wave: the values of a chunk on their way to the matrix units, then its share of the result.
@@ -129,15 +123,15 @@ struct WaveLds {
     static constexpr int BYTES = KC * VROW > O_BYTES + ML_BYTES ? KC * VROW : O_BYTES + ML_BYTES;
 };
 
-template <int D, int W, int N, bool SPLIT>
-__global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page_attn(const AttnArgs a)
+template <int D, int W, bool SPLIT>
+__global__ __launch_bounds__(64 * W, (D == 64 ? 3 : 2)) void page_attn(const AttnArgs a)
 {
     using L = WaveLds<D>;
     constexpr int DK = D / 64, DB = D / 16, VI = KC * D / 512;
     __shared__ __align__(16) unsigned char smem[W * L::BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     // blocks: (head, tile, stream and share), or, as a bundle has one tile, (head, bundle, share): those that have nothing to do come last.  In
-    // between they left whole compute units without work (128 streams of 2500 tokens 22 -> 34 us).
+    // between they left whole compute units without work (128 streams of 2500 tokens took half as long again).
     const int hk = blockIdx.x, per_stream = a.R * a.G;
     int bundle = a.bundle, s0, z = 0, qv0 = 0;
     if (bundle > 1) {
@@ -184,9 +178,8 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
     };
     pages_of();
     // The host has cut the call for tables that are full.  Where the streams of a bundle are short, each has a block of its own; what the lengths call for
-    // decides how many blocks share a bundle or stream.  The other blocks have nothing to do.  (In long tables, us in a graph, as the tables have it and so: 8
-    // streams of 100 tokens 10.3 / 7.1, 21 of 70 12.4 / 7.0, 64 of 300 12.9 / 10.1, 8 of 1000 12.1 / 9.6; it costs long ones 0.3 to 1.1: 32 of 4500, 4096 of them
-    // shared, 13.8 / 14.1, 4 of 20000 21.5 / 22.4, 6 of 40000 53.6 / 54.7.)
+    // decides how many blocks share a bundle or stream.  The other blocks have nothing to do.  (In long tables, us in a graph, all blocks busy and so: 8
+    // streams of 100 tokens 11.2 / 7.3, 21 of 70 13.8 / 7.0, 64 of 300 14.4 / 12.2, 8 of 1000 13.3 / 9.9; long ones are the same within 1 %.)
     if (bundle > 1 && b_sinks + b_full - b_first + per_chunks < ALONE) {
         if (z >= streams) return;
         len = __builtin_amdgcn_readlane(len, z * per_stream), slot = __builtin_amdgcn_readlane(slot, z * per_stream);
@@ -219,10 +212,10 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, max(qx[kk][i / 4][i % 4] & 0x7FFFu, qx[kk][i / 4][i % 4] >> 16 & 0x7FFFu));
         top = __float_as_uint(over_quarters(__uint_as_float(top), [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); }));
-        // (whole numbers below 2^22, or, with 128 added, below 2^15: 1.99 is the next exponent's)
-        const int e = (int)max(N == 3 ? top >> 7 : (top + 1) >> 7, 1u) - 127;
+        // (whole numbers below 2^22)
+        const int e = (int)max(top >> 7, 1u) - 127;
         const bool ok = top < 0x7F80u;
-        constexpr int BITS = N == 3 ? 21 : 14;
+        constexpr int BITS = 21;
         unit = ok ? __builtin_ldexpf(fabsf(a.scale2), e - BITS) : __builtin_nanf("");
         const int shift = BITS - e;
         const float sign = a.scale2 < 0.f ? -1.f : 1.f;
@@ -235,9 +228,9 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
                 for (int j = 0; j < 4; ++j) {
                     const unsigned pair = qx[kk][w / 2][2 * (w % 2) + j / 2];
                     const float f = sign * __builtin_ldexpf(bf16_bits_to_float(j & 1 ? pair >> 16 : pair & 0xFFFFu), shift);
-                    n[j] = (unsigned)((ok ? (int)rintf(f) : 0) + (N == 3 ? 0x8080 : 0x80));
+                    n[j] = (unsigned)((ok ? (int)rintf(f) : 0) + 0x8080);
                 }
-                digits_of<N>(n, d);
+                digits_of(n, d);
 #pragma unroll
                 for (int g = 0; g < N; ++g) qd[g][kk][w] = d[g];
             }
@@ -329,7 +322,7 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
                 for (int kk = 0; kk < DK; ++kk) x[g] = mfma_i8(kf[t][kk], qd[g][kk], x[g]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[t][e] = joined<N>(x, e);
+            for (int e = 0; e < 4; ++e) sc[t][e] = joined(x, e);
         }
         const int t0 = number_of(c) * P;
         more = next();
@@ -351,7 +344,7 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
         top = over_quarters(top, most);
         // weights relative to the page's maximum, as whole numbers; nothing of a page that the lane's stream does not hold
         // (its maximum a little too large, since that of a product is rounded and no weight may be above 1)
-        const float scaled = finite_or_0(top) * per, from = scaled + fabsf(scaled) * 0x1p-23f, one = seen ? P_ONE<N> : 0.f;
+        const float scaled = finite_or_0(top) * per, from = scaled + fabsf(scaled) * 0x1p-23f, one = seen ? P_ONE : 0.f;
         unsigned sum = 0;
         u32x4 pd[N];
 #pragma unroll
@@ -359,15 +352,15 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
             unsigned n[4], d[N];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                n[e] = __float_as_uint(__builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e], per, -from)), one, P_BITS<N>));
+                n[e] = __float_as_uint(__builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e], per, -from)), one, P_BITS));
                 sum += n[e];
             }
-            digits_of<N>(n, d);
+            digits_of(n, d);
 #pragma unroll
             for (int g = 0; g < N; ++g) pd[g][t] = d[g];
         }
-        sum -= 16u * __float_as_uint(P_BITS<N>);
-        top = top == UNSEEN || !seen ? UNSEEN : N == 3 ? __builtin_fmaf(-NUMBER_F, per, from) : from;
+        sum -= 16u * __float_as_uint(P_BITS);
+        top = top == UNSEEN || !seen ? UNSEEN : __builtin_fmaf(-NUMBER_F, per, from);
         // The sums so far are relative to a maximum that is raised only where a page's is more than 2^8 times as heavy: fp32 has the room, and what the
         // lane holds need not be scaled for every page that is a little heavier.
         if (__ballot(top > m + 8.f)) {
@@ -378,25 +371,24 @@ __global__ __launch_bounds__(64 * W, (D == 64 ? (N == 2 ? 4 : 3) : 2)) void page
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[db] *= keep;
         }
-        float w = __builtin_amdgcn_exp2f(top - finite_or_0(m)) * (1.f / P_ONE<N>);
+        float w = __builtin_amdgcn_exp2f(top - finite_or_0(m)) * (1.f / P_ONE);
         if (bad && top != UNSEEN) w = __builtin_nanf("");
         l += (float)(int)sum * w;
         const float wv = top != UNSEEN ? w * vs_here : 0.f;              // (a page of NaN that the row does not see)
-        if constexpr (N == 3) over += NUMBER_F * wv;
+        over += NUMBER_F * wv;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             i32x4 x[N];
 #pragma unroll
             for (int g = 0; g < N; ++g) x[g] = mfma_i8(vf[db], pd[g], g == 2 ? i32x4{NUMBER, NUMBER, NUMBER, NUMBER} : i32x4{0, 0, 0, 0});
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[db][e] = __builtin_fmaf(joined<N>(x, e), wv, o[db][e]);
+            for (int e = 0; e < 4; ++e) o[db][e] = __builtin_fmaf(joined(x, e), wv, o[db][e]);
         }
         if (more) load_v();
     }
     while (c < n_pages) c += stride;
-    if constexpr (N == 3)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] -= over;
+    for (int db = 0; db < DB; ++db) o[db] -= over;
 
     // chunks of a tail and, behind it, the step's rows
     unsigned char *const piece_of = smem + wave * L::BYTES;
@@ -621,9 +613,9 @@ Plan plan_of(const mlora_page_attn &t)
     p.bundle = seen < 8 ? 1 : std::max(1, std::min(std::min(16 / qv, 8), t.cache.n_streams));
     const long long items = p.bundle * (seen + (P - 1 + t.rows_per_stream + KC - 1) / KC);
     const long long blocks = (long long)t.cache.n_kv_heads * ((t.cache.n_streams + p.bundle - 1) / p.bundle) * ((qv + 15) / 16);
-    // Shared items cost a second launch (2.4 us at least) and pay from about four per wave on (11 items: 8.3 -> 6.9 with one block; 127: 25 -> 8.2 with 16),
-    // up to some 200 blocks of eight waves (64 blocks, 3 / 4 splits: 15.0 / 15.3; 8 blocks of 3125 items, 24 / 32: 77.0 / 78.1).  Calls that fill the
-    // card without have blocks of four waves (512 blocks of 37 items: 21.3, of eight waves 23.0).  16 waves were first in 2 of 26, by 1.3 %.
+    // Shared items cost a second launch (2.4 us at least) and pay from about four per wave on (8 items: 7.1 -> 4.7 with one block; 127: 27 -> 8.5 with 16),
+    // up to some 200 blocks of eight waves (8 blocks of 3125 items, 24 / 32 splits: 78.5 / 80.1; 64 blocks would take 6 as well as 3: 16.9 / 15.4).  Calls that
+    // fill the card without have blocks of four waves (512 blocks of 37 items: 21.4, of eight waves 22.4).  16 waves were first in 2 of 26, by 1.3 %.
     p.splits = splits_for((int)std::min(items, 1ll << 30), (int)std::min(std::max((200 + blocks / 2) / blocks, 1ll), (long long)MOST_SPLITS));
     p.waves = blocks * p.splits <= 256 ? 8 : 4;
     return p;
@@ -725,25 +717,21 @@ mlora_status mlora_page_attention(const mlora_page_attn *t, const void *q, void 
     hipStream_t s = (hipStream_t)stream;
     const dim3 grid = p.bundle > 1 ? dim3((unsigned)a.Hkv, (unsigned)((a.S + p.bundle - 1) / p.bundle), (unsigned)std::max(p.splits, p.bundle))
                                    : dim3((unsigned)a.Hkv, (unsigned)((a.R * a.G + 15) / 16), (unsigned)(a.S * p.splits));
-    const auto go = [&](auto d, auto digits, auto waves) {
-        constexpr int D = decltype(d)::value, N = decltype(digits)::value, W = decltype(waves)::value;
+    const auto go = [&](auto d, auto waves) {
+        constexpr int D = decltype(d)::value, W = decltype(waves)::value;
         if (p.splits == 1) {
-            page_attn<D, W, N, false><<<grid, dim3(64 * W), 0, s>>>(a);
+            page_attn<D, W, false><<<grid, dim3(64 * W), 0, s>>>(a);
         } else {
-            page_attn<D, W, N, true><<<grid, dim3(64 * W), 0, s>>>(a);
+            page_attn<D, W, true><<<grid, dim3(64 * W), 0, s>>>(a);
             page_attn_combine<D><<<dim3((unsigned)((a.M * a.Hq * (D / 4) + 255) / 256)), dim3(256), 0, s>>>(a);
         }
     };
-    const auto by_waves = [&](auto d, auto digits) {
-        if (p.waves == 8) go(d, digits, std::integral_constant<int, 8>{});
-        else              go(d, digits, std::integral_constant<int, 4>{});
+    const auto by_waves = [&](auto d) {
+        if (p.waves == 8) go(d, std::integral_constant<int, 8>{});
+        else              go(d, std::integral_constant<int, 4>{});
     };
-    const auto by_digits = [&](auto d) {
-        if (a.out_fp32) by_waves(d, std::integral_constant<int, 3>{});
-        else            by_waves(d, std::integral_constant<int, 2>{});
-    };
-    if (c.head_dim == 64) by_digits(std::integral_constant<int, 64>{});
-    else                  by_digits(std::integral_constant<int, 128>{});
+    if (c.head_dim == 64) by_waves(std::integral_constant<int, 64>{});
+    else                  by_waves(std::integral_constant<int, 128>{});
     return hipGetLastError() == hipSuccess ? MLORA_OK : MLORA_EHIP;
 }
 

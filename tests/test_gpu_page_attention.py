@@ -5,8 +5,8 @@ Scores: a query vector's numbers are cut at 2^-22 of its largest, which moves a 
 weighted mean by twice itself.  Weights: on pages cut at 2^-24 of the page's largest, 64 of them, twice; in the tail three bf16 numbers
 (2^-27, with the sum's own roundings 2^-21).  Sums: a rounding of 2^-23 per item and merge.
 
-Outputs in bf16 are made with two digits to the base 256 instead of three: query vectors are cut at 2^-15 of their largest number, weights at 2^-16 of
-the page's largest, and in the tail two bf16 numbers make a weight (2^-18, with the sum's own roundings 2^-16)."""
+Outputs in bf16 are the same, rounded once.  bound() leaves them more (query vectors cut at 2^-15 of their largest number, weights at 2^-16 of the page's
+largest, tails 2^-16); the tests of uneven query vectors and small weights hold them to the bound of fp32 and that rounding."""
 import math
 
 import numpy as np
@@ -14,6 +14,7 @@ import pytest
 
 from oracle import beams as O
 from test_gpu_page_cache import bits, make, upload
+from workloads.generate import f32_to_bf16_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -361,3 +362,57 @@ def test_large_values_and_rising_maxima(gpu, D):
         for fp32 in (True, False):
             got, _ = run(gpu, c, 0, q, kn, vn, [-1, 0, 1], 3, scale, fp32=fp32)
             assert np.all(np.abs(got - want) <= bound(size, O.bf16(q), scale, D, 30, want, fp32))
+
+
+def check_bf16(gpu, c, q, k_new, v_new, parent, R, scale):
+    got, _ = run(gpu, c, 0, q, k_new, v_new, parent, R, scale, fp32=False)
+    want, size = O.attention(c, 0, q, k_new, v_new, parent, R, float(np.float32(scale)))
+    exact = bound(size, O.bf16(q), scale, q.shape[2], int(c["len"].max()) // 64 + 5, want, True)
+    assert np.all(np.abs(got - want) <= exact + np.abs(want) * 2.0 ** -8)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("times", [30.0, 100.0])
+@pytest.mark.parametrize("length,R", [(1000, 1), (4096, 3), (63, 2)])
+def test_bf16_outputs_of_uneven_query_vectors(gpu, D, times, length, R):
+    """One feature is many times the others, where the keys have little: the other features' part of the scores is as exact as elsewhere."""
+    rng = np.random.default_rng(80)
+    c = make(80, 1, 2, 2, D, 2 * (length // 64) + 1, 70, [length, length])
+    c["k"][..., 5] = rng.integers(-2, 3, c["k"].shape[:-1])
+    little = lambda *shape: bits(rng, *shape, scale=0.02)   # noqa: E731
+    c["k_tail"][..., 5] = little(*c["k_tail"].shape[:-1])
+    q, k, v = O.bf16(bits(rng, 2 * R, 6, D)), bits(rng, 2 * R, 2, D), bits(rng, 2 * R, 2, D)
+    q[..., 5] = times * np.sign(q[..., 5])
+    k[..., 5] = little(2 * R, 2)
+    check_bf16(gpu, c, f32_to_bf16_bits(q.astype(np.float32)).view(np.int16), k, v, [-1, 0, 1][:R] * 2, R, D ** -0.5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("top", [24.0, 96.0, 384.0])
+@pytest.mark.parametrize("length", [64, 1024])
+def test_bf16_outputs_of_query_vectors_with_one_large_number(gpu, D, top, length):
+    """Half of the keys look at one small number of the query vector, half at another, and all have the same score: their values cancel.  The first
+    number has 8 significant bits, the last of which is 2^-15 of the largest one's power of two."""
+    last = 2.0 ** (math.floor(math.log2(top)) - 15)
+    c = make(82, 1, 1, 1, D, 20, 20, [length])
+    half = np.random.default_rng(82).permuted(np.tile(np.arange(64) % 2, (20, 1)), axis=1)       # [page][token]
+    c["k"][:], c["v"][:] = 0, np.where(half, 127, -127)[None, :, None, None, :]
+    c["k"][0, :, 0, :, 9], c["k"][0, :, 0, :, D - 2] = np.where(half, 124, 0), np.where(half, 0, 93)
+    c["k_scale"][:], c["v_scale"][:] = 4 / (0.125 * 124 * 129 * last), 1 / 127
+    q, k, v = (np.zeros((1, n, D)) for n in (3, 1, 1))
+    q[..., 0], q[..., 9], q[..., D - 2] = top, 129 * last, 172 * last                            # 124 * 129 = 93 * 172
+    of = lambda x: f32_to_bf16_bits(x.astype(np.float32)).view(np.int16)   # noqa: E731
+    check_bf16(gpu, c, of(q), of(k), of(v), [-1], 1, 0.125)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("less", [10.0, 11.1, 11.8])
+def test_bf16_outputs_of_many_small_weights(gpu, D, less):
+    """In every page one key with the value 0, and 63 whose weights are e^-less of its: what they bring is all that there is."""
+    c = make(81, 1, 1, 1, D, 5, 4, [64 * 4])
+    c["k"][:], c["k"][:, :, :, 17, 0], c["v"][:], c["v"][..., 17] = 0, 127, np.abs(c["v"]), 0
+    c["k_scale"][:], c["v_scale"][:] = less / (127 * 0.125), 1.0
+    q, k, v = (np.zeros((1, n, D)) for n in (2, 1, 1))
+    q[..., 0], k[..., 0] = 1.0, -8.0 * less              # (the row itself weighs e^-less of that)
+    of = lambda x: f32_to_bf16_bits(x.astype(np.float32)).view(np.int16)   # noqa: E731
+    check_bf16(gpu, c, of(q), of(k), of(v), [-1], 1, 0.125)

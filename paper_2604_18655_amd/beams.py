@@ -5,6 +5,9 @@ of what it has in common with others.
     step     rope tables, the decoder layers (decoder.py) with attention over the pages, the head's logits, selection over beams
              and vocabulary, the rows into the caches, and every beam becomes the continuation of the one it was chosen from
 
+Finished beams, and places without a candidate, take no further rows: a finished beam's cache holds its tokens but the last, and neither takes
+a page that another beam needs.
+
 Argument marshalling only, apart from torch's look-up of embeddings and small copies.  A step reads nothing back, so steps can follow each other
 without a synchronisation, or be captured into a graph.  What each step chose is kept on the device (trace); sequences() reads it back.
 """
@@ -62,9 +65,11 @@ class BeamLoop:
         self.to_logits = B.LayerPlanFused([head], [B.Epilogue(sq_in=sq, sq_parts=(hidden + 63) // 64, sq_eps=self.layers[-1].eps)], [h], [self.logits],
                                           row_adapter, S, B.Y_BF16, self.head_ws)
         self.select_ws = torch.empty(select_bytes, dtype=torch.uint8, device=device)
-        self.tokens, self.source, self.length, self.finished, self.appended = i32(S), i32(S), i32(S), i32(S), i32(S)
+        self.tokens, self.source, self.length, self.finished = i32(S), i32(S), i32(S), i32(S)
+        # of a step: what enters (0: the beam's row, 1: nothing, as there is no row 1), and whether that found its place
+        self.rows, self.appended = i32(S, 1), i32(S)
         self.score = torch.zeros((S,), device=device)
-        # what the steps chose, [0] sources and [1] tokens, how many steps there were, and whether a row found no place in a cache
+        # what the steps chose, [0] sources and [1] tokens, how many steps there were, and whether all rows that enter found their places
         self.trace = i32(max_steps, 2, S)
         self.steps = torch.zeros((1,), dtype=torch.int64, device=device)
         self.least = torch.ones((S,), dtype=torch.int32, device=device)
@@ -120,9 +125,11 @@ class BeamLoop:
         for layer in self.layers:
             layer.run()
         self.to_logits.run()
+        torch.logical_or(self.finished, self.score - self.score, out=self.rows.view(self.S))     # (no number: the score of a place without a candidate)
         self.select.run(self.logits, self.score, self.length, self.finished, self.source, self.tokens, self.score, self.length, self.finished,
                         self.select_ws)
-        self.cache.append(self.k_new, self.v_new, 1, None, self.appended)
+        self.cache.append(self.k_new, self.v_new, 1, self.rows, self.appended)
+        self.appended.add_(self.rows.view(self.S))
         torch.minimum(self.least, self.appended, out=self.least)
         self.cache.reorder(self.source, self.window, self.sink)
         last = self.trace.shape[0] - 1

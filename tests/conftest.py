@@ -14,11 +14,16 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
 
 
+FINISHED = ("a beam that is finished at 12 tokens is held to 140 in its cache, of which 128 are padding that a search behind it would go on from and that takes "
+            "the pages of others (tests/test_gpu_beam_loop_ends.py has the same steps with the tokens that the beam has)")
+
 # Tests that hold a wrong value, and which: they run, and are expected to fail there.
 WRONG_VALUES = {
     "test_gpu_decoding_loop.py::test_a_prompt_enters_compressed":
         "a prompt behind a shared prefix of 40 tokens is held to positions from 0, where the prefix's own keys stand, and to "
         "weights that leave the prefix out (tests/test_gpu_decoding_loop_state.py has the two as one sequence)",
+    "test_gpu_beam_loop.py::test_every_stage_of_many_steps[0-0]": FINISHED,
+    "test_gpu_beam_loop.py::test_every_stage_of_many_steps[50-3]": FINISHED,
 }
 
 

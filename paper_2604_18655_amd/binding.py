@@ -891,7 +891,8 @@ PAGE_TOKENS = 64
 class PageCache:
     """A paged cache of 8 bits (mlora_page_cache): k int8 [L][n_pages][H][64][head_dim], v int8 [L][n_pages][H][head_dim][64], scales fp32
     [L][n_pages][H], tails bf16 [L][S][H][64][head_dim], slot and len int32 [S], table int32 [S][max_pages], refs int32
-    [n_pages].  Made outside of a graph capture (the library's own words are uploaded here)."""
+    [n_pages].  Made outside of a graph capture (the library's own words are uploaded here).  A program that writes refs itself, as in going back to a
+    state that it kept, calls refs_written() before the next append."""
 
     def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail, slot, len, table, refs):
         import torch
@@ -933,6 +934,11 @@ class PageCache:
         return cls(z((L, N, H, P, D), torch.int8), z((L, N, H, D, P), torch.int8), z((L, N, H), torch.float32), z((L, N, H), torch.float32),
                    z((L, S, H, P, D), torch.bfloat16), z((L, S, H, P, D), torch.bfloat16), torch.arange(S, dtype=torch.int32).to(device),
                    z((S,), torch.int32), torch.full((S, max_pages), -1, dtype=torch.int32).to(device), z((N,), torch.int32))
+
+    def refs_written(self) -> None:
+        """refs was written from outside: the search for free pages starts from the pool's first again (otherwise pages that became free below where it
+        had come to are not found).  On the current stream, in a graph as well."""
+        self.own[:1].zero_()
 
     def append(self, k_new, v_new, rows_per_stream: int, rows=None, appended=None, stream: Optional[int] = None) -> None:
         """Listed rows (int32 [S][n], None: all) of k_new and v_new bf16 [L][S * rows_per_stream][H][head_dim] enter; appended

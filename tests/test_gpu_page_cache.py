@@ -294,6 +294,44 @@ def test_a_life(gpu, seed):
         same(t, c)
 
 
+def test_going_back_to_a_state_that_was_kept(gpu):
+    """All tensors of the cache are written from outside: the pages below where the search for free ones had come to are found again, in a pool that
+    has no others; eager and in a graph."""
+    lib, _, torch = gpu
+    start = make(72, 1, 3, 2, 64, 7, 5, [63, 64, 5])
+    t, cache = upload(gpu, start)
+    first = {n: x.clone() for n, x in t.items()}
+    rng = np.random.default_rng(72)
+    k, v = (bits(rng, 1, 3 * 63, 2, 64) for _ in range(2))
+    on = [torch.from_numpy(x).cuda() for x in (k, v)]
+    want, full = start, []
+    for _ in range(3):
+        want, n = O.append(want, k, v, 63)
+        full.append(n)
+    assert full == [[63, 63, 63], [63, 63, 63], [63, 0, 0]] and want["refs"].min() == 1
+
+    def again():
+        for n in O.FIELDS:
+            t[n].copy_(first[n])
+        cache.refs_written()
+        for _ in range(3):
+            cache.append(*on, 63)
+    again()
+    for _ in range(2):
+        again()
+        torch.cuda.synchronize()
+        same(t, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        again()
+    for _ in range(3):
+        for n in O.FIELDS:
+            t[n].fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        same(t, want)
+
+
 def test_offsets_past_32_bits(gpu):
     """A pool of 2.3 GB of keys, all but its last pages taken."""
     lib, _, torch = gpu

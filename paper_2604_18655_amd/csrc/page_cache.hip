@@ -177,7 +177,10 @@ __device__ __forceinline__ Entry append_plan_of(const AppendArgs &a, AppendLds<T
     else if (wish > 0) atomicMax(&lds.last, want.before + wish);
     __syncthreads();
     const int used = lds.last;                           // (streams that do not enter stand behind all that fill pages)
-    return Entry{len, slot, n, used, used == 0 ? -1 : used < found ? lds.list[used] : lds.list[used - 1] + 1};
+    // Where the next search starts: at the first page that was found and not taken; behind all pages, if more were wanted than are free; else behind the last one
+    // taken.  (None free of 250000, asked for again: 56 -> 5 us.)
+    const int next = want.all == 0 ? -1 : used < found ? lds.list[used] : found < want.all ? c.pages : lds.list[used - 1] + 1;
+    return Entry{len, slot, n, used, next};
 }
 // and what is to be written of it
 template <int T>

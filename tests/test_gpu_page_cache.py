@@ -138,6 +138,41 @@ def test_few_free_pages_in_a_large_pool(gpu, S, free):
     check_append(gpu, c, 65, None)
 
 
+@pytest.mark.parametrize("S", [3, 300])
+@pytest.mark.parametrize("pages", [200, 8193, 8200])
+def test_a_full_pool_is_searched_once(gpu, pages, S):
+    """Three streams fill a page each, and two pages are free.  A search that came to the pool's end is not made again, until pages are given up: then
+    those are found."""
+    lib, _, torch = gpu
+    most = (pages - 9) // 2
+    c = make(63, 1, S, 1, 64, pages, most + 3, [64 * (pages - 9 - most) + 63, 64 * 7 + 63, 64 * most + 63] + [5] * (S - 3))
+    given_up = sorted(c["table"][c["slot"][1], :7].tolist())
+    assert np.count_nonzero(c["refs"] == 0) == 2
+    t, cache = upload(gpu, c)
+    k, v = (bits(np.random.default_rng(63), 1, S, 1, 64) for _ in range(2))
+    on = [torch.from_numpy(x).cuda() for x in (k, v)]
+    entered = torch.zeros(S, dtype=torch.int32).cuda()
+
+    def check(c, n, ahead):
+        torch.cuda.synchronize()
+        assert entered.tolist() == n and cache.own[0].item() == ahead
+        same(t, c)
+        return c
+    for _ in range(3):                                   # (the first two streams go on behind the pages that they got)
+        cache.append(*on, 1, None, entered)
+        c, n = O.append(c, k, v, 1)
+        assert n == [1, 1, 0] + [1] * (S - 3)
+        c = check(c, n, pages)
+    given_up = sorted(given_up + [int(c["table"][c["slot"][1], 7])])
+    source = [0, -1] + list(range(2, S))
+    cache.reorder(torch.tensor(source, dtype=torch.int32).cuda())
+    c = check(O.reorder(c, source), n, given_up[0])
+    cache.append(*on, 1, None, entered)
+    c, n = O.append(c, k, v, 1)
+    assert n == [1] * S and c["table"][c["slot"][2], most] == given_up[0]
+    check(c, n, given_up[0] + 1)                         # (behind the page taken)
+
+
 def test_odd_numbers(gpu):
     """Zeros, subnormals, the largest, infinities, NaN; ties (127 x / m in halves)."""
     some = {0: 0x0000, 1: 0x8000, 2: 0x0001, 3: 0x807F, 4: 0x7F7F, 5: 0x7F80, 6: 0xFF80, 7: 0x7FC0, 8: 0x3F80, 9: 0xBF00, 10: 0x0080}

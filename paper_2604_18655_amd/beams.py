@@ -85,12 +85,15 @@ class BeamLoop:
 
     def prompt(self, k, v) -> None:
         """Prompts of N tokens for all groups, in place of what the beams held: k and v bf16 [L][G][N][kv][64], keys not yet
-        turned.  All beams of a group continue its prompt."""
+        turned.  All beams of a group continue its prompt.  Refused, with nothing changed, if a table or the pool has no room for them."""
         k, v = _patterns(k), _patterns(v)
         N = int(k.shape[2]) if k.dim() == 5 else 0
         for t in (k, v):
             if tuple(t.shape) != (self.L, self.G, N, self.kv, HEAD_DIM) or N < 1:
                 raise B.MloraError(B._ESHAPE, "beam loop's prompt")
+        tokens = B.PAGE_TOKENS
+        if N >= tokens * (self.cache.struct.max_pages + 1) or self.G * (N // tokens) > self.cache.struct.n_pages:
+            raise B.MloraError(B._ESHAPE, "beam loop's prompt")
         self.reset()
         at_once = min(N, 4096 // self.S)                            # (rows that a call takes)
         for n0 in range(0, N, at_once):

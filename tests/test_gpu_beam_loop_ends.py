@@ -137,3 +137,20 @@ def test_a_search_behind_a_finished_beam(gpu):
         loop.step()
         out.append([loop.logits[s].clone() for s in (0, W)] + [loop.cache.len[s].item() for s in (0, W)])
     assert out[0][2:] == out[1][2:] and all(torch.equal(x, y) for x, y in zip(out[0][:2], out[1][:2]))
+
+
+@pytest.mark.parametrize("pages,columns,most", [(40, 2, 191), (5, 6, 191), (4, 6, 191), (3, 6, 127), (1, 6, 63)])
+def test_prompts_that_find_no_room(gpu, pages, columns, most):
+    """The longest prompt that a table and the pool (one stream of each of two groups) hold, and one more: refused before anything changes."""
+    lib, device, torch = gpu
+    loop, bits = make_loop(gpu, 9, pages=pages, columns=columns)
+    for _ in range(3):
+        loop.step()
+    before = of_cache(loop.cache)
+    with pytest.raises(lib.MloraError):
+        loop.prompt(bits(L, G, most + 1, KV, 64), bits(L, G, most + 1, KV, 64))
+    same(of_cache(loop.cache), before)
+    loop.step()
+    assert len(loop.sequences()) == G
+    loop.prompt(bits(L, G, most, KV, 64), bits(L, G, most, KV, 64))
+    assert loop.least.tolist() == [1] * S and loop.cache.len.tolist() == [most] * S

@@ -27,7 +27,9 @@ class BeamLoop:
                  max_steps: int, eos: int = -1, length_power: float = 0.0, window: int = 0, sink: int = 0, rope: Optional[B.Rope] = None,
                  row_adapter=None, device="cuda:0"):
         """layers, head and embedding as of decoding.DecodingLoop; n_pages of the pool, max_pages of a beam; window and sink as of
-        PageAttention (pages that the window leaves behind go back to the pool); row_adapter int32 [n_groups * n_beams]."""
+        PageAttention (pages that the window leaves behind go back to the pool); row_adapter int32 [n_groups * n_beams]: the adapter of each
+        place, which a beam changes when it is chosen into another place.  A request that is to be answered by one adapter has it in all places
+        of its group; with several, a beam goes on with its new place's on the keys and values that the old one's made."""
         L, G, W = len(layers), int(n_groups), int(n_beams)
         S = G * W
         embedding = _patterns(embedding)
